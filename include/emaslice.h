@@ -504,6 +504,112 @@ int slice_copy_blocks_series(void* ring_base, uint32_t ring_slots, uint64_t slot
                              uint64_t n_total, uint32_t per_launch, uint64_t block_bytes, int32_t scatter, uint32_t kind,
                              uint32_t ctas, void* stream);
 
+/* ---- Device-driven path ------------------------------------------------------------------------
+ * The calls above keep block tables on the host and build a work list per batch. The ones below read
+ * everything that changes from step to step (lengths, tables, free block ids, slots) from device memory
+ * and are one kernel launch each, so that a whole serving step can be captured in a CUDA graph and
+ * replayed while the requests grow, come and go. They use the same block format, table entries and two
+ * arenas, need no slice_t, keep no state and allocate nothing. (The paper has no counterpart: its serving
+ * engine builds tables on the host, Section 5.1.)
+ *   - Only what the host can see is returned as a code (SLICE_EINVAL before anything is enqueued, ECUDA when
+ *     the launch fails). What only the kernel can see is written to `status`, a device word that may be
+ *     NULL: SLICE_EINVAL, SLICE_ENOSPC or SLICE_ETIMEOUT. The kernels never write 0 there: the caller
+ *     clears the word, and reads it when it likes.
+ *   - The device of the call's memory must be current, and `stream` belong to it (EINVAL / ECUDA).
+ *   - Strides: bytes for rows of elements, multiples of 16; entries for tables, at least max_blocks. Pointers to
+ *     elements (arenas, q, k, v, out, workspace) are 16-byte aligned.
+ *   - Workspaces must not be in use by two calls at a time (calls on streams without an order between them, or
+ *     two captured graphs that may run together, need one each); calls in stream order may share one.
+ *   - Ids of a pool that are taken from a slice_t belong to a sequence of that slice which the caller
+ *     allocated for the purpose (slice_alloc_blocks); slice_reclaim rewrites that sequence's host table only,
+ *     so hand the ids back first. */
+
+/* One layer's cache. blocks[0] blocks in the arena of entries e >= 0, blocks[1] in that of entries e < 0
+ * (the lent part, or a staging slot; 0 and NULL when there is none). block = K plane
+ * [block_tokens][num_kv_heads][head_dim], then the V plane, in the swizzled order of the block format. */
+typedef struct {
+  uint32_t dtype;                         /* 0 = bf16, 1 = fp16                                   */
+  uint32_t num_kv_heads;                  /* 1..64                                                */
+  uint32_t head_dim;                      /* 64, 128 or 256                                       */
+  uint32_t block_tokens;                  /* 16, 32 or 64                                         */
+  uint32_t blocks[2];
+  void* base[2];                          /* device; the layer's block 0                          */
+  uint64_t block_stride[2];               /* bytes, a multiple of 16; 0 = dense                   */
+} paged_cache_t;
+
+/* Free block ids on the device: two stacks (first arena, second arena) with the top at the end. */
+typedef struct {
+  int32_t* ids[2];                        /* [capacity]; NULL when the capacity is 0              */
+  uint32_t capacity[2];
+  const int32_t* free_in;                 /* [2] ids on each stack before the call                */
+  int32_t* free_out;                      /* [2] and after it; may be the same array as free_in  */
+  uint32_t* work;                         /* a word that is 0 before the first call; every call
+                                             leaves it 0                                         */
+} paged_pool_t;
+
+#define PAGED_NO_SLOT INT64_MIN
+
+/* Block tables and slot maps from request lengths. Request i holds lens[i] tokens in the blocks
+ * tables[i][0 .. ceil(lens[i] / block_tokens)) and is to hold new_lens[i]:
+ *   growing     the blocks it lacks are popped (request order, then logical order; the first arena's stack
+ *               until it is empty, then the second one's, whose entries are complements) and written
+ *               to its table;
+ *   shrinking   (0 = finished) the blocks it no longer needs are pushed, requests and logical blocks in
+ *               descending order, each on its arena's stack: taking back what one call grew restores
+ *               stacks and tops exactly. They can be popped from the next call on;
+ *   its new tokens lens[i] .. new_lens[i] - 1 come, in request order, to
+ *               offsets[i] .. offsets[i + 1] - 1 of the token arrays: positions[t] is the token's position,
+ *               slots[t] = block * block_tokens + row, or the complement of that for the second arena.
+ *               slots and positions past offsets[nseq] become PAGED_NO_SLOT and -1.
+ * Table cells of other blocks are left alone. offsets [nseq + 1]; slots, positions [max_tokens].
+ * Status: EINVAL (a length below 0 or above max_blocks * block_tokens, more new tokens than max_tokens,
+ * a stack's top outside its capacity), ENOSPC (too few free ids): then nothing has changed, free_out is
+ * free_in, and all offsets are 0. EINVAL also when ids pushed would exceed a stack's capacity: those are dropped.
+ * Returns EINVAL (NULL, block_tokens), ECUDA. */
+int paged_build_tables(const paged_pool_t* pool, const int32_t* lens, const int32_t* new_lens, uint32_t nseq, uint32_t block_tokens,
+                       int32_t* tables, uint64_t table_stride, uint32_t max_blocks, int32_t* offsets, int64_t* slots, int32_t* positions,
+                       uint32_t max_tokens, int32_t* status, void* stream);
+
+/* K and V rows [ntok][num_kv_heads][head_dim] of new tokens (canonical order; strides between tokens) into the
+ * blocks their slots name. PAGED_NO_SLOT skips a row. Slots must be distinct: of two equal ones, each
+ * 16 bytes of the row may come from either. Status: EINVAL (a slot outside its arena: the row is skipped).
+ * Returns EINVAL, ECUDA. */
+int paged_write_kv(const paged_cache_t* cache, const void* k, uint64_t k_stride, const void* v, uint64_t v_stride, const int64_t* slots,
+                   uint32_t ntok, int32_t* status, void* stream);
+
+/* Bytes of workspace that the two calls below need for num_q_rows query rows per sequence (num_q_heads, or twice
+ * num_heads for the differential form), independent of batch and lengths. Before its first use the
+ * workspace's first 1024 bytes must be 0; every call leaves them 0. */
+int paged_decode_workspace(const paged_cache_t* cache, uint32_t num_q_rows, uint64_t* out_bytes);
+
+/* Attention of one new token per sequence: for query head h (KV head h / G, G = num_q_heads / num_kv_heads in 1..16)
+ *   out[i][h] = softmax(sm_scale * q[i][h] K^T) V over positions max(0, len - window) .. len - 1
+ * (window 0: all), read through tables[i]; cells of blocks without such a position are not read.
+ *   q, out   [nseq] rows of [num_q_heads][head_dim], q_stride / out_stride bytes apart
+ *   lse      [nseq][num_q_heads] f32 (natural-log sum of exponentials), or NULL
+ * A sequence of length 0 gets zeros and minus infinity. What block tails hold does not matter; the rows of V that are
+ * attended to must be finite. Arithmetic: 16-bit products, f32 accumulation and softmax, result rounded once.
+ * The result does not depend on timing. Status: EINVAL (length below 0 or above max_blocks * block_tokens: zeros, like
+ * an empty sequence; an entry outside its arena: reads as zeros, the row is not meaningful).
+ * Returns EINVAL, ESCRATCH (workspace too small), ECUDA. */
+int paged_decode_tables(const paged_cache_t* cache, const int32_t* tables, uint64_t table_stride, uint32_t max_blocks, const int32_t* lens,
+                        uint32_t nseq, const void* q, uint64_t q_stride, uint32_t num_q_heads, float sm_scale, uint32_t window, void* out,
+                        uint64_t out_stride, float* lse_or_null, void* workspace, uint64_t workspace_bytes, int32_t* status, void* stream);
+
+/* Differential attention of one new token per sequence: two softmax maps over the same values, the second one
+ * subtracted with a learned weight. With D = head_dim, d = D / 2, the K plane's heads are pairs: head g of the cache
+ * holds K1 in its first d elements and K2 in the others; V heads are D wide. For head h (KV head
+ * h / G, G = num_heads / num_kv_heads in 1..8), q1 = q[i][2h], q2 = q[i][2h + 1]:
+ *   x = softmax(sm_scale * q1 K1^T) V - lam[h] * softmax(sm_scale * q2 K2^T) V
+ *   out[i][h] = out_scale * x, or out_scale * x / sqrt(mean(x^2) + eps) * norm_weight when that is given.
+ *   q        [nseq] rows of [2 * num_heads][d]; out [nseq] rows of [num_heads][D]
+ *   lam      [num_heads] f32, norm_weight [D] f32 (device)
+ * Everything else as in paged_decode_tables (zeros for an empty sequence). */
+int paged_decode_diff(const paged_cache_t* cache, const int32_t* tables, uint64_t table_stride, uint32_t max_blocks, const int32_t* lens,
+                      uint32_t nseq, const void* q, uint64_t q_stride, uint32_t num_heads, const float* lam, float sm_scale, uint32_t window,
+                      const float* norm_weight_or_null, float eps, float out_scale, void* out, uint64_t out_stride, void* workspace,
+                      uint64_t workspace_bytes, int32_t* status, void* stream);
+
 const char* slice_strerror(int code);
 
 #ifdef __cplusplus

@@ -24,6 +24,8 @@ FLAG_TEST_WITHHOLD_Q, FLAG_TEST_FAIL_COPY = 8, 16      # test hooks (see include
 COPY_DEFAULT, COPY_VECTOR, COPY_BULK, COPY_BULK_SHARED = 0, 1, 2, 3
 LAYOUT_LAYER_MAJOR, LAYOUT_SLAB_MAJOR, LAYOUT_LAYER_GROUP_MAJOR = 0, 1, 2
 TAKE_ALL = 0xFFFFFFFF
+PAGED_NO_SLOT = -(1 << 63)
+PAGED_POOL_WORK_BYTES = 4                              # PagedPool's work word (zero before the first call)
 
 EXPORTS = [
     "slice_create", "slice_destroy", "slice_alloc_blocks", "slice_set_seq_len", "slice_free_seq",
@@ -34,6 +36,7 @@ EXPORTS = [
     "slice_set_peer_used", "slice_schedule_gll",
     "slice_step_begin", "slice_step_submit_q", "slice_step_wait_out", "slice_step_flags", "slice_step_relay",
     "slice_copy_blocks_series",
+    "paged_build_tables", "paged_write_kv", "paged_decode_workspace", "paged_decode_tables", "paged_decode_diff",
 ]
 
 
@@ -81,6 +84,20 @@ class SlicePreemptStats(C.Structure):
         return {n: int(getattr(self, n)) for n, _ in self._fields_}
 
 
+class PagedCacheDesc(C.Structure):
+    _fields_ = [
+        ("dtype", C.c_uint32), ("num_kv_heads", C.c_uint32), ("head_dim", C.c_uint32), ("block_tokens", C.c_uint32),
+        ("blocks", C.c_uint32 * 2), ("base", C.c_void_p * 2), ("block_stride", C.c_uint64 * 2),
+    ]
+
+
+class PagedPoolDesc(C.Structure):
+    _fields_ = [
+        ("ids", C.c_void_p * 2), ("capacity", C.c_uint32 * 2), ("free_in", C.c_void_p), ("free_out", C.c_void_p),
+        ("work", C.c_void_p),
+    ]
+
+
 _lib = None
 
 
@@ -126,6 +143,13 @@ def lib() -> C.CDLL:
         L.slice_cta_trace.argtypes = [vp, i32, vp, u64, vp, vp]
         L.slice_copy_blocks.argtypes = [vp, vp, vp, vp, u32, u64, u32, u32, vp]
         L.slice_copy_blocks_series.argtypes = [vp, u32, u64, vp, vp, u64, u32, u64, i32, u32, u32, vp]
+        pc, f32 = C.POINTER(PagedCacheDesc), C.c_float
+        L.paged_build_tables.argtypes = [C.POINTER(PagedPoolDesc), vp, vp, u32, u32, vp, u64, u32, vp, vp, vp, u32, vp, vp]
+        L.paged_write_kv.argtypes = [pc, vp, u64, vp, u64, vp, u32, vp, vp]
+        L.paged_decode_workspace.argtypes = [pc, u32, C.POINTER(u64)]
+        L.paged_decode_tables.argtypes = [pc, vp, u64, u32, vp, u32, vp, u64, u32, f32, u32, vp, u64, vp, vp, u64, vp, vp]
+        L.paged_decode_diff.argtypes = [pc, vp, u64, u32, vp, u32, vp, u64, u32, vp, f32, u32, vp, f32, f32, vp, u64, vp, u64,
+                                        vp, vp]
         L.slice_strerror.argtypes = [C.c_int]
         L.slice_strerror.restype = C.c_char_p
         _lib = L
@@ -420,3 +444,141 @@ def slice_schedule_gll(slices) -> int:
     if rc != OK:
         raise SliceError(rc, "slice_schedule_gll")
     return int(out.value)
+
+
+# -- device-driven path: torch tensors in, one launch per call ---------------------------------------
+
+def _need(ok: bool, what: str):
+    if not ok:
+        raise ValueError(what)
+
+
+def _words(t, name: str, device, dtype: str = "torch.int32", shape=None):
+    """Address of a dense array of whole numbers (or f32) on `device`."""
+    _need(str(t.dtype) == dtype and t.is_contiguous() and t.device == device and (shape is None or tuple(t.shape) == shape),
+          f"{name}: expected a contiguous {dtype} tensor on {device}" + (f" of shape {shape}" if shape is not None else ""))
+    return t.data_ptr()
+
+
+def _row_stride(t, name: str, device, dtype, rows: int, cols: int):
+    """Byte stride between the entries of a [n][rows][cols] tensor whose inner two dimensions are dense."""
+    _need(t.dim() == 3 and t.dtype == dtype and t.device == device and t.shape[1] == rows and t.shape[2] == cols,
+          f"{name}: expected [n][{rows}][{cols}] of {dtype} on {device}, got {tuple(t.shape)} of {t.dtype} on {t.device}")
+    s = t.stride()
+    _need((s[2] == 1 or cols == 1) and (s[1] == cols or rows == 1), f"{name}: the inner two dimensions have to be contiguous")
+    return (s[0] if t.shape[0] > 1 else rows * cols) * 2
+
+
+class PagedCache:
+    """One layer's paged cache: arenas of blocks [blocks][2][block_tokens][num_kv_heads][head_dim] in bf16 or fp16 (block format:
+    see kv_block_swizzle), entries e >= 0 of a table naming `local`'s block e, entries e < 0 `lent`'s block ~e. Blocks may be
+    further apart than their size (first stride); the rest is dense. Holds the two tensors, nothing else."""
+
+    def __init__(self, local, lent=None):
+        parts = [t for t in (local, lent) if t is not None and t.shape[0] > 0]
+        _need(bool(parts), "a cache needs at least one block")
+        ref = parts[0]
+        kinds = {"torch.bfloat16": 0, "torch.float16": 1}
+        d = PagedCacheDesc()
+        for j, t in enumerate((local, lent)):
+            if t is None or t.shape[0] == 0:
+                continue
+            _need(t.dim() == 5 and t.shape[1] == 2 and tuple(t.shape[1:]) == tuple(ref.shape[1:]) and t.dtype == ref.dtype
+                  and t.device == ref.device and str(t.dtype) in kinds, "arenas: [blocks][2][block_tokens][num_kv_heads][head_dim], "
+                  "bf16 or fp16, alike in both")
+            _need(t[0].is_contiguous(), "arenas: blocks have to be dense")
+            d.blocks[j], d.base[j] = t.shape[0], t.data_ptr()
+            d.block_stride[j] = t.stride(0) * 2 if t.shape[0] > 1 else 0
+        d.dtype, d.block_tokens, d.num_kv_heads, d.head_dim = kinds[str(ref.dtype)], ref.shape[2], ref.shape[3], ref.shape[4]
+        self.desc, self._ref = d, C.byref(d)
+        self.local, self.lent = local, lent
+        self.dtype, self.device = ref.dtype, ref.device
+        self.block_tokens, self.num_kv_heads, self.head_dim = ref.shape[2], ref.shape[3], ref.shape[4]
+
+
+class PagedPool:
+    """Free block ids on the device: two stacks of int32 (top at the end; `lent_ids` may be None), their counts before (`free`) and
+    after a call (`free_out`, may be the same tensor), int32 [2] each, and a zeroed work word of PAGED_POOL_WORK_BYTES."""
+
+    def __init__(self, local_ids, lent_ids, free, free_out, work):
+        dev = free.device
+        d = PagedPoolDesc()
+        for j, t in enumerate((local_ids, lent_ids)):
+            if t is not None and t.numel():
+                d.ids[j], d.capacity[j] = _words(t, "ids", dev), t.numel()
+        d.free_in, d.free_out = _words(free, "free", dev, shape=(2,)), _words(free_out, "free_out", dev, shape=(2,))
+        _need(work.is_contiguous() and work.device == dev and work.numel() * work.element_size() >= PAGED_POOL_WORK_BYTES,
+              "work: PAGED_POOL_WORK_BYTES on the pool's device")
+        d.work = work.data_ptr()
+        self.desc, self._ref, self.device = d, C.byref(d), dev
+        self._keep = (local_ids, lent_ids, free, free_out, work)
+
+
+def _table(tables, n: int, device):
+    _need(tables.dim() == 2 and str(tables.dtype) == "torch.int32" and tables.device == device and tables.shape[0] == n
+          and (tables.stride(1) == 1 or tables.shape[1] == 1), f"tables: expected int32 [{n}][max_blocks] on {device}, rows contiguous")
+    return tables.data_ptr(), (tables.stride(0) if n > 1 else tables.shape[1]), tables.shape[1]
+
+
+def _status(status, device):
+    return None if status is None else _words(status, "status", device, shape=(1,))
+
+
+def paged_build_tables(pool: PagedPool, lens, new_lens, block_tokens: int, tables, offsets, slots, positions, status=None,
+                       stream=None) -> int:
+    dev, n = pool.device, lens.numel()
+    tab, stride, width = _table(tables, n, dev)
+    _need(slots.numel() == positions.numel(), "slots and positions are of one length")
+    return lib().paged_build_tables(pool._ref, _words(lens, "lens", dev), _words(new_lens, "new_lens", dev, shape=(n,)), n, block_tokens,
+                                    tab, stride, width, _words(offsets, "offsets", dev, shape=(n + 1,)),
+                                    _words(slots, "slots", dev, "torch.int64"), _words(positions, "positions", dev), slots.numel(),
+                                    _status(status, dev), _stream(stream))
+
+
+def paged_write_kv(cache: PagedCache, k, v, slots, status=None, stream=None) -> int:
+    dev, h, d = cache.device, cache.num_kv_heads, cache.head_dim
+    ks, vs = _row_stride(k, "k", dev, cache.dtype, h, d), _row_stride(v, "v", dev, cache.dtype, h, d)
+    _need(k.shape[0] == v.shape[0] == slots.numel(), "k, v and slots are of one length")
+    return lib().paged_write_kv(cache._ref, k.data_ptr(), ks, v.data_ptr(), vs, _words(slots, "slots", dev, "torch.int64"), k.shape[0],
+                                _status(status, dev), _stream(stream))
+
+
+def paged_decode_workspace(cache: PagedCache, num_q_rows: int) -> int:
+    """Bytes of workspace (zeroed by the caller before its first use) for num_q_rows query rows: num_q_heads, or twice num_heads for
+    the differential form."""
+    out = C.c_uint64(0)
+    rc = lib().paged_decode_workspace(cache._ref, num_q_rows, C.byref(out))
+    if rc != OK:
+        raise SliceError(rc, "paged_decode_workspace")
+    return int(out.value)
+
+
+def _workspace(work, device):
+    _need(work.is_contiguous() and work.device == device, "workspace: a contiguous tensor on the cache's device")
+    return work.data_ptr(), work.numel() * work.element_size()
+
+
+def paged_decode_tables(cache: PagedCache, tables, lens, q, sm_scale: float, out, workspace, lse=None, window: int = 0, status=None,
+                        stream=None) -> int:
+    dev, n, heads, d = cache.device, lens.numel(), q.shape[1], cache.head_dim
+    qs, os_ = _row_stride(q, "q", dev, cache.dtype, heads, d), _row_stride(out, "out", dev, cache.dtype, heads, d)
+    _need(q.shape[0] == out.shape[0] == n and window >= 0, "q, out and lens are of one length, a window is 0 or more")
+    tab, stride, width = _table(tables, n, dev)
+    ws, wb = _workspace(workspace, dev)
+    return lib().paged_decode_tables(cache._ref, tab, stride, width, _words(lens, "lens", dev), n, q.data_ptr(), qs, heads, sm_scale, window,
+                                     out.data_ptr(), os_, None if lse is None else _words(lse, "lse", dev, "torch.float32", (n, heads)),
+                                     ws, wb, _status(status, dev), _stream(stream))
+
+
+def paged_decode_diff(cache: PagedCache, tables, lens, q, lam, sm_scale: float, out, workspace, norm_weight=None, eps: float = 1e-5,
+                      out_scale: float = 1.0, window: int = 0, status=None, stream=None) -> int:
+    dev, n, heads, d = cache.device, lens.numel(), out.shape[1], cache.head_dim
+    qs = _row_stride(q, "q", dev, cache.dtype, 2 * heads, d // 2)
+    os_ = _row_stride(out, "out", dev, cache.dtype, heads, d)
+    _need(q.shape[0] == out.shape[0] == n and window >= 0, "q, out and lens are of one length, a window is 0 or more")
+    tab, stride, width = _table(tables, n, dev)
+    ws, wb = _workspace(workspace, dev)
+    return lib().paged_decode_diff(cache._ref, tab, stride, width, _words(lens, "lens", dev), n, q.data_ptr(), qs, heads,
+                                   _words(lam, "lam", dev, "torch.float32", (heads,)), sm_scale, window,
+                                   None if norm_weight is None else _words(norm_weight, "norm_weight", dev, "torch.float32", (d,)),
+                                   eps, out_scale, out.data_ptr(), os_, ws, wb, _status(status, dev), _stream(stream))

@@ -10,6 +10,8 @@ namespace ema {
 
 // Value written to the device status word when a bounded wait expires.
 constexpr int kDevTimeout = -6;
+// Values that the device-driven operators write to their caller's status word.
+constexpr int kStatusInvalid = -1, kStatusNoSpace = -2;
 
 // One batched block copy: item i moves block_bytes from src(entry src_entry[i]) to
 // dst(entry dst_entry[i]) for each of nlayers layers. An entry e >= 0 addresses id e of base[0],
@@ -215,5 +217,77 @@ struct AppendParams {
   uint32_t block_tokens;
 };
 cudaError_t launch_append(const AppendParams& p, cudaStream_t stream);
+
+// paged_tables.cu: block tables and slot maps from request lengths (see paged_build_tables).
+struct BuildTablesParams {
+  int32_t* ids[2];             // free stacks, top at the end
+  uint32_t capacity[2];
+  const int32_t* free_in;      // [2] ids on each stack; free_out may be the same array
+  int32_t* free_out;
+  uint32_t* work;              // ticket word, zero before and after
+  const int32_t* lens;         // [nseq]
+  const int32_t* new_lens;
+  uint32_t nseq;
+  uint32_t block_shift;        // log2(tokens per block)
+  int32_t* tables;             // row i at i * table_stride entries
+  uint64_t table_stride;
+  uint32_t max_blocks;
+  int32_t* offsets;            // [nseq + 1]
+  int64_t* slots;              // [max_tokens]
+  int32_t* positions;
+  uint32_t max_tokens;
+  int* status;
+};
+cudaError_t launch_build_tables(const BuildTablesParams& p, int num_sms, cudaStream_t stream);
+
+// paged_tables.cu: rows of new tokens into their blocks (see paged_write_kv).
+struct WriteKvParams {
+  uint8_t* base[2];
+  uint64_t block_stride[2];
+  uint32_t blocks[2];
+  uint32_t block_shift;
+  uint32_t row_bytes;          // num_kv_heads * head_dim * 2
+  const uint8_t* k;            // [ntok] rows, strides in bytes
+  const uint8_t* v;
+  uint64_t k_stride, v_stride;
+  const int64_t* slots;
+  uint32_t ntok;
+  int* status;
+  uint32_t units, lane_shift;  // filled in by the launch
+};
+cudaError_t launch_write_kv(WriteKvParams p, cudaStream_t stream);
+
+// paged_decode.cu: attention of one token per sequence through device tables (see paged_decode_tables and
+// paged_decode_diff). The tensor maps are made by the launch.
+constexpr uint32_t kPagedMaxCtas = 256;         // most CTAs; arrival counters at the start of the workspace
+struct PagedDecodeParams {
+  uint8_t* base[2];
+  uint64_t block_stride[2];
+  uint32_t blocks[2];
+  uint32_t dtype;              // 0 bf16, 1 fp16
+  uint32_t num_kv_heads, head_dim, block_tokens;
+  const int32_t* tables;
+  uint64_t table_stride;       // entries
+  uint32_t max_blocks;
+  const int32_t* lens;
+  uint32_t nseq;
+  const uint8_t* q;            // rows of a sequence contiguous, q_stride bytes to the next sequence
+  uint64_t q_stride;
+  uint32_t rows;               // query rows per KV head: G, or 2 G for the differential form (two maps, interleaved)
+  uint32_t window;             // 0: the whole length
+  float scale_log2;
+  uint8_t* out;
+  uint64_t out_stride;         // bytes
+  float* lse;                  // [nseq][heads] or NULL
+  uint32_t* counters;          // [kPagedMaxCtas], zero before and after
+  float* part_o;               // [2 * CTAs][rows][head_dim]
+  float* part_ml;              // [2 * CTAs][rows][2]
+  const float* lam;            // differential form: [heads]; NULL otherwise
+  const float* norm_weight;    // [head_dim] or NULL
+  float eps, out_scale;
+  int* status;
+};
+size_t paged_workspace_bytes(uint32_t rows, uint32_t head_dim);
+cudaError_t launch_paged_decode(const PagedDecodeParams& p, int num_sms, cudaStream_t stream);
 
 }  // namespace ema

@@ -1,0 +1,365 @@
+// paged_tables.cu — the bookkeeping half of the device-driven path: block tables and slot maps built on
+// the GPU from request lengths (build_tables_kernel) and the scatter of new K/V rows through such a slot
+// map (write_kv_kernel).
+//
+// build_tables_kernel. With T tokens per block, request i going from a to b tokens needs
+// max(0, ceil(b/T) - ceil(a/T)) blocks; the k-th block needed (request order, then logical order) is the
+// k-th id popped: ids0[free0 - 1 - k], and once the first stack is empty ids1[free1 - 1 - (k - free0)],
+// whose table entry is the complement. New token t of the batch belongs to the request with
+// offsets[i] <= t < offsets[i + 1], at position a + t - offsets[i]. Both prefix sums are over the
+// requests, a few KB: every CTA computes them for itself (no CTA waits for another one) and fills its
+// share of the token slots; the thread that fills the first token of a new block writes the block's table
+// entry. Only the stacks' new tops and the blocks that shrinking requests give back must wait until every
+// CTA has read the old ones: the CTA that draws the last ticket does both.
+// Bound by latency: launch, one read of the lengths, the block-wide scan, one read of a table or
+// stack entry, the stores.
+#include "kernels.h"
+#include "ptx.cuh"
+
+namespace ema {
+
+namespace {
+
+constexpr uint32_t kBuildThreads = 512;
+constexpr uint32_t kBuildWarps = kBuildThreads / 32;
+constexpr uint32_t kBuildTokens = 2048;          // token slots of one CTA's step; at most that many requests have tokens in them
+constexpr int64_t kNoSlot = INT64_MIN;
+
+struct Sums {
+  long long add, need, gone;  // tokens, blocks popped, blocks given back
+};
+
+__device__ __forceinline__ Sums plus(const Sums& a, const Sums& b) { return {a.add + b.add, a.need + b.need, a.gone + b.gone}; }
+
+__device__ __forceinline__ Sums shfl_up(const Sums& a, int d) {
+  return {__shfl_up_sync(0xffffffffu, a.add, d), __shfl_up_sync(0xffffffffu, a.need, d), __shfl_up_sync(0xffffffffu, a.gone, d)};
+}
+
+// Exclusive prefix of v over the CTA's threads, and the total.
+__device__ Sums block_exclusive(const Sums& v, Sums* warp_sums, Sums& total) {
+  const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x >> 5;
+  Sums inc = v;
+#pragma unroll
+  for (int d = 1; d < 32; d <<= 1) {
+    const Sums o = shfl_up(inc, d);
+    if (lane >= static_cast<uint32_t>(d)) inc = plus(inc, o);
+  }
+  __syncthreads();  // the array may still be read from an earlier call
+  if (lane == 31) warp_sums[warp] = inc;
+  __syncthreads();
+  Sums before = {0, 0, 0}, all = {0, 0, 0};
+#pragma unroll
+  for (uint32_t w = 0; w < kBuildWarps; ++w) {
+    if (w == warp) before = all;
+    all = plus(all, warp_sums[w]);
+  }
+  total = all;
+  return {before.add + inc.add - v.add, before.need + inc.need - v.need, before.gone + inc.gone - v.gone};
+}
+
+__device__ uint32_t block_exclusive_u32(uint32_t v, uint32_t* warp_sums, uint32_t& total) {
+  const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x >> 5;
+  uint32_t inc = v;
+#pragma unroll
+  for (int d = 1; d < 32; d <<= 1) {
+    const uint32_t o = __shfl_up_sync(0xffffffffu, inc, d);
+    if (lane >= static_cast<uint32_t>(d)) inc += o;
+  }
+  __syncthreads();
+  if (lane == 31) warp_sums[warp] = inc;
+  __syncthreads();
+  uint32_t before = 0, all = 0;
+#pragma unroll
+  for (uint32_t w = 0; w < kBuildWarps; ++w) {
+    if (w == warp) before = all;
+    all += warp_sums[w];
+  }
+  total = all;
+  return before + inc - v;
+}
+
+__device__ __forceinline__ uint32_t blocks_of(int32_t tokens, uint32_t shift) {
+  return (static_cast<uint32_t>(tokens) + (1u << shift) - 1) >> shift;
+}
+
+__device__ __forceinline__ Sums sums_of(int32_t a, int32_t b, uint32_t shift) {
+  const uint32_t ob = blocks_of(a, shift), nb = blocks_of(b, shift);
+  return {b > a ? b - a : 0, nb > ob ? static_cast<long long>(nb - ob) : 0, ob > nb ? static_cast<long long>(ob - nb) : 0};
+}
+
+// A request with new tokens among those of the CTA's step.
+struct Entry {
+  uint32_t seq, offset, first;  // batch position, its first new token, its first popped block
+  int32_t old_len;
+};
+
+__global__ void __launch_bounds__(kBuildThreads) build_tables_kernel(const BuildTablesParams p) {
+  __shared__ Sums warp_sums[kBuildWarps];
+  __shared__ uint32_t warp_u32[kBuildWarps];
+  __shared__ Entry list[kBuildTokens];
+  __shared__ uint32_t last_cta;
+  __shared__ uint32_t gone_after[kBuildThreads];
+  const uint32_t tid = threadIdx.x, lane = tid & 31u, warp = tid >> 5;
+  const uint32_t shift = p.block_shift, mask = (1u << shift) - 1;
+
+  // Every thread owns a run of requests.
+  const uint32_t run = (p.nseq + kBuildThreads - 1) / kBuildThreads;
+  const uint32_t r0 = min(tid * run, p.nseq), r1 = min(r0 + run, p.nseq);
+  const long long room = static_cast<long long>(p.max_blocks) << shift;
+  const int32_t free0 = p.free_in[0], free1 = p.free_in[1];
+  Sums mine = {0, 0, 0};
+  bool bad = free0 < 0 || free1 < 0 || static_cast<uint32_t>(free0) > p.capacity[0] || static_cast<uint32_t>(free1) > p.capacity[1];
+  for (uint32_t i = r0; i < r1; ++i) {
+    const int32_t a = p.lens[i], b = p.new_lens[i];
+    if (a < 0 || b < 0 || a > room || b > room)
+      bad = true;
+    else
+      mine = plus(mine, sums_of(a, b, shift));
+  }
+  bad = __syncthreads_or(bad);
+  Sums total;
+  const Sums before = block_exclusive(mine, warp_sums, total);
+  int code = 0;
+  if (bad || total.add > static_cast<long long>(p.max_tokens))
+    code = kStatusInvalid;
+  else if (total.need > static_cast<long long>(free0) + free1)
+    code = kStatusNoSpace;
+  const uint32_t tokens = code ? 0 : static_cast<uint32_t>(total.add);
+
+  if (blockIdx.x == 0) {
+    uint32_t at = code ? 0 : static_cast<uint32_t>(before.add);
+    for (uint32_t i = r0; i < r1; ++i) {
+      p.offsets[i] = static_cast<int32_t>(at);
+      if (!code) at += static_cast<uint32_t>(sums_of(p.lens[i], p.new_lens[i], shift).add);
+    }
+    if (tid == 0) {
+      p.offsets[p.nseq] = static_cast<int32_t>(tokens);
+      if (code) ptx::report_status(p.status, code);
+    }
+  }
+
+  for (uint64_t t0 = static_cast<uint64_t>(blockIdx.x) * kBuildTokens; t0 < p.max_tokens; t0 += static_cast<uint64_t>(gridDim.x) * kBuildTokens) {
+    const uint32_t lo = static_cast<uint32_t>(t0), hi = min(lo + kBuildTokens, p.max_tokens);
+    uint32_t entries = 0;
+    if (lo < tokens) {
+      // The requests with tokens in [lo, hi), in order.
+      uint32_t count = 0;
+      Sums at = before;
+      const bool near = before.add < hi && before.add + mine.add > lo;
+      if (near)
+        for (uint32_t i = r0; i < r1; ++i) {
+          const Sums s = sums_of(p.lens[i], p.new_lens[i], shift);
+          count += s.add > 0 && at.add < hi && at.add + s.add > lo;
+          at = plus(at, s);
+        }
+      uint32_t slot = block_exclusive_u32(count, warp_u32, entries);
+      if (count) {
+        at = before;
+        for (uint32_t i = r0; i < r1; ++i) {
+          const int32_t a = p.lens[i];
+          const Sums s = sums_of(a, p.new_lens[i], shift);
+          if (s.add > 0 && at.add < hi && at.add + s.add > lo)
+            list[slot++] = {i, static_cast<uint32_t>(at.add), static_cast<uint32_t>(at.need), a};
+          at = plus(at, s);
+        }
+      }
+      __syncthreads();
+    }
+    for (uint32_t t = lo + tid; t < hi; t += kBuildThreads) {
+      int64_t slot = kNoSlot;
+      int32_t pos = -1;
+      if (t < tokens) {
+        uint32_t b = 0, e = entries;  // the last entry whose offset is <= t
+        while (e - b > 1) {
+          const uint32_t m = (b + e) >> 1;
+          if (list[m].offset <= t)
+            b = m;
+          else
+            e = m;
+        }
+        const Entry en = list[b];
+        pos = en.old_len + static_cast<int32_t>(t - en.offset);
+        const uint32_t block = static_cast<uint32_t>(pos) >> shift, held = blocks_of(en.old_len, shift);
+        int32_t* cell = p.tables + static_cast<uint64_t>(en.seq) * p.table_stride + block;
+        int32_t entry;
+        if (block < held) {
+          entry = *cell;
+        } else {
+          const uint32_t k = en.first + block - held;
+          entry = k < static_cast<uint32_t>(free0) ? p.ids[0][free0 - 1 - k] : ~p.ids[1][free1 - 1 - (k - static_cast<uint32_t>(free0))];
+          if ((static_cast<uint32_t>(pos) & mask) == 0) *cell = entry;
+        }
+        const uint32_t row = static_cast<uint32_t>(pos) & mask;
+        slot = entry >= 0 ? (static_cast<int64_t>(entry) << shift) + row : ~((static_cast<int64_t>(~entry) << shift) + row);
+      }
+      p.slots[t] = slot;
+      p.positions[t] = pos;
+    }
+    __syncthreads();  // the list is filled again
+  }
+
+  // The rest happens once, after every CTA has read the stacks and their tops.
+  if (gridDim.x > 1) {
+    __threadfence();
+    __syncthreads();
+    if (tid == 0) last_cta = atomicAdd(p.work, 1u) == gridDim.x - 1;
+    __syncthreads();
+    if (!last_cta) return;
+    __threadfence();
+    if (tid == 0) *p.work = 0;
+  } else {
+    __syncthreads();
+  }
+  const int32_t popped0 = code ? 0 : static_cast<int32_t>(min(total.need, static_cast<long long>(free0)));
+  const int32_t popped1 = code ? 0 : static_cast<int32_t>(total.need) - popped0;
+  const uint32_t top0 = static_cast<uint32_t>(free0 - popped0), top1 = static_cast<uint32_t>(free1 - popped1);
+  uint32_t given0 = 0, given1 = 0;
+  if (!code && total.gone > 0) {
+    // Blocks given back, requests and logical blocks in descending order: number f of that order
+    // belongs to the thread run that has gone_after <= f, and there to the request found by walking down.
+    const uint32_t gone = static_cast<uint32_t>(total.gone);
+    gone_after[tid] = static_cast<uint32_t>(total.gone - before.gone - mine.gone);
+    __syncthreads();
+    for (uint32_t f0 = 0; f0 < gone; f0 += kBuildThreads) {
+      const uint32_t f = f0 + tid;
+      int32_t e = 0;
+      const bool on = f < gone;
+      if (on) {
+        uint32_t b = 0, n = kBuildThreads;  // gone_after falls with the thread: the first run whose value is <= f
+        while (n > 0) {
+          const uint32_t half = n >> 1;
+          if (gone_after[b + half] > f) {
+            b += half + 1;
+            n -= half + 1;
+          } else {
+            n = half;
+          }
+        }
+        uint32_t left = f - gone_after[b];
+        const uint32_t s0 = min(b * run, p.nseq);
+        uint32_t i = min(s0 + run, p.nseq);
+        while (i > s0) {
+          --i;
+          const int32_t a = p.lens[i];
+          const uint32_t g = static_cast<uint32_t>(sums_of(a, p.new_lens[i], shift).gone);
+          if (left < g) {
+            e = p.tables[static_cast<uint64_t>(i) * p.table_stride + blocks_of(a, shift) - 1 - left];
+            break;
+          }
+          left -= g;
+        }
+      }
+      const bool first = on && e >= 0, second = on && e < 0;
+      const uint32_t m0 = __ballot_sync(0xffffffffu, first), m1 = __ballot_sync(0xffffffffu, second);
+      __syncthreads();
+      if (lane == 0) warp_u32[warp] = __popc(m0) | (__popc(m1) << 16);
+      __syncthreads();
+      uint32_t rank0 = given0, rank1 = given1;
+      for (uint32_t w = 0; w < kBuildWarps; ++w) {
+        const uint32_t c = warp_u32[w];
+        if (w < warp) {
+          rank0 += c & 0xffffu;
+          rank1 += c >> 16;
+        }
+        given0 += c & 0xffffu;
+        given1 += c >> 16;
+      }
+      const uint32_t below = (1u << lane) - 1;
+      if (first) {
+        const uint64_t at = static_cast<uint64_t>(top0) + rank0 + __popc(m0 & below);
+        if (at < p.capacity[0])
+          p.ids[0][at] = e;
+        else
+          ptx::report_status(p.status, kStatusInvalid);
+      }
+      if (second) {
+        const uint64_t at = static_cast<uint64_t>(top1) + rank1 + __popc(m1 & below);
+        if (at < p.capacity[1])
+          p.ids[1][at] = ~e;
+        else
+          ptx::report_status(p.status, kStatusInvalid);
+      }
+    }
+  }
+  if (tid == 0) {
+    const uint64_t n0 = static_cast<uint64_t>(top0) + given0, n1 = static_cast<uint64_t>(top1) + given1;
+    p.free_out[0] = static_cast<int32_t>(code ? n0 : (n0 < p.capacity[0] ? n0 : p.capacity[0]));
+    p.free_out[1] = static_cast<int32_t>(code ? n1 : (n1 < p.capacity[1] ? n1 : p.capacity[1]));
+  }
+}
+
+// Scatter of rows. A row (all KV heads of one token, K or V) is `units` 16-byte units; unit u of block row
+// r is stored at unit u ^ (r & 7) of its 128 bytes. `lanes` (8, 16 or 32) neighbouring threads take a
+// token together, kRowsPerThread tokens at a time so that each thread has that many independent loads of K
+// and of V in flight. Bound by HBM: the rows are read and written once.
+constexpr uint32_t kWriteThreads = 256;
+constexpr uint32_t kRowsPerThread = 4;
+
+__global__ void __launch_bounds__(kWriteThreads) write_kv_kernel(const WriteKvParams p) {
+  const uint32_t lanes = 1u << p.lane_shift;
+  const uint32_t sub = threadIdx.x & (lanes - 1);
+  const uint32_t groups = kWriteThreads >> p.lane_shift, group = threadIdx.x >> p.lane_shift;
+  const uint64_t plane = static_cast<uint64_t>(p.row_bytes) << p.block_shift;
+  const uint32_t row_mask = (1u << p.block_shift) - 1;
+  const uint64_t t0 = static_cast<uint64_t>(blockIdx.x) * groups * kRowsPerThread + group;
+  uint8_t* dst[kRowsPerThread];
+  uint32_t swz[kRowsPerThread];
+#pragma unroll
+  for (uint32_t j = 0; j < kRowsPerThread; ++j) {
+    const uint64_t t = t0 + static_cast<uint64_t>(j) * groups;
+    dst[j] = nullptr;
+    swz[j] = 0;
+    if (t >= p.ntok) continue;
+    const int64_t slot = p.slots[t];
+    if (slot == kNoSlot) continue;
+    const uint32_t arena = slot < 0;
+    const uint64_t at = static_cast<uint64_t>(arena ? ~slot : slot);
+    const uint64_t id = at >> p.block_shift;
+    if (id >= (arena ? p.blocks[1] : p.blocks[0])) {
+      if (sub == 0) ptx::report_status(p.status, kStatusInvalid);
+      continue;
+    }
+    const uint32_t r = static_cast<uint32_t>(at) & row_mask;
+    dst[j] = (arena ? p.base[1] + id * p.block_stride[1] : p.base[0] + id * p.block_stride[0]) + static_cast<uint64_t>(r) * p.row_bytes;
+    swz[j] = r & 7u;
+  }
+  for (uint32_t u = sub; u < p.units; u += lanes) {
+    uint4 k[kRowsPerThread], v[kRowsPerThread];
+#pragma unroll
+    for (uint32_t j = 0; j < kRowsPerThread; ++j)
+      if (dst[j]) {
+        const uint64_t t = t0 + static_cast<uint64_t>(j) * groups;
+        k[j] = ptx::ld_stream_v4(p.k + t * p.k_stride + u * 16);
+        v[j] = ptx::ld_stream_v4(p.v + t * p.v_stride + u * 16);
+      }
+#pragma unroll
+    for (uint32_t j = 0; j < kRowsPerThread; ++j)
+      if (dst[j]) {
+        uint8_t* d = dst[j] + ((u & ~7u) + ((u & 7u) ^ swz[j])) * 16;
+        *reinterpret_cast<uint4*>(d) = k[j];
+        *reinterpret_cast<uint4*>(d + plane) = v[j];
+      }
+  }
+}
+
+}  // namespace
+
+cudaError_t launch_build_tables(const BuildTablesParams& p, int num_sms, cudaStream_t stream) {
+  const uint64_t steps = (static_cast<uint64_t>(p.max_tokens) + kBuildTokens - 1) / kBuildTokens;
+  const uint64_t most = static_cast<uint64_t>(num_sms);
+  const unsigned grid = static_cast<unsigned>(steps < 1 ? 1 : steps < most ? steps : most);
+  build_tables_kernel<<<grid, kBuildThreads, 0, stream>>>(p);
+  return cudaGetLastError();
+}
+
+cudaError_t launch_write_kv(WriteKvParams p, cudaStream_t stream) {
+  if (p.ntok == 0) return cudaSuccess;
+  p.units = p.row_bytes / 16;
+  p.lane_shift = p.units >= 32 ? 5 : p.units >= 16 ? 4 : 3;
+  const uint32_t per_cta = (kWriteThreads >> p.lane_shift) * kRowsPerThread;
+  const uint64_t grid = (static_cast<uint64_t>(p.ntok) + per_cta - 1) / per_cta;
+  write_kv_kernel<<<static_cast<unsigned>(grid), kWriteThreads, 0, stream>>>(p);
+  return cudaGetLastError();
+}
+
+}  // namespace ema

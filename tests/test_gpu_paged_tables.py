@@ -1,0 +1,258 @@
+"""Block tables and slot maps built on the GPU, and rows written through them, against plain models."""
+import numpy as np
+import pytest
+import torch
+
+from paper_2609_27040_b200 import binding as B
+from paper_2609_27040_b200 import build as build_mod
+from tests.paged_helpers import NO_SLOT, PoolModel, ceil_div, stored_place
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _built():
+    build_mod.build()
+
+
+def gpu(x, dtype=torch.int32):
+    return torch.tensor(x, dtype=dtype, device="cuda")
+
+
+class Bench:
+    """A pool and its tables on the device beside the model."""
+
+    def __init__(self, n, T, width, blocks0, blocks1, seed, extra=0):
+        rng = np.random.default_rng(seed)
+        ids0, ids1 = rng.permutation(blocks0).tolist(), rng.permutation(blocks1).tolist()
+        self.n, self.T, self.width = n, T, width
+        self.model = PoolModel(ids0, ids1)
+        self.model.width = width
+        self.rows = [{} for _ in range(n)]
+        pad = lambda x: gpu(x + [-7] * extra) if x or extra else None   # noqa: E731
+        self.ids = [pad(ids0), pad(ids1)]
+        self.free = gpu([blocks0, blocks1])
+        self.work = torch.zeros(1, dtype=torch.int32, device="cuda")
+        self.tables = torch.full((n, width + 3), -99, dtype=torch.int32, device="cuda")[:, :width]     # rows further apart than they are long
+        self.status = gpu([0])
+        self.lens = [0] * n
+
+    def pool(self, free_out=None):
+        return B.PagedPool(self.ids[0], self.ids[1], self.free, self.free if free_out is None else free_out, self.work)
+
+    def call(self, new_lens, max_tokens, stream=None):
+        self.offsets = torch.full((self.n + 1,), -5, dtype=torch.int32, device="cuda")
+        self.slots = torch.full((max_tokens,), 5, dtype=torch.int64, device="cuda")
+        self.positions = torch.full((max_tokens,), 5, dtype=torch.int32, device="cuda")
+        torch.cuda.synchronize()
+        assert B.paged_build_tables(self.pool(), gpu(self.lens), gpu(new_lens), self.T, self.tables, self.offsets, self.slots,
+                                    self.positions, self.status, stream) == B.OK
+        torch.cuda.synchronize()
+
+    def step(self, new_lens, max_tokens):
+        self.call(new_lens, max_tokens)
+        status, offsets, slots, positions = self.model.step(self.T, self.lens, new_lens, self.rows, max_tokens)
+        assert int(self.status) == status
+        assert self.offsets.tolist() == offsets
+        assert self.slots.tolist() == slots
+        assert self.positions.tolist() == positions
+        self.same_state()
+        if status == 0:
+            self.lens = list(new_lens)
+        self.status.zero_()
+        return status
+
+    def same_state(self):
+        free = self.free.tolist()
+        assert free == [len(s) for s in self.model.stacks]
+        for j in (0, 1):
+            if self.ids[j] is not None:
+                assert self.ids[j][:free[j]].tolist() == self.model.stacks[j]
+        want = np.full((self.n, self.width), -99)
+        for i, row in enumerate(self.rows):
+            for j, e in row.items():
+                want[i, j] = e
+        assert (self.tables.cpu().numpy() == want).all()
+        assert int(self.work) == 0
+
+
+@pytest.mark.parametrize("n,T,hi,blocks0,blocks1", [
+    (1, 16, 40, 3, 0), (1, 64, 64, 0, 1), (5, 16, 100, 10, 30), (33, 32, 700, 200, 600), (512, 16, 60, 900, 2000),
+    (513, 16, 60, 3000, 1), (700, 64, 300, 5, 4000), (2500, 16, 50, 5000, 6000), (40, 16, 3000, 500, 8000)])
+def test_random_walks_follow_the_model(n, T, hi, blocks0, blocks1):
+    rng = np.random.default_rng(n * 7 + T)
+    b = Bench(n, T, ceil_div(hi, T) + 1, blocks0, blocks1, n)
+    seen = set()
+    for k in range(8):
+        kind = k % 4
+        old = np.array(b.lens)
+        if kind == 0:                                            # prompts of all requests that hold nothing, some stay empty
+            new = np.where((old == 0) & (rng.random(n) < 0.8), rng.integers(0, hi + 1, n), old)
+        elif kind == 1:                                          # one token each, as far as there is room
+            new = np.minimum(old + 1, hi)
+        elif kind == 2:                                          # some finish, some fall back, some grow
+            new = np.where(rng.random(n) < 0.3, 0, np.where(rng.random(n) < 0.5, rng.integers(0, hi + 1, n), old))
+        else:
+            new = np.where(rng.random(n) < 0.5, rng.integers(0, hi + 1, n), old)
+        total = int(np.maximum(new - old, 0).sum())
+        seen.add(b.step(new.tolist(), total + int(rng.integers(0, 70)) if k % 3 else max(total, 1)))
+    assert 0 in seen
+
+
+def test_growth_taken_back_restores_the_stacks_exactly():
+    b = Bench(90, 16, 30, 200, 900, 3)
+    rng = np.random.default_rng(1)
+    b.step(rng.integers(0, 200, 90).tolist(), 40000)
+    ids = [x.clone() for x in b.ids]
+    free, lens = b.free.clone(), list(b.lens)
+    b.step([x + int(rng.integers(0, 200)) for x in lens], 40000)
+    b.step(lens, 1)
+    assert (b.free == free).all() and all((x == y).all() for x, y in zip(ids, b.ids))
+
+
+@pytest.mark.parametrize("what", ["no space", "no space by one", "too many tokens", "too long", "below zero", "old too long", "top"])
+def test_refused_steps_change_nothing(what):
+    b = Bench(20, 16, 10, 30, 40, 5)
+    assert b.step([50] * 10 + [0] * 10, 500) == 0                 # 40 of 70 blocks
+    new, tokens = list(b.lens), 400
+    if what == "no space":
+        new = [160] * 20
+        tokens = 5000
+    elif what == "no space by one":
+        new[10:] = [48] * 10                                      # 30 more: exactly what is left
+        new[0] = 65                                               # and one
+        tokens = 5000
+    elif what == "too many tokens":
+        new[0], tokens = 61, 10
+    elif what == "too long":
+        new[3] = 161
+    elif what == "below zero":
+        new[3] = -1
+    elif what == "old too long":
+        b.lens[15] = 161
+    before = [t.clone() for t in (b.tables, b.ids[0], b.ids[1], b.free)]
+    if what == "top":
+        b.free[0] = 31
+        b.call(new, tokens)
+        assert int(b.status) == B.EINVAL and b.free.tolist()[0] == 31
+        b.free.copy_(before[3])
+        assert (b.slots == NO_SLOT).all() and (b.positions == -1).all() and (b.offsets == 0).all()
+    else:
+        assert b.step(new, tokens) == (B.ENOSPC if "space" in what else B.EINVAL)
+    assert all((x == y).all() for x, y in zip(before, (b.tables, b.ids[0], b.ids[1], b.free)))
+
+
+def test_exactly_all_blocks_and_no_requests():
+    b = Bench(3, 16, 4, 4, 3, 2)
+    assert b.step([64, 33, 0], 97) == 0 and b.free.tolist() == [0, 0]
+    assert b.step([64, 33, 0], 1) == 0
+    assert b.step([64, 33, 1], 5) == B.ENOSPC
+    assert b.step([0, 0, 0], 1) == 0 and b.free.tolist() == [4, 3]
+    empty = Bench(0, 16, 1, 2, 2, 2)
+    empty.call([], 70)
+    assert empty.offsets.tolist() == [0] and (empty.slots == NO_SLOT).all() and empty.free.tolist() == [2, 2]
+
+
+def test_pushes_beyond_a_stacks_capacity_are_dropped_and_reported():
+    b = Bench(1, 16, 8, 3, 0, 2)
+    b.tables[0, :8] = torch.arange(100, 108, dtype=torch.int32)   # blocks that never came from this pool
+    b.lens = [128]
+    b.call([0], 1)
+    assert int(b.status) == B.EINVAL and b.free.tolist() == [3, 0] and int(b.work) == 0
+
+
+def test_a_separate_count_leaves_the_first_one():
+    b = Bench(4, 16, 8, 20, 20, 2)
+    out = gpu([-1, -1])
+    args = (gpu([0] * 4), gpu([17, 0, 64, 1]), 16, b.tables, gpu([0] * 5), torch.zeros(90, dtype=torch.int64, device="cuda"),
+            torch.zeros(90, dtype=torch.int32, device="cuda"))
+    for _ in range(2):                                            # the same call again gives the same answer
+        assert B.paged_build_tables(b.pool(out), *args) == B.OK
+        torch.cuda.synchronize()
+        assert b.free.tolist() == [20, 20] and out.tolist() == [13, 20]
+
+
+def test_a_captured_step_follows_new_lengths():
+    """One graph of a build call, replayed with other lengths in the same buffers; many CTAs (large token room)."""
+    n, T, room = 300, 16, 30000
+    b = Bench(n, T, 20, 2000, 4000, 9)
+    lens, new = gpu([0] * n), gpu([0] * n)
+    offsets, slots = gpu([0] * (n + 1)), torch.zeros(room, dtype=torch.int64, device="cuda")
+    positions, status = gpu([0] * room), gpu([0])
+    s = torch.cuda.Stream()
+    g = torch.cuda.CUDAGraph()
+    pool = b.pool()
+    with torch.cuda.stream(s):
+        with torch.cuda.graph(g, stream=s):
+            assert B.paged_build_tables(pool, lens, new, T, b.tables, offsets, slots, positions, status, torch.cuda.current_stream()) == B.OK
+    rng = np.random.default_rng(4)
+    for k in range(12):
+        old = b.lens
+        want = [int(x) for x in (rng.integers(0, 100, n) if k % 3 == 0 else np.minimum(np.array(old) + 1, 300) if k % 3 == 1
+                                 else np.where(rng.random(n) < 0.4, 0, np.minimum(np.array(old) + rng.integers(0, 40, n), 300)))]
+        lens.copy_(gpu(old))
+        new.copy_(gpu(want))
+        torch.cuda.synchronize()
+        g.replay()
+        torch.cuda.synchronize()
+        st, o, sl, po = b.model.step(T, old, want, b.rows, room)
+        assert (int(status), offsets.tolist(), slots.tolist(), positions.tolist()) == (st, o, sl, po)
+        b.same_state()
+        b.lens = want
+
+
+# -- rows through the slot map -------------------------------------------------------------------
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("Hkv,D,T,n", [(8, 128, 16, 250), (1, 64, 64, 33), (3, 64, 16, 1), (2, 64, 32, 77), (10, 256, 32, 40), (5, 128, 16, 601)])
+def test_rows_land_in_their_slots(dtype, Hkv, D, T, n):
+    rng = np.random.default_rng(Hkv * D + n)
+    blocks = [ceil_div(n, T) + 2, ceil_div(n, T) + 1]
+    gen = torch.Generator(device="cuda").manual_seed(n)
+    arenas = [torch.randn((b, 3, T, Hkv, D), device="cuda", generator=gen).to(dtype)[:, :2] for b in blocks]   # blocks apart from one another
+    fused = torch.randn((n, 4 * Hkv, D), device="cuda", generator=gen).to(dtype)
+    k, v = fused[:, Hkv:2 * Hkv], fused[:, 3 * Hkv:]
+    slots = rng.permutation(np.concatenate([np.arange(blocks[0] * T), ~np.arange(blocks[1] * T)]))[:n]
+    slots[rng.random(n) < 0.1] = NO_SLOT
+    want = [a.clone() for a in arenas]
+    for t in range(n):
+        s = int(slots[t])
+        if s == NO_SLOT:
+            continue
+        a, s = (0, s) if s >= 0 else (1, ~s)
+        place = torch.from_numpy(stored_place(s % T, Hkv * D)).cuda()
+        for plane, x in ((0, k), (1, v)):
+            row = torch.empty(Hkv * D, dtype=dtype, device="cuda")
+            row[place] = x[t].reshape(-1)
+            want[a][s // T, plane, s % T] = row.view(Hkv, D)
+    cache = B.PagedCache(arenas[0], arenas[1])
+    status = gpu([0])
+    torch.cuda.synchronize()
+    assert B.paged_write_kv(cache, k, v, gpu(slots.tolist(), torch.int64), status) == B.OK
+    torch.cuda.synchronize()
+    assert int(status) == 0
+    for a, w in zip(arenas, want):
+        assert torch.equal(a.contiguous().view(torch.int16), w.contiguous().view(torch.int16))
+    if D == 128 and T == 16:                                      # and what the format's own converter says
+        canonical = [B.kv_block_swizzle(a.contiguous().view(torch.int16)).view(dtype) for a in arenas]
+        for t in range(n):
+            s = int(slots[t])
+            if s != NO_SLOT:
+                a, s = (0, s) if s >= 0 else (1, ~s)
+                assert torch.equal(canonical[a][s // T, 0, s % T], k[t]) and torch.equal(canonical[a][s // T, 1, s % T], v[t])
+
+
+def test_slots_outside_the_cache_are_skipped_and_reported():
+    arenas = [torch.zeros((3, 2, 16, 2, 64), dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    guard = [torch.zeros_like(a) for a in arenas]
+    k = torch.ones((4, 2, 64), dtype=torch.bfloat16, device="cuda")
+    status = gpu([0])
+    slots = gpu([48, ~48, (1 << 62), NO_SLOT + 1], torch.int64)
+    torch.cuda.synchronize()
+    assert B.paged_write_kv(B.PagedCache(*arenas), k, k, slots, status) == B.OK
+    torch.cuda.synchronize()
+    assert int(status) == B.EINVAL and all(torch.equal(a, g) for a, g in zip(arenas, guard))
+    status.zero_()
+    assert B.paged_write_kv(B.PagedCache(arenas[0]), k, k, gpu([~0, 5, NO_SLOT, 47], torch.int64), status) == B.OK   # no second arena
+    torch.cuda.synchronize()
+    assert int(status) == B.EINVAL and float(arenas[0].float().sum()) == 2 * 2 * 2 * 64

@@ -1,0 +1,180 @@
+"""Refusals of the device-driven path that need no GPU: what the C entry points and the binding check
+before anything is enqueued."""
+import ctypes as C
+
+import pytest
+import torch
+
+from paper_2609_27040_b200 import binding as B
+from paper_2609_27040_b200 import build as build_mod
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _built():
+    build_mod.build()
+
+
+def desc(**kw):
+    d = B.PagedCacheDesc()
+    d.dtype, d.num_kv_heads, d.head_dim, d.block_tokens = 0, 8, 128, 16
+    d.blocks[0], d.base[0] = 4, 1 << 20
+    for k, v in kw.items():
+        if isinstance(v, tuple):
+            getattr(d, k)[v[0]] = v[1]
+        else:
+            setattr(d, k, v)
+    return d
+
+
+BAD_CACHES = [dict(dtype=2), dict(num_kv_heads=0), dict(num_kv_heads=65), dict(head_dim=96), dict(head_dim=512), dict(block_tokens=8),
+              dict(block_tokens=48), dict(blocks=(0, 0)), dict(base=(0, 0)), dict(base=(0, (1 << 20) + 8)), dict(blocks=(1, 3)),
+              dict(block_stride=(0, 65536 - 16)), dict(block_stride=(0, 65536 + 8)), dict(blocks=(0, 0x80000000))]
+P = 1 << 20                                                        # an aligned address that is never touched: these calls are refused first
+
+
+def decode(cache, **kw):
+    a = dict(tables=P, table_stride=10, max_blocks=10, lens=P, nseq=2, q=P, q_stride=32 * 256, heads=32, scale=1.0, window=0, out=P,
+             out_stride=32 * 256, lse=None, work=P, work_bytes=1 << 30, status=None, stream=None)
+    a.update(kw)
+    return B.lib().paged_decode_tables(C.byref(cache), *a.values())
+
+
+def diff(cache, **kw):
+    a = dict(tables=P, table_stride=10, max_blocks=10, lens=P, nseq=2, q=P, q_stride=32 * 256, heads=32, lam=P, scale=1.0, window=0,
+             norm=None, eps=1e-5, out_scale=1.0, out=P, out_stride=32 * 256, work=P, work_bytes=1 << 30, status=None, stream=None)
+    a.update(kw)
+    return B.lib().paged_decode_diff(C.byref(cache), *a.values())
+
+
+def write(cache, **kw):
+    a = dict(k=P, ks=2048, v=P, vs=2048, slots=P, ntok=3, status=None, stream=None)
+    a.update(kw)
+    return B.lib().paged_write_kv(C.byref(cache), *a.values())
+
+
+@pytest.mark.parametrize("kw", BAD_CACHES, ids=str)
+def test_bad_caches_are_refused_everywhere(kw):
+    d = desc(**kw)
+    n = C.c_uint64(7)
+    assert decode(d) == diff(d) == write(d) == B.EINVAL
+    assert B.lib().paged_decode_workspace(C.byref(d), 32, C.byref(n)) == B.EINVAL and n.value == 7
+
+
+@pytest.mark.parametrize("kw", [dict(tables=None), dict(lens=None), dict(q=None), dict(out=None), dict(work=None), dict(max_blocks=0),
+                                dict(table_stride=9), dict(max_blocks=1 << 28, table_stride=1 << 28), dict(q_stride=32 * 256 - 16),
+                                dict(out_stride=8), dict(q_stride=32 * 256 + 8), dict(q=P + 8), dict(out=P + 2), dict(work=P + 4),
+                                dict(tables=P + 2), dict(lens=P + 1), dict(status=P + 1), dict(heads=0), dict(heads=12), dict(heads=136),
+                                dict(nseq=0x80000000)], ids=str)
+def test_bad_decode_arguments_are_refused(kw):
+    assert decode(desc(), **kw) == B.EINVAL
+    if kw.get("heads") != 136:
+        assert diff(desc(), **kw) == B.EINVAL
+
+
+def test_bad_differential_arguments_are_refused():
+    assert diff(desc(), lam=None) == B.EINVAL
+    assert diff(desc(), heads=72) == B.EINVAL                      # nine heads to a KV head
+    assert diff(desc(), norm=P, eps=-1.0) == B.EINVAL
+    assert diff(desc(), norm=P, eps=float("nan")) == B.EINVAL
+    assert diff(desc(), norm=P + 2) == B.EINVAL and diff(desc(), lam=P + 1) == B.EINVAL
+
+
+def test_workspace_too_small():
+    need = C.c_uint64(0)
+    assert B.lib().paged_decode_workspace(C.byref(desc()), 32, C.byref(need)) == B.OK and need.value > 1024
+    assert decode(desc(), work_bytes=need.value - 1) == B.ESCRATCH
+    twice = C.c_uint64(0)
+    assert B.lib().paged_decode_workspace(C.byref(desc()), 64, C.byref(twice)) == B.OK and twice.value > need.value
+    assert diff(desc(), work_bytes=need.value) == B.ESCRATCH       # the differential form has two rows to a head
+    for rows in (0, 12, 136):
+        assert B.lib().paged_decode_workspace(C.byref(desc()), rows, C.byref(need)) == B.EINVAL
+    assert B.lib().paged_decode_workspace(C.byref(desc()), 32, None) == B.EINVAL
+
+
+def test_nothing_to_do_is_ok():
+    assert decode(desc(), nseq=0) == diff(desc(), nseq=0) == write(desc(), ntok=0) == B.OK
+
+
+@pytest.mark.parametrize("kw", [dict(k=None), dict(v=None), dict(slots=None), dict(ks=2040), dict(vs=1024), dict(k=P + 8), dict(v=P + 2),
+                                dict(slots=P + 4), dict(status=P + 2), dict(ntok=0x80000000)], ids=str)
+def test_bad_write_arguments_are_refused(kw):
+    assert write(desc(), **kw) == B.EINVAL
+
+
+def build(pool_kw=None, **kw):
+    p = B.PagedPoolDesc()
+    p.ids[0], p.capacity[0], p.free_in, p.free_out, p.work = P, 10, P, P, P
+    for k, v in (pool_kw or {}).items():
+        if isinstance(v, tuple):
+            getattr(p, k)[v[0]] = v[1]
+        else:
+            setattr(p, k, v)
+    a = dict(lens=P, new=P, n=3, T=16, tables=P, stride=8, width=8, offsets=P, slots=P, positions=P, tokens=100, status=None, stream=None)
+    a.update(kw)
+    return B.lib().paged_build_tables(C.byref(p), *a.values())
+
+
+def test_bad_build_arguments_are_refused():
+    for kw in (dict(lens=None), dict(new=None), dict(T=0), dict(T=24), dict(T=128), dict(tables=None), dict(stride=7), dict(width=0),
+               dict(width=1 << 28, stride=1 << 28), dict(offsets=None), dict(slots=None), dict(positions=None), dict(tokens=0x80000000),
+               dict(n=0x7fffffff), dict(slots=P + 4), dict(tables=P + 2), dict(offsets=P + 2), dict(status=P + 3), dict(lens=P + 2)):
+        assert build(**kw) == B.EINVAL, kw
+    for kw in (dict(ids=(0, None)), dict(capacity=(1, 5)), dict(capacity=(0, 0x80000000)), dict(free_in=None), dict(free_out=None),
+               dict(work=None), dict(work=P + 2), dict(ids=(0, P + 2))):
+        assert build(kw) == B.EINVAL, kw
+
+
+def test_binding_refuses_tensors_that_do_not_fit():
+    bf, i32, f32 = torch.bfloat16, torch.int32, torch.float32
+    arena = torch.zeros((4, 2, 16, 2, 64), dtype=bf)
+    for bad in (torch.zeros((4, 2, 16, 2, 64)), arena[:, :1], arena.transpose(2, 3), torch.zeros((4, 3, 16, 2, 64), dtype=bf), arena[0],
+                arena[:0]):
+        with pytest.raises(ValueError):
+            B.PagedCache(bad)
+    with pytest.raises(ValueError):
+        B.PagedCache(arena, torch.zeros((4, 2, 16, 2, 64), dtype=torch.float16))
+    with pytest.raises(ValueError):
+        B.PagedCache(arena, torch.zeros((4, 2, 32, 2, 64), dtype=bf))
+    c = B.PagedCache(arena[::2], arena[1:])
+    assert c.desc.block_stride[0] == 2 * 2 * 16 * 2 * 64 * 2 and list(c.desc.blocks) == [2, 3]
+    good = dict(tables=torch.zeros((3, 5), dtype=i32), lens=torch.zeros(3, dtype=i32), q=torch.zeros((3, 4, 64), dtype=bf), sm_scale=1.0,
+                out=torch.zeros((3, 4, 64), dtype=bf), workspace=torch.zeros(B.paged_decode_workspace(c, 4), dtype=torch.uint8))
+    for kw in (dict(tables=good["tables"].long()), dict(tables=good["tables"][:2]), dict(tables=torch.zeros((5, 3), dtype=i32).T),
+               dict(lens=torch.zeros(3, dtype=torch.int64)), dict(lens=torch.zeros(6, dtype=i32)[::2]), dict(q=good["q"].half()),
+               dict(q=good["q"][:2]), dict(q=torch.zeros((3, 64, 4), dtype=bf).transpose(1, 2)), dict(out=good["out"].float()),
+               dict(out=torch.zeros((3, 4, 32), dtype=bf)), dict(lse=torch.zeros((3, 5), dtype=f32)), dict(window=-1),
+               dict(status=torch.zeros(2, dtype=i32)), dict(workspace=torch.zeros(64)[::2])):
+        with pytest.raises(ValueError):
+            B.paged_decode_tables(c, **{**good, **kw})
+    d = dict(good, q=torch.zeros((3, 8, 32), dtype=bf), lam=torch.zeros(4))
+    for kw in (dict(q=good["q"]), dict(lam=torch.zeros(3)), dict(lam=torch.zeros(4).half()), dict(norm_weight=torch.zeros(32)), dict(window=-3)):
+        with pytest.raises(ValueError):
+            B.paged_decode_diff(c, **{**d, **kw})
+    k = torch.zeros((5, 2, 64), dtype=bf)
+    for a in ((k, k[:4], torch.zeros(5, dtype=torch.int64)), (k, k, torch.zeros(5, dtype=i32)), (k.half(), k, torch.zeros(5, dtype=torch.int64)),
+              (k, torch.zeros((5, 64, 2), dtype=bf).transpose(1, 2), torch.zeros(5, dtype=torch.int64))):
+        with pytest.raises(ValueError):
+            B.paged_write_kv(c, *a)
+    w = torch.zeros(1, dtype=i32)
+    for a in ((torch.zeros(4), None, torch.zeros(2, dtype=i32), torch.zeros(2, dtype=i32), w),
+              (torch.zeros(4, dtype=i32), None, torch.zeros(3, dtype=i32), torch.zeros(2, dtype=i32), w),
+              (torch.zeros(4, dtype=i32), None, torch.zeros(2, dtype=i32), torch.zeros(2, dtype=i32), torch.zeros(0, dtype=i32))):
+        with pytest.raises(ValueError):
+            B.PagedPool(*a)
+
+
+def test_descriptor_sizes_match_the_header():
+    assert C.sizeof(B.PagedCacheDesc) == 4 * 4 + 2 * 4 + 2 * 8 + 2 * 8
+    assert C.sizeof(B.PagedPoolDesc) == 2 * 8 + 2 * 4 + 3 * 8
+
+
+def test_memory_that_no_gpu_can_reach_is_refused():
+    """Host tensors through the whole binding: every call answers with a code, none launches."""
+    arena = torch.zeros((4, 2, 16, 2, 64), dtype=torch.bfloat16)
+    c = B.PagedCache(arena)
+    k = torch.zeros((5, 2, 64), dtype=torch.bfloat16)
+    assert B.paged_write_kv(c, k, k, torch.zeros(5, dtype=torch.int64)) in (B.EINVAL, B.ECUDA)
+    q = torch.zeros((3, 4, 64), dtype=torch.bfloat16)
+    i32 = torch.int32
+    assert B.paged_decode_tables(c, torch.zeros((3, 5), dtype=i32), torch.zeros(3, dtype=i32), q, 1.0, q.clone(),
+                                 torch.zeros(B.paged_decode_workspace(c, 4), dtype=torch.uint8)) in (B.EINVAL, B.ECUDA)
