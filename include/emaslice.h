@@ -579,7 +579,7 @@ int paged_write_kv(const paged_cache_t* cache, const void* k, uint64_t k_stride,
 
 /* Bytes of workspace that the two calls below need for num_q_rows query rows per sequence (num_q_heads, or twice
  * num_heads for the differential form), independent of batch and lengths. Before its first use the
- * workspace's first 1024 bytes must be 0; every call leaves them 0. */
+ * workspace's first 16384 bytes must be 0; every call leaves them 0. */
 int paged_decode_workspace(const paged_cache_t* cache, uint32_t num_q_rows, uint64_t* out_bytes);
 
 /* Attention of one new token per sequence: for query head h (KV head h / G, G = num_q_heads / num_kv_heads in 1..16)

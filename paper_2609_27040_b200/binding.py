@@ -447,26 +447,39 @@ def slice_schedule_gll(slices) -> int:
 
 
 # -- device-driven path: torch tensors in, one launch per call ---------------------------------------
+# The checks read as little of a tensor as they can and build their messages only when they fail: a call
+# takes the host a few microseconds, about what its kernel takes the GPU on a small batch.
 
-def _need(ok: bool, what: str):
-    if not ok:
-        raise ValueError(what)
+_I32 = _I64 = _F32 = None                             # torch's dtypes, once a cache or a pool has been made
 
 
-def _words(t, name: str, device, dtype: str = "torch.int32", shape=None):
-    """Address of a dense array of whole numbers (or f32) on `device`."""
-    _need(str(t.dtype) == dtype and t.is_contiguous() and t.device == device and (shape is None or tuple(t.shape) == shape),
-          f"{name}: expected a contiguous {dtype} tensor on {device}" + (f" of shape {shape}" if shape is not None else ""))
+def _torch_types():
+    global _I32, _I64, _F32
+    import torch
+    _I32, _I64, _F32 = torch.int32, torch.int64, torch.float32
+    return {torch.bfloat16: 0, torch.float16: 1}
+
+
+def _refuse(what: str):
+    raise ValueError(what)
+
+
+def _words(t, name: str, dev: int, dtype, shape=None) -> int:
+    """Address of a dense array of whole numbers (or f32) on device number `dev` (-1: host memory)."""
+    if t.dtype is not dtype or t.get_device() != dev or not t.is_contiguous() or (shape is not None and t.shape != shape):
+        _refuse(f"{name}: expected a contiguous {dtype} tensor on device {dev}" + (f" of shape {shape}" if shape is not None else "")
+                + f", got {tuple(t.shape)} of {t.dtype} on {t.device}")
     return t.data_ptr()
 
 
-def _row_stride(t, name: str, device, dtype, rows: int, cols: int):
-    """Byte stride between the entries of a [n][rows][cols] tensor whose inner two dimensions are dense."""
-    _need(t.dim() == 3 and t.dtype == dtype and t.device == device and t.shape[1] == rows and t.shape[2] == cols,
-          f"{name}: expected [n][{rows}][{cols}] of {dtype} on {device}, got {tuple(t.shape)} of {t.dtype} on {t.device}")
-    s = t.stride()
-    _need((s[2] == 1 or cols == 1) and (s[1] == cols or rows == 1), f"{name}: the inner two dimensions have to be contiguous")
-    return (s[0] if t.shape[0] > 1 else rows * cols) * 2
+def _row_stride(t, name: str, dev: int, dtype, n: int, rows: int, cols: int) -> int:
+    """Byte stride between the entries of an [n][rows][cols] tensor whose inner two dimensions are dense."""
+    if t.dtype is not dtype or t.get_device() != dev or t.shape != (n, rows, cols):
+        _refuse(f"{name}: expected [{n}][{rows}][{cols}] of {dtype} on device {dev}, got {tuple(t.shape)} of {t.dtype} on {t.device}")
+    s0, s1, s2 = t.stride()
+    if (s2 != 1 and cols > 1) or (s1 != cols and rows > 1):
+        _refuse(f"{name}: the inner two dimensions have to be contiguous, got strides {t.stride()}")
+    return (s0 if n > 1 else rows * cols) * 2
 
 
 class PagedCache:
@@ -475,24 +488,26 @@ class PagedCache:
     further apart than their size (first stride); the rest is dense. Holds the two tensors, nothing else."""
 
     def __init__(self, local, lent=None):
+        kinds = _torch_types()
         parts = [t for t in (local, lent) if t is not None and t.shape[0] > 0]
-        _need(bool(parts), "a cache needs at least one block")
+        if not parts:
+            _refuse("a cache needs at least one block")
         ref = parts[0]
-        kinds = {"torch.bfloat16": 0, "torch.float16": 1}
         d = PagedCacheDesc()
         for j, t in enumerate((local, lent)):
             if t is None or t.shape[0] == 0:
                 continue
-            _need(t.dim() == 5 and t.shape[1] == 2 and tuple(t.shape[1:]) == tuple(ref.shape[1:]) and t.dtype == ref.dtype
-                  and t.device == ref.device and str(t.dtype) in kinds, "arenas: [blocks][2][block_tokens][num_kv_heads][head_dim], "
-                  "bf16 or fp16, alike in both")
-            _need(t[0].is_contiguous(), "arenas: blocks have to be dense")
+            if t.dim() != 5 or t.shape[1] != 2 or t.shape[1:] != ref.shape[1:] or t.dtype is not ref.dtype or t.device != ref.device \
+                    or t.dtype not in kinds:
+                _refuse("arenas: [blocks][2][block_tokens][num_kv_heads][head_dim], bf16 or fp16, alike in both")
+            if not t[0].is_contiguous():
+                _refuse("arenas: blocks have to be dense")
             d.blocks[j], d.base[j] = t.shape[0], t.data_ptr()
             d.block_stride[j] = t.stride(0) * 2 if t.shape[0] > 1 else 0
-        d.dtype, d.block_tokens, d.num_kv_heads, d.head_dim = kinds[str(ref.dtype)], ref.shape[2], ref.shape[3], ref.shape[4]
+        d.dtype, d.block_tokens, d.num_kv_heads, d.head_dim = kinds[ref.dtype], ref.shape[2], ref.shape[3], ref.shape[4]
         self.desc, self._ref = d, C.byref(d)
         self.local, self.lent = local, lent
-        self.dtype, self.device = ref.dtype, ref.device
+        self.dtype, self.device, self._dev = ref.dtype, ref.device, ref.get_device()
         self.block_tokens, self.num_kv_heads, self.head_dim = ref.shape[2], ref.shape[3], ref.shape[4]
 
 
@@ -501,46 +516,44 @@ class PagedPool:
     after a call (`free_out`, may be the same tensor), int32 [2] each, and a zeroed work word of PAGED_POOL_WORK_BYTES."""
 
     def __init__(self, local_ids, lent_ids, free, free_out, work):
-        dev = free.device
+        _torch_types()
+        dev = free.get_device()
         d = PagedPoolDesc()
         for j, t in enumerate((local_ids, lent_ids)):
             if t is not None and t.numel():
-                d.ids[j], d.capacity[j] = _words(t, "ids", dev), t.numel()
-        d.free_in, d.free_out = _words(free, "free", dev, shape=(2,)), _words(free_out, "free_out", dev, shape=(2,))
-        _need(work.is_contiguous() and work.device == dev and work.numel() * work.element_size() >= PAGED_POOL_WORK_BYTES,
-              "work: PAGED_POOL_WORK_BYTES on the pool's device")
+                d.ids[j], d.capacity[j] = _words(t, "ids", dev, _I32), t.numel()
+        d.free_in, d.free_out = _words(free, "free", dev, _I32, (2,)), _words(free_out, "free_out", dev, _I32, (2,))
+        if not work.is_contiguous() or work.get_device() != dev or work.numel() * work.element_size() < PAGED_POOL_WORK_BYTES:
+            _refuse("work: PAGED_POOL_WORK_BYTES on the pool's device")
         d.work = work.data_ptr()
-        self.desc, self._ref, self.device = d, C.byref(d), dev
+        self.desc, self._ref, self.device, self._dev = d, C.byref(d), free.device, dev
         self._keep = (local_ids, lent_ids, free, free_out, work)
 
 
-def _table(tables, n: int, device):
-    _need(tables.dim() == 2 and str(tables.dtype) == "torch.int32" and tables.device == device and tables.shape[0] == n
-          and (tables.stride(1) == 1 or tables.shape[1] == 1), f"tables: expected int32 [{n}][max_blocks] on {device}, rows contiguous")
-    return tables.data_ptr(), (tables.stride(0) if n > 1 else tables.shape[1]), tables.shape[1]
-
-
-def _status(status, device):
-    return None if status is None else _words(status, "status", device, shape=(1,))
+def _table(t, n: int, dev: int):
+    """Address, entries from a row to the next, and width of the tables."""
+    if t.dim() != 2 or t.dtype is not _I32 or t.get_device() != dev or t.shape[0] != n or (t.stride(1) != 1 and t.shape[1] > 1):
+        _refuse(f"tables: expected int32 [{n}][max_blocks] on device {dev}, rows contiguous, got {tuple(t.shape)} of {t.dtype} on {t.device}")
+    width = t.shape[1]
+    return t.data_ptr(), (t.stride(0) if n > 1 else width), width
 
 
 def paged_build_tables(pool: PagedPool, lens, new_lens, block_tokens: int, tables, offsets, slots, positions, status=None,
                        stream=None) -> int:
-    dev, n = pool.device, lens.numel()
+    dev, n, room = pool._dev, lens.numel(), slots.numel()
     tab, stride, width = _table(tables, n, dev)
-    _need(slots.numel() == positions.numel(), "slots and positions are of one length")
-    return lib().paged_build_tables(pool._ref, _words(lens, "lens", dev), _words(new_lens, "new_lens", dev, shape=(n,)), n, block_tokens,
-                                    tab, stride, width, _words(offsets, "offsets", dev, shape=(n + 1,)),
-                                    _words(slots, "slots", dev, "torch.int64"), _words(positions, "positions", dev), slots.numel(),
-                                    _status(status, dev), _stream(stream))
+    return lib().paged_build_tables(pool._ref, _words(lens, "lens", dev, _I32), _words(new_lens, "new_lens", dev, _I32, (n,)), n, block_tokens,
+                                    tab, stride, width, _words(offsets, "offsets", dev, _I32, (n + 1,)), _words(slots, "slots", dev, _I64),
+                                    _words(positions, "positions", dev, _I32, (room,)), room,
+                                    None if status is None else _words(status, "status", dev, _I32, (1,)), _stream(stream))
 
 
 def paged_write_kv(cache: PagedCache, k, v, slots, status=None, stream=None) -> int:
-    dev, h, d = cache.device, cache.num_kv_heads, cache.head_dim
-    ks, vs = _row_stride(k, "k", dev, cache.dtype, h, d), _row_stride(v, "v", dev, cache.dtype, h, d)
-    _need(k.shape[0] == v.shape[0] == slots.numel(), "k, v and slots are of one length")
-    return lib().paged_write_kv(cache._ref, k.data_ptr(), ks, v.data_ptr(), vs, _words(slots, "slots", dev, "torch.int64"), k.shape[0],
-                                _status(status, dev), _stream(stream))
+    dev, n = cache._dev, slots.numel()
+    ks = _row_stride(k, "k", dev, cache.dtype, n, cache.num_kv_heads, cache.head_dim)
+    vs = _row_stride(v, "v", dev, cache.dtype, n, cache.num_kv_heads, cache.head_dim)
+    return lib().paged_write_kv(cache._ref, k.data_ptr(), ks, v.data_ptr(), vs, _words(slots, "slots", dev, _I64), n,
+                                None if status is None else _words(status, "status", dev, _I32, (1,)), _stream(stream))
 
 
 def paged_decode_workspace(cache: PagedCache, num_q_rows: int) -> int:
@@ -553,32 +566,35 @@ def paged_decode_workspace(cache: PagedCache, num_q_rows: int) -> int:
     return int(out.value)
 
 
-def _workspace(work, device):
-    _need(work.is_contiguous() and work.device == device, "workspace: a contiguous tensor on the cache's device")
-    return work.data_ptr(), work.numel() * work.element_size()
+def _workspace(work, dev: int):
+    if not work.is_contiguous() or work.get_device() != dev:
+        _refuse("workspace: a contiguous tensor on the cache's device")
+    return work.data_ptr(), work.nbytes
 
 
 def paged_decode_tables(cache: PagedCache, tables, lens, q, sm_scale: float, out, workspace, lse=None, window: int = 0, status=None,
                         stream=None) -> int:
-    dev, n, heads, d = cache.device, lens.numel(), q.shape[1], cache.head_dim
-    qs, os_ = _row_stride(q, "q", dev, cache.dtype, heads, d), _row_stride(out, "out", dev, cache.dtype, heads, d)
-    _need(q.shape[0] == out.shape[0] == n and window >= 0, "q, out and lens are of one length, a window is 0 or more")
+    dev, n, heads, d = cache._dev, lens.numel(), q.shape[1], cache.head_dim
+    qs, os_ = _row_stride(q, "q", dev, cache.dtype, n, heads, d), _row_stride(out, "out", dev, cache.dtype, n, heads, d)
+    if window < 0:
+        _refuse("a window is 0 (none) or more")
     tab, stride, width = _table(tables, n, dev)
     ws, wb = _workspace(workspace, dev)
-    return lib().paged_decode_tables(cache._ref, tab, stride, width, _words(lens, "lens", dev), n, q.data_ptr(), qs, heads, sm_scale, window,
-                                     out.data_ptr(), os_, None if lse is None else _words(lse, "lse", dev, "torch.float32", (n, heads)),
-                                     ws, wb, _status(status, dev), _stream(stream))
+    return lib().paged_decode_tables(cache._ref, tab, stride, width, _words(lens, "lens", dev, _I32), n, q.data_ptr(), qs, heads, sm_scale,
+                                     window, out.data_ptr(), os_, None if lse is None else _words(lse, "lse", dev, _F32, (n, heads)), ws, wb,
+                                     None if status is None else _words(status, "status", dev, _I32, (1,)), _stream(stream))
 
 
 def paged_decode_diff(cache: PagedCache, tables, lens, q, lam, sm_scale: float, out, workspace, norm_weight=None, eps: float = 1e-5,
                       out_scale: float = 1.0, window: int = 0, status=None, stream=None) -> int:
-    dev, n, heads, d = cache.device, lens.numel(), out.shape[1], cache.head_dim
-    qs = _row_stride(q, "q", dev, cache.dtype, 2 * heads, d // 2)
-    os_ = _row_stride(out, "out", dev, cache.dtype, heads, d)
-    _need(q.shape[0] == out.shape[0] == n and window >= 0, "q, out and lens are of one length, a window is 0 or more")
+    dev, n, heads, d = cache._dev, lens.numel(), out.shape[1], cache.head_dim
+    qs, os_ = _row_stride(q, "q", dev, cache.dtype, n, 2 * heads, d // 2), _row_stride(out, "out", dev, cache.dtype, n, heads, d)
+    if window < 0:
+        _refuse("a window is 0 (none) or more")
     tab, stride, width = _table(tables, n, dev)
     ws, wb = _workspace(workspace, dev)
-    return lib().paged_decode_diff(cache._ref, tab, stride, width, _words(lens, "lens", dev), n, q.data_ptr(), qs, heads,
-                                   _words(lam, "lam", dev, "torch.float32", (heads,)), sm_scale, window,
-                                   None if norm_weight is None else _words(norm_weight, "norm_weight", dev, "torch.float32", (d,)),
-                                   eps, out_scale, out.data_ptr(), os_, ws, wb, _status(status, dev), _stream(stream))
+    return lib().paged_decode_diff(cache._ref, tab, stride, width, _words(lens, "lens", dev, _I32), n, q.data_ptr(), qs, heads,
+                                   _words(lam, "lam", dev, _F32, (heads,)), sm_scale, window,
+                                   None if norm_weight is None else _words(norm_weight, "norm_weight", dev, _F32, (d,)), eps, out_scale,
+                                   out.data_ptr(), os_, ws, wb, None if status is None else _words(status, "status", dev, _I32, (1,)),
+                                   _stream(stream))

@@ -259,13 +259,26 @@ cudaError_t launch_write_kv(WriteKvParams p, cudaStream_t stream);
 
 // paged_decode.cu: attention of one token per sequence through device tables (see paged_decode_tables and
 // paged_decode_diff). The tensor maps are made by the launch.
-constexpr uint32_t kPagedMaxCtas = 256;         // most CTAs; arrival counters at the start of the workspace
+constexpr uint32_t kPagedMaxCtas = 160;         // most CTAs of a launch
+// The line of all work has three zones, up to 7, 12 and 16 sixteenths of it, whose items are cut into pieces of a 2nd, a 4th and
+// an 8th of a CTA's share.
+constexpr uint32_t kPagedZone0 = 7, kPagedZone1 = 12, kPagedCut0 = 2, kPagedCut1 = 4, kPagedCut2 = 8;
+// Most pieces of cut items: an item of n chunks is cut into at most n / size, and belongs to the zone it begins in, so that
+// items that begin in the first zone may reach to the end, and so on.
+constexpr uint32_t kPagedMaxParts = kPagedMaxCtas * kPagedCut2;
+constexpr uint32_t kPagedFan = 16;              // pieces that are added at a time
+// Words at the start of the workspace, zero before and after: ticket counter, CTAs done, arrivals at every level of the
+// trees in which the pieces of cut items meet (three levels: 16^3 >= kPagedMaxParts).
+constexpr uint32_t kPagedTicket = 0, kPagedDone = 1, kPagedTree = 32;
+constexpr uint32_t kPagedCounterBytes = 16384;
+static_assert((kPagedTree + 3 * kPagedMaxParts) * 4 <= kPagedCounterBytes, "counters");
+static_assert(kPagedFan * kPagedFan * kPagedFan >= kPagedMaxParts, "levels");
 struct PagedDecodeParams {
   uint8_t* base[2];
   uint64_t block_stride[2];
   uint32_t blocks[2];
   uint32_t dtype;              // 0 bf16, 1 fp16
-  uint32_t num_kv_heads, head_dim, block_tokens;
+  uint32_t num_kv_heads, head_dim, block_tokens, block_shift;
   const int32_t* tables;
   uint64_t table_stride;       // entries
   uint32_t max_blocks;
@@ -275,13 +288,13 @@ struct PagedDecodeParams {
   uint64_t q_stride;
   uint32_t rows;               // query rows per KV head: G, or 2 G for the differential form (two maps, interleaved)
   uint32_t window;             // 0: the whole length
-  float scale_log2;
+  float scale_log2;            // |scale| * log2(e), above 0
+  uint32_t q_keep, q_flip;     // pairs of q are taken as (pair & q_keep) ^ q_flip: scales of 0 and below 0
   uint8_t* out;
   uint64_t out_stride;         // bytes
   float* lse;                  // [nseq][heads] or NULL
-  uint32_t* counters;          // [kPagedMaxCtas], zero before and after
-  float* part_o;               // [2 * CTAs][rows][head_dim]
-  float* part_ml;              // [2 * CTAs][rows][2]
+  uint32_t* counters;          // kPagedCounterBytes
+  float* parts;                // [kPagedMaxParts] partial rows
   const float* lam;            // differential form: [heads]; NULL otherwise
   const float* norm_weight;    // [head_dim] or NULL
   float eps, out_scale;

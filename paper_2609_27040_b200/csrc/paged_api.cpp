@@ -57,7 +57,7 @@ int decode(const paged_cache_t* c, const int32_t* tables, uint64_t table_stride,
   if (!cache_ok(c, stride)) return SLICE_EINVAL;
   if (rows == 0 || rows > 16) return SLICE_EINVAL;
   if (nseq == 0) return SLICE_OK;
-  if (!tables || !lens || !q || !out || !workspace || nseq > kMost) return SLICE_EINVAL;
+  if (!tables || !lens || !q || !out || !workspace || static_cast<uint64_t>(nseq) * c->num_kv_heads > kMost / 2) return SLICE_EINVAL;
   if (max_blocks == 0 || table_stride < max_blocks || static_cast<uint64_t>(max_blocks) * c->block_tokens > kMost) return SLICE_EINVAL;
   const uint64_t q_row = static_cast<uint64_t>(rows) * c->num_kv_heads * (lam ? c->head_dim / 2 : c->head_dim) * 2;
   const uint64_t out_row = static_cast<uint64_t>(out_heads) * c->head_dim * 2;
@@ -79,6 +79,7 @@ int decode(const paged_cache_t* c, const int32_t* tables, uint64_t table_stride,
   p.num_kv_heads = c->num_kv_heads;
   p.head_dim = c->head_dim;
   p.block_tokens = c->block_tokens;
+  p.block_shift = block_shift(c->block_tokens);
   p.tables = tables;
   p.table_stride = table_stride;
   p.max_blocks = max_blocks;
@@ -88,13 +89,20 @@ int decode(const paged_cache_t* c, const int32_t* tables, uint64_t table_stride,
   p.q_stride = q_stride;
   p.rows = rows;
   p.window = window;
-  p.scale_log2 = sm_scale * 1.4426950408889634f;
+  // The kernel works with a scale above 0: the sign goes to q, and a scale of 0 is a query of zeros. (Not a number: every
+  // comparison is false, and the scale itself makes the result one.)
+  p.scale_log2 = (sm_scale < 0.f ? -sm_scale : sm_scale) * 1.4426950408889634f;
+  p.q_keep = 0xffffffffu;
+  p.q_flip = sm_scale < 0.f ? 0x80008000u : 0u;
+  if (p.scale_log2 == 0.f) {
+    p.scale_log2 = 1.f;
+    p.q_keep = p.q_flip = 0u;
+  }
   p.out = static_cast<uint8_t*>(out);
   p.out_stride = out_stride;
   p.lse = lse;
   p.counters = static_cast<uint32_t*>(workspace);
-  p.part_o = reinterpret_cast<float*>(p.counters + ema::kPagedMaxCtas);
-  p.part_ml = p.part_o + static_cast<size_t>(2) * ema::kPagedMaxCtas * rows * c->head_dim;
+  p.parts = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + ema::kPagedCounterBytes);
   p.lam = lam;
   p.norm_weight = norm_weight;
   p.eps = eps;

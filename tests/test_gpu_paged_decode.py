@@ -77,7 +77,7 @@ class Case:
         assert rc == B.OK
         torch.cuda.synchronize()
         assert int(self.status) == 0
-        assert not self.work[:1024].any()
+        assert not self.work[:16384].any()
 
     def check(self):
         eps = torch.finfo(self.dtype).eps
@@ -172,6 +172,24 @@ def test_differential_windows(window):
     c.check()
 
 
+@pytest.mark.parametrize("n,hi,Hkv", [(700, 60, 4), (3000, 70, 4), (400, 300, 8), (900, 400, 3)])
+def test_many_short_sequences(n, hi, Hkv):
+    lens = np.random.default_rng(n).integers(0, hi, n).tolist()
+    for diff in (False, True):
+        c = Case(lens, Hkv, 2, 128, 16, BF, lent=0.3, seed=n, diff=diff)
+        c.run()
+        c.check()
+
+
+@pytest.mark.parametrize("scale", [0.0, -0.0, -0.11, -3.0, 1e-30])
+def test_scales_of_either_sign_and_of_zero(scale):
+    for diff in (False, True):
+        c = Case([40, 1, 0, 513], 2, 3, 128, 16, BF, seed=11, diff=diff)
+        c.scale = scale
+        c.run(norm=False)
+        c.check()
+
+
 def test_equal_maps_cancel_exactly():
     """q1 = q2, K1 = K2 and a weight of 1: both maps are the same arithmetic, so nothing is left of any row."""
     c = Case([5, 700, 64], 4, 2, 128, 16, BF, diff=True)
@@ -244,7 +262,7 @@ def test_a_captured_call_follows_tables_and_lengths():
         torch.cuda.synchronize()
         c.lens = lens
         c.check()
-        assert int(c.status) == 0 and not c.work[:1024].any()
+        assert int(c.status) == 0 and not c.work[:16384].any()
 
 
 def test_blocks_apart_and_offsets_beyond_32_bits():

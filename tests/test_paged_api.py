@@ -81,7 +81,7 @@ def test_bad_differential_arguments_are_refused():
 
 def test_workspace_too_small():
     need = C.c_uint64(0)
-    assert B.lib().paged_decode_workspace(C.byref(desc()), 32, C.byref(need)) == B.OK and need.value > 1024
+    assert B.lib().paged_decode_workspace(C.byref(desc()), 32, C.byref(need)) == B.OK and need.value > 16384
     assert decode(desc(), work_bytes=need.value - 1) == B.ESCRATCH
     twice = C.c_uint64(0)
     assert B.lib().paged_decode_workspace(C.byref(desc()), 64, C.byref(twice)) == B.OK and twice.value > need.value
