@@ -549,6 +549,50 @@ typedef struct {
 
 #define PAGED_NO_SLOT INT64_MIN
 
+/* The calls take their arguments in a struct (host memory, read during the call only); unused ones are 0. */
+typedef struct {
+  const paged_pool_t* pool;
+  const int32_t *lens, *new_lens;         /* [nseq]                                               */
+  int32_t* tables;                        /* [nseq] rows of max_blocks cells                      */
+  uint64_t table_stride;                  /* cells from a row to the next                         */
+  int32_t* offsets;                       /* [nseq + 1]                                           */
+  int64_t* slots;                         /* [max_tokens]                                         */
+  int32_t* positions;                     /* [max_tokens]                                         */
+  int32_t* status;                        /* device word or NULL                                  */
+  uint32_t nseq, block_tokens, max_blocks, max_tokens;
+} paged_build_tables_t;
+
+typedef struct {
+  const paged_cache_t* cache;
+  const void *k, *v;                      /* [ntok] rows of [num_kv_heads][head_dim]              */
+  uint64_t k_stride, v_stride;            /* bytes from a row to the next                         */
+  const int64_t* slots;                   /* [ntok]                                               */
+  int32_t* status;
+  uint32_t ntok;
+} paged_write_kv_t;
+
+typedef struct {
+  const paged_cache_t* cache;
+  const int32_t* tables;                  /* [nseq] rows of max_blocks cells                      */
+  uint64_t table_stride;
+  const int32_t* lens;                    /* [nseq]                                               */
+  const void* q;
+  uint64_t q_stride;                      /* bytes from a sequence's rows to the next one's       */
+  void* out;
+  uint64_t out_stride;
+  float* lse;                             /* paged_decode_tables: [nseq][num_heads], or NULL      */
+  const float* lam;                       /* paged_decode_diff: [num_heads]                       */
+  const float* norm_weight;               /* paged_decode_diff: [head_dim], or NULL               */
+  void* workspace;
+  uint64_t workspace_bytes;
+  int32_t* status;
+  uint32_t nseq, max_blocks;
+  uint32_t num_heads;                     /* query heads, which are the output's heads            */
+  uint32_t window;                        /* 0: none                                              */
+  float sm_scale;
+  float eps, out_scale;                   /* paged_decode_diff                                    */
+} paged_decode_t;
+
 /* Block tables and slot maps from request lengths. Request i holds lens[i] tokens in the blocks
  * tables[i][0 .. ceil(lens[i] / block_tokens)) and is to hold new_lens[i]:
  *   growing     the blocks it lacks are popped (request order, then logical order; the first arena's stack
@@ -566,35 +610,30 @@ typedef struct {
  * a stack's top outside its capacity), ENOSPC (too few free ids): then nothing has changed, free_out is
  * free_in, and all offsets are 0. EINVAL also when ids pushed would exceed a stack's capacity: those are dropped.
  * Returns EINVAL (NULL, block_tokens), ECUDA. */
-int paged_build_tables(const paged_pool_t* pool, const int32_t* lens, const int32_t* new_lens, uint32_t nseq, uint32_t block_tokens,
-                       int32_t* tables, uint64_t table_stride, uint32_t max_blocks, int32_t* offsets, int64_t* slots, int32_t* positions,
-                       uint32_t max_tokens, int32_t* status, void* stream);
+int paged_build_tables(const paged_build_tables_t* args, void* stream);
 
 /* K and V rows [ntok][num_kv_heads][head_dim] of new tokens (canonical order; strides between tokens) into the
  * blocks their slots name. PAGED_NO_SLOT skips a row. Slots must be distinct: of two equal ones, each
  * 16 bytes of the row may come from either. Status: EINVAL (a slot outside its arena: the row is skipped).
  * Returns EINVAL, ECUDA. */
-int paged_write_kv(const paged_cache_t* cache, const void* k, uint64_t k_stride, const void* v, uint64_t v_stride, const int64_t* slots,
-                   uint32_t ntok, int32_t* status, void* stream);
+int paged_write_kv(const paged_write_kv_t* args, void* stream);
 
-/* Bytes of workspace that the two calls below need for num_q_rows query rows per sequence (num_q_heads, or twice
- * num_heads for the differential form), independent of batch and lengths. Before its first use the
- * workspace's first 16384 bytes must be 0; every call leaves them 0. */
+/* Bytes of workspace that the two calls below need for num_q_rows query rows per sequence (num_heads, or twice
+ * that for the differential form), independent of batch and lengths. Before its first use the
+ * workspace's first 16384 bytes must be 0; every call leaves them 0 (one that ended with SLICE_ETIMEOUT may not: clear them again). */
 int paged_decode_workspace(const paged_cache_t* cache, uint32_t num_q_rows, uint64_t* out_bytes);
 
-/* Attention of one new token per sequence: for query head h (KV head h / G, G = num_q_heads / num_kv_heads in 1..16)
+/* Attention of one new token per sequence: for query head h (KV head h / G, G = num_heads / num_kv_heads in 1..16)
  *   out[i][h] = softmax(sm_scale * q[i][h] K^T) V over positions max(0, len - window) .. len - 1
  * (window 0: all), read through tables[i]; cells of blocks without such a position are not read.
- *   q, out   [nseq] rows of [num_q_heads][head_dim], q_stride / out_stride bytes apart
- *   lse      [nseq][num_q_heads] f32 (natural-log sum of exponentials), or NULL
+ *   q, out   [nseq] rows of [num_heads][head_dim], q_stride / out_stride bytes apart
+ *   lse      [nseq][num_heads] f32 (natural-log sum of exponentials), or NULL
  * A sequence of length 0 gets zeros and minus infinity. What block tails hold does not matter; the rows of V that are
  * attended to must be finite. Arithmetic: 16-bit products, f32 accumulation and softmax, result rounded once.
  * The result does not depend on timing. Status: EINVAL (length below 0 or above max_blocks * block_tokens: zeros, like
  * an empty sequence; an entry outside its arena: reads as zeros, the row is not meaningful).
  * Returns EINVAL, ESCRATCH (workspace too small), ECUDA. */
-int paged_decode_tables(const paged_cache_t* cache, const int32_t* tables, uint64_t table_stride, uint32_t max_blocks, const int32_t* lens,
-                        uint32_t nseq, const void* q, uint64_t q_stride, uint32_t num_q_heads, float sm_scale, uint32_t window, void* out,
-                        uint64_t out_stride, float* lse_or_null, void* workspace, uint64_t workspace_bytes, int32_t* status, void* stream);
+int paged_decode_tables(const paged_decode_t* args, void* stream);
 
 /* Differential attention of one new token per sequence: two softmax maps over the same values, the second one
  * subtracted with a learned weight. With D = head_dim, d = D / 2, the K plane's heads are pairs: head g of the cache
@@ -605,10 +644,7 @@ int paged_decode_tables(const paged_cache_t* cache, const int32_t* tables, uint6
  *   q        [nseq] rows of [2 * num_heads][d]; out [nseq] rows of [num_heads][D]
  *   lam      [num_heads] f32, norm_weight [D] f32 (device)
  * Everything else as in paged_decode_tables (zeros for an empty sequence). */
-int paged_decode_diff(const paged_cache_t* cache, const int32_t* tables, uint64_t table_stride, uint32_t max_blocks, const int32_t* lens,
-                      uint32_t nseq, const void* q, uint64_t q_stride, uint32_t num_heads, const float* lam, float sm_scale, uint32_t window,
-                      const float* norm_weight_or_null, float eps, float out_scale, void* out, uint64_t out_stride, void* workspace,
-                      uint64_t workspace_bytes, int32_t* status, void* stream);
+int paged_decode_diff(const paged_decode_t* args, void* stream);
 
 const char* slice_strerror(int code);
 

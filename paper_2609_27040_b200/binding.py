@@ -9,6 +9,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import struct as _struct
 from typing import Optional, Sequence
 
 import numpy as np
@@ -143,13 +144,9 @@ def lib() -> C.CDLL:
         L.slice_cta_trace.argtypes = [vp, i32, vp, u64, vp, vp]
         L.slice_copy_blocks.argtypes = [vp, vp, vp, vp, u32, u64, u32, u32, vp]
         L.slice_copy_blocks_series.argtypes = [vp, u32, u64, vp, vp, u64, u32, u64, i32, u32, u32, vp]
-        pc, f32 = C.POINTER(PagedCacheDesc), C.c_float
-        L.paged_build_tables.argtypes = [C.POINTER(PagedPoolDesc), vp, vp, u32, u32, vp, u64, u32, vp, vp, vp, u32, vp, vp]
-        L.paged_write_kv.argtypes = [pc, vp, u64, vp, u64, vp, u32, vp, vp]
-        L.paged_decode_workspace.argtypes = [pc, u32, C.POINTER(u64)]
-        L.paged_decode_tables.argtypes = [pc, vp, u64, u32, vp, u32, vp, u64, u32, f32, u32, vp, u64, vp, vp, u64, vp, vp]
-        L.paged_decode_diff.argtypes = [pc, vp, u64, u32, vp, u32, vp, u64, u32, vp, f32, u32, vp, f32, f32, vp, u64, vp, u64,
-                                        vp, vp]
+        for name in ("paged_build_tables", "paged_write_kv", "paged_decode_tables", "paged_decode_diff"):
+            getattr(L, name).argtypes = [C.c_char_p, vp]              # a packed argument struct, the stream
+        L.paged_decode_workspace.argtypes = [C.POINTER(PagedCacheDesc), u32, C.POINTER(u64)]
         L.slice_strerror.argtypes = [C.c_int]
         L.slice_strerror.restype = C.c_char_p
         _lib = L
@@ -447,8 +444,13 @@ def slice_schedule_gll(slices) -> int:
 
 
 # -- device-driven path: torch tensors in, one launch per call ---------------------------------------
-# The checks read as little of a tensor as they can and build their messages only when they fail: a call
-# takes the host a few microseconds, about what its kernel takes the GPU on a small batch.
+# On a small batch the host's part of a call takes longer than the kernel: the checks read as little of a tensor as they
+# can and build their messages only when they fail, and the argument structs of the C ABI are packed in one go (ctypes
+# takes 2 us to convert 18 arguments one by one, 0.6 us this way).
+
+_BUILD = _struct.Struct("=9Q4I")                       # paged_build_tables_t
+_WRITE = _struct.Struct("=7QI4x")                      # paged_write_kv_t
+_DECODE = _struct.Struct("=14Q4I3f4x")                 # paged_decode_t
 
 _I32 = _I64 = _F32 = None                             # torch's dtypes, once a cache or a pool has been made
 
@@ -505,7 +507,7 @@ class PagedCache:
             d.blocks[j], d.base[j] = t.shape[0], t.data_ptr()
             d.block_stride[j] = t.stride(0) * 2 if t.shape[0] > 1 else 0
         d.dtype, d.block_tokens, d.num_kv_heads, d.head_dim = kinds[ref.dtype], ref.shape[2], ref.shape[3], ref.shape[4]
-        self.desc, self._ref = d, C.byref(d)
+        self.desc, self._ref, self._addr = d, C.byref(d), C.addressof(d)
         self.local, self.lent = local, lent
         self.dtype, self.device, self._dev = ref.dtype, ref.device, ref.get_device()
         self.block_tokens, self.num_kv_heads, self.head_dim = ref.shape[2], ref.shape[3], ref.shape[4]
@@ -526,34 +528,38 @@ class PagedPool:
         if not work.is_contiguous() or work.get_device() != dev or work.numel() * work.element_size() < PAGED_POOL_WORK_BYTES:
             _refuse("work: PAGED_POOL_WORK_BYTES on the pool's device")
         d.work = work.data_ptr()
-        self.desc, self._ref, self.device, self._dev = d, C.byref(d), free.device, dev
+        self.desc, self._addr, self.device, self._dev = d, C.addressof(d), free.device, dev
         self._keep = (local_ids, lent_ids, free, free_out, work)
 
 
 def _table(t, n: int, dev: int):
     """Address, entries from a row to the next, and width of the tables."""
-    if t.dim() != 2 or t.dtype is not _I32 or t.get_device() != dev or t.shape[0] != n or (t.stride(1) != 1 and t.shape[1] > 1):
-        _refuse(f"tables: expected int32 [{n}][max_blocks] on device {dev}, rows contiguous, got {tuple(t.shape)} of {t.dtype} on {t.device}")
-    width = t.shape[1]
-    return t.data_ptr(), (t.stride(0) if n > 1 else width), width
+    shape, strides = t.shape, t.stride()
+    if len(shape) != 2 or t.dtype is not _I32 or t.get_device() != dev or shape[0] != n or (strides[1] != 1 and shape[1] > 1):
+        _refuse(f"tables: expected int32 [{n}][max_blocks] on device {dev}, rows contiguous, got {tuple(shape)} of {t.dtype} on {t.device}")
+    return t.data_ptr(), (strides[0] if n > 1 else shape[1]), shape[1]
+
+
+def _status(t, dev: int) -> int:
+    return 0 if t is None else _words(t, "status", dev, _I32, (1,))
 
 
 def paged_build_tables(pool: PagedPool, lens, new_lens, block_tokens: int, tables, offsets, slots, positions, status=None,
                        stream=None) -> int:
     dev, n, room = pool._dev, lens.numel(), slots.numel()
     tab, stride, width = _table(tables, n, dev)
-    return lib().paged_build_tables(pool._ref, _words(lens, "lens", dev, _I32), _words(new_lens, "new_lens", dev, _I32, (n,)), n, block_tokens,
-                                    tab, stride, width, _words(offsets, "offsets", dev, _I32, (n + 1,)), _words(slots, "slots", dev, _I64),
-                                    _words(positions, "positions", dev, _I32, (room,)), room,
-                                    None if status is None else _words(status, "status", dev, _I32, (1,)), _stream(stream))
+    args = _BUILD.pack(pool._addr, _words(lens, "lens", dev, _I32), _words(new_lens, "new_lens", dev, _I32, (n,)), tab, stride,
+                       _words(offsets, "offsets", dev, _I32, (n + 1,)), _words(slots, "slots", dev, _I64),
+                       _words(positions, "positions", dev, _I32, (room,)), _status(status, dev), n, block_tokens, width, room)
+    return lib().paged_build_tables(args, _stream(stream))
 
 
 def paged_write_kv(cache: PagedCache, k, v, slots, status=None, stream=None) -> int:
     dev, n = cache._dev, slots.numel()
     ks = _row_stride(k, "k", dev, cache.dtype, n, cache.num_kv_heads, cache.head_dim)
     vs = _row_stride(v, "v", dev, cache.dtype, n, cache.num_kv_heads, cache.head_dim)
-    return lib().paged_write_kv(cache._ref, k.data_ptr(), ks, v.data_ptr(), vs, _words(slots, "slots", dev, _I64), n,
-                                None if status is None else _words(status, "status", dev, _I32, (1,)), _stream(stream))
+    args = _WRITE.pack(cache._addr, k.data_ptr(), v.data_ptr(), ks, vs, _words(slots, "slots", dev, _I64), _status(status, dev), n)
+    return lib().paged_write_kv(args, _stream(stream))
 
 
 def paged_decode_workspace(cache: PagedCache, num_q_rows: int) -> int:
@@ -575,26 +581,29 @@ def _workspace(work, dev: int):
 def paged_decode_tables(cache: PagedCache, tables, lens, q, sm_scale: float, out, workspace, lse=None, window: int = 0, status=None,
                         stream=None) -> int:
     dev, n, heads, d = cache._dev, lens.numel(), q.shape[1], cache.head_dim
-    qs, os_ = _row_stride(q, "q", dev, cache.dtype, n, heads, d), _row_stride(out, "out", dev, cache.dtype, n, heads, d)
     if window < 0:
         _refuse("a window is 0 (none) or more")
     tab, stride, width = _table(tables, n, dev)
     ws, wb = _workspace(workspace, dev)
-    return lib().paged_decode_tables(cache._ref, tab, stride, width, _words(lens, "lens", dev, _I32), n, q.data_ptr(), qs, heads, sm_scale,
-                                     window, out.data_ptr(), os_, None if lse is None else _words(lse, "lse", dev, _F32, (n, heads)), ws, wb,
-                                     None if status is None else _words(status, "status", dev, _I32, (1,)), _stream(stream))
+    args = _DECODE.pack(cache._addr, tab, stride, _words(lens, "lens", dev, _I32),
+                        q.data_ptr(), _row_stride(q, "q", dev, cache.dtype, n, heads, d),
+                        out.data_ptr(), _row_stride(out, "out", dev, cache.dtype, n, heads, d),
+                        0 if lse is None else _words(lse, "lse", dev, _F32, (n, heads)), 0, 0, ws, wb, _status(status, dev),
+                        n, width, heads, window, sm_scale, 0.0, 1.0)
+    return lib().paged_decode_tables(args, _stream(stream))
 
 
 def paged_decode_diff(cache: PagedCache, tables, lens, q, lam, sm_scale: float, out, workspace, norm_weight=None, eps: float = 1e-5,
                       out_scale: float = 1.0, window: int = 0, status=None, stream=None) -> int:
     dev, n, heads, d = cache._dev, lens.numel(), out.shape[1], cache.head_dim
-    qs, os_ = _row_stride(q, "q", dev, cache.dtype, n, 2 * heads, d // 2), _row_stride(out, "out", dev, cache.dtype, n, heads, d)
     if window < 0:
         _refuse("a window is 0 (none) or more")
     tab, stride, width = _table(tables, n, dev)
     ws, wb = _workspace(workspace, dev)
-    return lib().paged_decode_diff(cache._ref, tab, stride, width, _words(lens, "lens", dev, _I32), n, q.data_ptr(), qs, heads,
-                                   _words(lam, "lam", dev, _F32, (heads,)), sm_scale, window,
-                                   None if norm_weight is None else _words(norm_weight, "norm_weight", dev, _F32, (d,)), eps, out_scale,
-                                   out.data_ptr(), os_, ws, wb, None if status is None else _words(status, "status", dev, _I32, (1,)),
-                                   _stream(stream))
+    args = _DECODE.pack(cache._addr, tab, stride, _words(lens, "lens", dev, _I32),
+                        q.data_ptr(), _row_stride(q, "q", dev, cache.dtype, n, 2 * heads, d // 2),
+                        out.data_ptr(), _row_stride(out, "out", dev, cache.dtype, n, heads, d),
+                        0, _words(lam, "lam", dev, _F32, (heads,)),
+                        0 if norm_weight is None else _words(norm_weight, "norm_weight", dev, _F32, (d,)), ws, wb, _status(status, dev),
+                        n, width, heads, window, sm_scale, eps, out_scale)
+    return lib().paged_decode_diff(args, _stream(stream))

@@ -32,24 +32,56 @@ BAD_CACHES = [dict(dtype=2), dict(num_kv_heads=0), dict(num_kv_heads=65), dict(h
 P = 1 << 20                                                        # an aligned address that is never touched: these calls are refused first
 
 
-def decode(cache, **kw):
-    a = dict(tables=P, table_stride=10, max_blocks=10, lens=P, nseq=2, q=P, q_stride=32 * 256, heads=32, scale=1.0, window=0, out=P,
-             out_stride=32 * 256, lse=None, work=P, work_bytes=1 << 30, status=None, stream=None)
+VP, U64, U32, F32 = C.c_void_p, C.c_uint64, C.c_uint32, C.c_float
+
+
+class Build(C.Structure):                                          # the header's argument structs, field by field
+    _fields_ = [("pool", VP), ("lens", VP), ("new", VP), ("tables", VP), ("stride", U64), ("offsets", VP), ("slots", VP), ("positions", VP),
+                ("status", VP), ("n", U32), ("T", U32), ("width", U32), ("tokens", U32)]
+
+
+class Write(C.Structure):
+    _fields_ = [("cache", VP), ("k", VP), ("v", VP), ("ks", U64), ("vs", U64), ("slots", VP), ("status", VP), ("ntok", U32)]
+
+
+class Decode(C.Structure):
+    _fields_ = [("cache", VP), ("tables", VP), ("table_stride", U64), ("lens", VP), ("q", VP), ("q_stride", U64), ("out", VP),
+                ("out_stride", U64), ("lse", VP), ("lam", VP), ("norm", VP), ("work", VP), ("work_bytes", U64), ("status", VP),
+                ("nseq", U32), ("max_blocks", U32), ("heads", U32), ("window", U32), ("scale", F32), ("eps", F32), ("out_scale", F32)]
+
+
+def call(name, args):
+    return getattr(B.lib(), name)(C.cast(C.byref(args), C.c_char_p), None)
+
+
+def decode(cache, name="paged_decode_tables", **kw):
+    a = dict(cache=C.addressof(cache), tables=P, table_stride=10, max_blocks=10, lens=P, nseq=2, q=P, q_stride=32 * 256, heads=32, scale=1.0,
+             out=P, out_stride=32 * 256, work=P, work_bytes=1 << 30)
     a.update(kw)
-    return B.lib().paged_decode_tables(C.byref(cache), *a.values())
+    return call(name, Decode(**a))
 
 
 def diff(cache, **kw):
-    a = dict(tables=P, table_stride=10, max_blocks=10, lens=P, nseq=2, q=P, q_stride=32 * 256, heads=32, lam=P, scale=1.0, window=0,
-             norm=None, eps=1e-5, out_scale=1.0, out=P, out_stride=32 * 256, work=P, work_bytes=1 << 30, status=None, stream=None)
-    a.update(kw)
-    return B.lib().paged_decode_diff(C.byref(cache), *a.values())
+    return decode(cache, "paged_decode_diff", **{**dict(lam=P, eps=1e-5, out_scale=1.0), **kw})
 
 
 def write(cache, **kw):
-    a = dict(k=P, ks=2048, v=P, vs=2048, slots=P, ntok=3, status=None, stream=None)
+    a = dict(cache=C.addressof(cache), k=P, ks=2048, v=P, vs=2048, slots=P, ntok=3)
     a.update(kw)
-    return B.lib().paged_write_kv(C.byref(cache), *a.values())
+    return call("paged_write_kv", Write(**a))
+
+
+def test_packed_arguments_are_the_headers_structs():
+    for fmt, cls in ((B._BUILD, Build), (B._WRITE, Write), (B._DECODE, Decode)):
+        assert fmt.size == C.sizeof(cls)
+        values = [float(i) if t is F32 else i + 1 for i, (_, t) in enumerate(cls._fields_)]
+        assert fmt.pack(*values) == bytes(cls(*values))
+
+
+def test_no_arguments_at_all():
+    for name in ("paged_build_tables", "paged_write_kv", "paged_decode_tables", "paged_decode_diff"):
+        assert getattr(B.lib(), name)(None, None) == B.EINVAL
+        assert getattr(B.lib(), name)(bytes(200), None) == B.EINVAL
 
 
 @pytest.mark.parametrize("kw", BAD_CACHES, ids=str)
@@ -77,15 +109,17 @@ def test_bad_differential_arguments_are_refused():
     assert diff(desc(), norm=P, eps=-1.0) == B.EINVAL
     assert diff(desc(), norm=P, eps=float("nan")) == B.EINVAL
     assert diff(desc(), norm=P + 2) == B.EINVAL and diff(desc(), lam=P + 1) == B.EINVAL
+    assert diff(desc(), lse=P) == B.EINVAL                         # one call's outputs and weights given to the other
+    assert decode(desc(), lam=P) == B.EINVAL and decode(desc(), norm=P) == B.EINVAL and decode(desc(), lse=P + 2) == B.EINVAL
 
 
 def test_workspace_too_small():
     need = C.c_uint64(0)
     assert B.lib().paged_decode_workspace(C.byref(desc()), 32, C.byref(need)) == B.OK and need.value > 16384
     assert decode(desc(), work_bytes=need.value - 1) == B.ESCRATCH
-    twice = C.c_uint64(0)
-    assert B.lib().paged_decode_workspace(C.byref(desc()), 64, C.byref(twice)) == B.OK and twice.value > need.value
-    assert diff(desc(), work_bytes=need.value) == B.ESCRATCH       # the differential form has two rows to a head
+    more = C.c_uint64(0)
+    assert B.lib().paged_decode_workspace(C.byref(desc()), 128, C.byref(more)) == B.OK and more.value > need.value
+    assert diff(desc(), heads=64, q_stride=64 * 256, out_stride=64 * 256, work_bytes=need.value) == B.ESCRATCH   # two rows to a head
     for rows in (0, 12, 136):
         assert B.lib().paged_decode_workspace(C.byref(desc()), rows, C.byref(need)) == B.EINVAL
     assert B.lib().paged_decode_workspace(C.byref(desc()), 32, None) == B.EINVAL
@@ -109,9 +143,9 @@ def build(pool_kw=None, **kw):
             getattr(p, k)[v[0]] = v[1]
         else:
             setattr(p, k, v)
-    a = dict(lens=P, new=P, n=3, T=16, tables=P, stride=8, width=8, offsets=P, slots=P, positions=P, tokens=100, status=None, stream=None)
+    a = dict(pool=C.addressof(p), lens=P, new=P, n=3, T=16, tables=P, stride=8, width=8, offsets=P, slots=P, positions=P, tokens=100)
     a.update(kw)
-    return B.lib().paged_build_tables(C.byref(p), *a.values())
+    return call("paged_build_tables", Build(**a))
 
 
 def test_bad_build_arguments_are_refused():
