@@ -542,7 +542,8 @@ typedef struct {
   int32_t* ids[2];                        /* [capacity]; NULL when the capacity is 0              */
   uint32_t capacity[2];
   const int32_t* free_in;                 /* [2] ids on each stack before the call                */
-  int32_t* free_out;                      /* [2] and after it; may be the same array as free_in  */
+  int32_t* free_out;                      /* [2] and after it: the same array as free_in, or
+                                             another one                                         */
   uint32_t* work;                         /* a word that is 0 before the first call; every call
                                              leaves it 0                                         */
 } paged_pool_t;

@@ -125,6 +125,7 @@ int paged_build_tables(const paged_build_tables_t* a, void* stream) {
   if (!aligned(pool.free_in, 4) || !aligned(pool.free_out, 4) || !aligned(pool.work, 4) || !aligned(a->status, 4)) return SLICE_EINVAL;
   for (int j = 0; j < 2; ++j)
     if ((pool.capacity[j] && !pool.ids[j]) || pool.capacity[j] > kMost || !aligned(pool.ids[j], 4)) return SLICE_EINVAL;
+  if (pool.free_out == pool.free_in + 1 || pool.free_in == pool.free_out + 1) return SLICE_EINVAL;  // the same counts, or others
   if (!a->offsets || !aligned(a->offsets, 4) || a->nseq > kMost - 1 || a->max_tokens > kMost) return SLICE_EINVAL;
   if (a->nseq && (!a->lens || !a->new_lens || !a->tables || !aligned(a->lens, 4) || !aligned(a->new_lens, 4) || !aligned(a->tables, 4)))
     return SLICE_EINVAL;

@@ -154,7 +154,7 @@ def test_bad_build_arguments_are_refused():
                dict(n=0x7fffffff), dict(slots=P + 4), dict(tables=P + 2), dict(offsets=P + 2), dict(status=P + 3), dict(lens=P + 2)):
         assert build(**kw) == B.EINVAL, kw
     for kw in (dict(ids=(0, None)), dict(capacity=(1, 5)), dict(capacity=(0, 0x80000000)), dict(free_in=None), dict(free_out=None),
-               dict(work=None), dict(work=P + 2), dict(ids=(0, P + 2))):
+               dict(work=None), dict(free_out=P + 4), dict(free_in=P + 4), dict(work=P + 2), dict(ids=(0, P + 2))):
         assert build(kw) == B.EINVAL, kw
 
 
