@@ -551,7 +551,7 @@ def paged_build_tables(pool: PagedPool, lens, new_lens, block_tokens: int, table
     args = _BUILD.pack(pool._addr, _words(lens, "lens", dev, _I32), _words(new_lens, "new_lens", dev, _I32, (n,)), tab, stride,
                        _words(offsets, "offsets", dev, _I32, (n + 1,)), _words(slots, "slots", dev, _I64),
                        _words(positions, "positions", dev, _I32, (room,)), _status(status, dev), n, block_tokens, width, room)
-    return lib().paged_build_tables(args, _stream(stream))
+    return (_lib or lib()).paged_build_tables(args, stream if stream is None or isinstance(stream, int) else stream.cuda_stream)
 
 
 def paged_write_kv(cache: PagedCache, k, v, slots, status=None, stream=None) -> int:
@@ -559,7 +559,7 @@ def paged_write_kv(cache: PagedCache, k, v, slots, status=None, stream=None) -> 
     ks = _row_stride(k, "k", dev, cache.dtype, n, cache.num_kv_heads, cache.head_dim)
     vs = _row_stride(v, "v", dev, cache.dtype, n, cache.num_kv_heads, cache.head_dim)
     args = _WRITE.pack(cache._addr, k.data_ptr(), v.data_ptr(), ks, vs, _words(slots, "slots", dev, _I64), _status(status, dev), n)
-    return lib().paged_write_kv(args, _stream(stream))
+    return (_lib or lib()).paged_write_kv(args, stream if stream is None or isinstance(stream, int) else stream.cuda_stream)
 
 
 def paged_decode_workspace(cache: PagedCache, num_q_rows: int) -> int:
@@ -590,7 +590,7 @@ def paged_decode_tables(cache: PagedCache, tables, lens, q, sm_scale: float, out
                         out.data_ptr(), _row_stride(out, "out", dev, cache.dtype, n, heads, d),
                         0 if lse is None else _words(lse, "lse", dev, _F32, (n, heads)), 0, 0, ws, wb, _status(status, dev),
                         n, width, heads, window, sm_scale, 0.0, 1.0)
-    return lib().paged_decode_tables(args, _stream(stream))
+    return (_lib or lib()).paged_decode_tables(args, stream if stream is None or isinstance(stream, int) else stream.cuda_stream)
 
 
 def paged_decode_diff(cache: PagedCache, tables, lens, q, lam, sm_scale: float, out, workspace, norm_weight=None, eps: float = 1e-5,
@@ -606,4 +606,4 @@ def paged_decode_diff(cache: PagedCache, tables, lens, q, lam, sm_scale: float, 
                         0, _words(lam, "lam", dev, _F32, (heads,)),
                         0 if norm_weight is None else _words(norm_weight, "norm_weight", dev, _F32, (d,)), ws, wb, _status(status, dev),
                         n, width, heads, window, sm_scale, eps, out_scale)
-    return lib().paged_decode_diff(args, _stream(stream))
+    return (_lib or lib()).paged_decode_diff(args, stream if stream is None or isinstance(stream, int) else stream.cuda_stream)

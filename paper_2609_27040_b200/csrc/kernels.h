@@ -301,6 +301,7 @@ struct PagedDecodeParams {
   int* status;
 };
 size_t paged_workspace_bytes(uint32_t rows, uint32_t head_dim);
-cudaError_t launch_paged_decode(const PagedDecodeParams& p, int num_sms, cudaStream_t stream);
+// dev < 64: the current device.
+cudaError_t launch_paged_decode(const PagedDecodeParams& p, int dev, int num_sms, cudaStream_t stream);
 
 }  // namespace ema

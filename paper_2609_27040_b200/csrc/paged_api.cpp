@@ -31,7 +31,7 @@ bool cache_ok(const paged_cache_t* c, uint64_t (&stride)[2]) {
 }
 
 // The call's memory has to be reachable from the current device: memory of another one is refused.
-int device_ok(const void* p, int* sms) {
+int device_ok(const void* p, int* sms, int* device = nullptr) {
   static int sms_of[64] = {};
   int dev = 0;
   if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return SLICE_ECUDA;
@@ -44,6 +44,7 @@ int device_ok(const void* p, int* sms) {
   if (at.type == cudaMemoryTypeUnregistered) return SLICE_EINVAL;
   if (!sms_of[dev] && cudaDeviceGetAttribute(&sms_of[dev], cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) return SLICE_ECUDA;
   *sms = sms_of[dev];
+  if (device) *device = dev;
   return SLICE_OK;
 }
 
@@ -69,8 +70,8 @@ int decode(const paged_decode_t* a, bool diff, void* stream) {
       !aligned(a->lse, 4) || !aligned(a->lam, 4) || !aligned(a->norm_weight, 4) || !aligned(a->status, 4))
     return SLICE_EINVAL;
   if (a->workspace_bytes < ema::paged_workspace_bytes(rows, c->head_dim)) return SLICE_ESCRATCH;
-  int sms = 0;
-  const int rc = device_ok(a->out, &sms);
+  int sms = 0, dev = 0;
+  const int rc = device_ok(a->out, &sms, &dev);
   if (rc) return rc;
   ema::PagedDecodeParams p{};
   for (int j = 0; j < 2; ++j) {
@@ -111,7 +112,7 @@ int decode(const paged_decode_t* a, bool diff, void* stream) {
   p.eps = a->eps;
   p.out_scale = a->out_scale;
   p.status = a->status;
-  return launched(ema::launch_paged_decode(p, sms, static_cast<cudaStream_t>(stream)));
+  return launched(ema::launch_paged_decode(p, dev, sms, static_cast<cudaStream_t>(stream)));
 }
 
 }  // namespace

@@ -167,6 +167,22 @@ __device__ __forceinline__ bool wait_on(uint64_t* bar, uint32_t parity, Sh& sh, 
   return false;
 }
 
+// The same for what the CTA's other warps do: however long that takes, as long as it goes on.
+template <typename Sh>
+__device__ __forceinline__ bool wait_for(uint64_t* bar, uint32_t parity, Sh& sh, int* status) {
+  if (ptx::mbar_try_wait(ptx::smem_u32(bar), parity)) return true;
+  for (;;) {
+    if (*reinterpret_cast<volatile uint32_t*>(&sh.dead)) return false;
+    const uint32_t before = *reinterpret_cast<volatile uint32_t*>(&sh.started);
+    if (ptx::mbar_wait(ptx::smem_u32(bar), parity, nullptr, 0)) return true;
+    if (*reinterpret_cast<volatile uint32_t*>(&sh.started) == before) {
+      ptx::report_status(status, kDevTimeout);
+      *reinterpret_cast<volatile uint32_t*>(&sh.dead) = 1;
+      return false;
+    }
+  }
+}
+
 // Whether the phase has completed: does not wait.
 __device__ __forceinline__ bool ready(uint64_t* bar, uint32_t parity) {
   uint32_t done;
@@ -559,10 +575,15 @@ __device__ void schedule(const PagedDecodeParams& p, Shared<D, NT>& sh, const Zo
     // Not too far ahead: what is drawn here cannot be drawn by a CTA that is faster. The consumers count the chunks that they
     // have started copies of.
     uint64_t t0 = 0;
-    for (uint32_t polls = 0; j && static_cast<int32_t>(number - *reinterpret_cast<volatile uint32_t*>(&sh.started)) >= static_cast<int32_t>(kAhead); ++polls) {
+    uint32_t seen = 0;
+    for (uint32_t polls = 0; j; ++polls) {
+      const uint32_t started = *reinterpret_cast<volatile uint32_t*>(&sh.started);
+      if (static_cast<int32_t>(number - started) < static_cast<int32_t>(kAhead)) break;
       if (*reinterpret_cast<volatile uint32_t*>(&sh.dead)) return;
-      if (polls == 0) t0 = ptx::global_timer_ns();
-      if ((polls & 63u) == 63u && ptx::global_timer_ns() - t0 > 4000000000ull) {  // longer than the consumers' own waits
+      if (polls == 0 || started != seen) {
+        t0 = ptx::global_timer_ns();
+        seen = started;
+      } else if ((polls & 63u) == 63u && ptx::global_timer_ns() - t0 > 4000000000ull) {  // longer than the consumers' own waits
         *reinterpret_cast<volatile uint32_t*>(&sh.dead) = 1;
         ptx::report_status(p.status, kDevTimeout);
         return;
@@ -571,7 +592,7 @@ __device__ void schedule(const PagedDecodeParams& p, Shared<D, NT>& sh, const Zo
     }
     __syncwarp();
     while (j - tail >= kNotes) {
-      if (!__all_sync(0xffffffffu, wait_on(&sh.note_empty[tail % kNotes], tail / kNotes & 1u, sh, p.status))) return;
+      if (!__all_sync(0xffffffffu, wait_for(&sh.note_empty[tail % kNotes], tail / kNotes & 1u, sh, p.status))) return;
       ++tail;
     }
     if (left == 0) {
@@ -600,13 +621,20 @@ __device__ void schedule(const PagedDecodeParams& p, Shared<D, NT>& sh, const Zo
       uint32_t before = sh.pieces_before[x];
       parts = sh.parts_before[x];
       at = sh.chunks_before[x];
-      for (seq = x * run;; ++seq) {
+      for (seq = x * run; seq < p.nseq; ++seq) {
         span = span_of<kTok>(p, seq);
         cut = cut_of(zones, at, span.chunks, p.num_kv_heads);
         if (ticket < before + cut.all) break;
         before += cut.all;
         parts += cut.parts;
         at += static_cast<unsigned long long>(span.chunks) * p.num_kv_heads;
+      }
+      if (seq == p.nseq) {  // only if the lengths have changed since they were added up: no more is read
+        if (lane == 0) {
+          note.chunks = 0;
+          arrive(&sh.note_full[j % kNotes]);
+        }
+        return;
       }
       head = 0;
       index = ticket - before;
@@ -629,11 +657,27 @@ __device__ void schedule(const PagedDecodeParams& p, Shared<D, NT>& sh, const Zo
         head = 0;
         do {
           at += static_cast<unsigned long long>(span.chunks) * p.num_kv_heads;
-          span = span_of<kTok>(p, ++seq);
+          ++seq;
+          span = seq < p.nseq ? span_of<kTok>(p, seq) : Span{0, 0, 0, 1};
         } while (span.chunks == 0);  // there is one: the ticket exists
+        if (seq == p.nseq) {
+          if (lane == 0) {
+            note.chunks = 0;
+            arrive(&sh.note_full[j % kNotes]);
+          }
+          return;
+        }
         cut = cut_of(zones, at, span.chunks, p.num_kv_heads);
       }
       count = pieces_of(cut, head);
+    }
+    if (count > 1 && parts + count > kPagedMaxParts) {  // as above: never with lengths that stay as they are
+      if (lane == 0) {
+        ptx::report_status(p.status, kStatusInvalid);
+        note.chunks = 0;
+        arrive(&sh.note_full[j % kNotes]);
+      }
+      return;
     }
     const uint32_t a = static_cast<uint32_t>(static_cast<uint64_t>(span.chunks) * index / count);
     const uint32_t b = static_cast<uint32_t>(static_cast<uint64_t>(span.chunks) * (index + 1) / count);
@@ -681,9 +725,10 @@ struct Feed {
   uint32_t c, chunks, step;     // next chunk of this warp in it, the piece's length, and from one of its chunks to the next
   uint32_t k;                   // c is chunk number k of those whose copies the lanes hold
   uint32_t seq, lo, len, chunk;
-  uint32_t id, x, row;          // this lane's copy: block, first element and token row
+  uint32_t x, row;              // this lane's copy: first element and token row
+  int32_t entry;                // and the table's entry for it
   uint32_t boxes;               // which lanes have one
-  bool second, end;
+  bool end;
 
   __device__ void init(const PagedDecodeParams& p) {
     box_shift = p.block_shift < kTokShift ? p.block_shift : kTokShift;
@@ -711,20 +756,14 @@ struct Feed {
     const uint32_t t = (chunk + mine) * kTok + ((lane & ((1u << split) - 1)) << box_shift);
     const bool on = mine < chunks && t < len && t + (1u << box_shift) > lo;
     k = 0;
-    id = 0;
-    second = false;
-    if (on) {
-      const int32_t e = p.tables[static_cast<uint64_t>(seq) * p.table_stride + (t >> p.block_shift)];
-      second = e < 0;
-      id = static_cast<uint32_t>(second ? ~e : e);
-      const uint32_t blocks = second ? p.blocks[1] : p.blocks[0];
-      if (id >= blocks) {  // a bad page: reads as zeros (a box outside the tensor), and is reported
-        ptx::report_status(p.status, kStatusInvalid);
-        id = blocks ? blocks : second ? p.blocks[0] : p.blocks[1];  // of an arena without blocks the map is the other one's
-      }
-    }
+    entry = on ? p.tables[static_cast<uint64_t>(seq) * p.table_stride + (t >> p.block_shift)] : 0;
     row = t & (p.block_tokens - 1);
     boxes = __ballot_sync(0xffffffffu, on);
+  }
+
+  // Reads the entries of a piece just opened, before anything else waits.
+  __device__ void prepare(const PagedDecodeParams& p) {
+    if (!end && c < chunks && k >= 32u >> split) look(p, threadIdx.x & 31u);
   }
 
   // Starts the copies of the next chunk, if there is one yet.
@@ -751,6 +790,13 @@ struct Feed {
     __syncwarp();
     if ((lane >> split) == k && (boxes >> lane & 1u)) {
       const uint32_t dst = ptx::smem_u32(sh.stage[warp][stage]) + (((lane & ((1u << split) - 1)) << box_shift) * (D * 2));
+      const bool second = entry < 0;
+      const uint32_t blocks = second ? p.blocks[1] : p.blocks[0];
+      uint32_t id = static_cast<uint32_t>(second ? ~entry : entry);
+      if (id >= blocks) {  // a bad page: reads as zeros (a box outside the tensor), and is reported
+        ptx::report_status(p.status, kStatusInvalid);
+        id = blocks ? blocks : second ? p.blocks[0] : p.blocks[1];  // of an arena without blocks the map is the other one's
+      }
       const CUtensorMap* map = second ? &maps.m[1] : &maps.m[0];
       tma_box(dst, map, x, row, id, bar, policy);
       tma_box(dst + kHalf, map, x, p.block_tokens + row, id, bar, policy);
@@ -840,13 +886,14 @@ __device__ void consume(const PagedDecodeParams& p, const Maps& maps, Shared<D, 
   feed.init(p);
   Rows<D, NT> r;
   for (uint32_t j = 0; alive; ++j) {
-    alive = __all_sync(0xffffffffu, wait_on(&sh.note_full[j % kNotes], j / kNotes & 1u, sh, p.status));
+    alive = __all_sync(0xffffffffu, wait_for(&sh.note_full[j % kNotes], j / kNotes & 1u, sh, p.status));
     if (!alive) break;
     const Note note = sh.note[j % kNotes];
     if (note.chunks == 0) break;
     if (j == 0 || feed.j < j) feed.open(note, j);  // nothing of the pieces before is left to copy
     const uint32_t c0 = first_chunk<S::kWarps>(note), step = note.solo ? 1u : S::kWarps;
     if (c0 < note.chunks) {
+      feed.prepare(p);
       uint32_t qf[kSteps][NT][2];
       load_q<D, NT>(p, note.seq, note.head, qf);
       while (issued - taken < kDepth && feed.issue(p, maps, sh, issued % kDepth, policy)) ++issued;
@@ -871,7 +918,7 @@ __device__ void consume(const PagedDecodeParams& p, const Maps& maps, Shared<D, 
     if (note.solo || (note.chunks == 1 && note.count == 1)) {
       if (c0 == 0) write_out<D, NT, kBf16>(p, r, note.seq, note.head);  // nobody else has rows of it
     } else {
-      alive = __all_sync(0xffffffffu, wait_on(&sh.rows_empty, (merges & 1u) ^ 1u, sh, p.status));
+      alive = __all_sync(0xffffffffu, wait_for(&sh.rows_empty, (merges & 1u) ^ 1u, sh, p.status));
       if (!alive) break;
       if (c0 < note.chunks) store_part<D, NT>(p, r, sh.part[warp]);
       __syncwarp();
@@ -888,10 +935,10 @@ __device__ void consume(const PagedDecodeParams& p, const Maps& maps, Shared<D, 
     return;
   }
   // Nothing left to stream: sums over parts go faster with all warps.
-  if (!__all_sync(0xffffffffu, wait_on(&sh.rows_empty, (merges & 1u) ^ 1u, sh, p.status))) return;
+  if (!__all_sync(0xffffffffu, wait_for(&sh.rows_empty, (merges & 1u) ^ 1u, sh, p.status))) return;
   if (lane == 0) atomicAdd(&sh.idle, 1u);
   for (uint32_t k = 0;; ++k) {
-    if (!__all_sync(0xffffffffu, wait_on(&sh.job_full, k & 1u, sh, p.status))) return;
+    if (!__all_sync(0xffffffffu, wait_for(&sh.job_full, k & 1u, sh, p.status))) return;
     if (sh.job_count == 0) return;
     sum_parts<D, NT>(p, sh, sh.job_slot, sh.job_stride, sh.job_count, sh.job_tile + warp, S::kWarps, r.m, r.l, [] { return true; });
     __syncwarp();
@@ -907,13 +954,13 @@ __device__ void merge(const PagedDecodeParams& p, Shared<D, NT>& sh) {
   uint32_t merges = 0, jobs = 0;
   Rows<D, NT> r;
   for (uint32_t j = 0;; ++j) {
-    if (!__all_sync(0xffffffffu, wait_on(&sh.note_full[j % kNotes], j / kNotes & 1u, sh, p.status))) return;
+    if (!__all_sync(0xffffffffu, wait_for(&sh.note_full[j % kNotes], j / kNotes & 1u, sh, p.status))) return;
     const Note note = sh.note[j % kNotes];
     if (note.chunks == 0) break;
     __syncwarp();
     if (lane == 0) arrive(&sh.note_empty[j % kNotes]);  // read: the copy is what counts from here on
     if (note.solo || (note.chunks == 1 && note.count == 1)) continue;
-    if (!__all_sync(0xffffffffu, wait_on(&sh.rows_full, merges & 1u, sh, p.status))) return;
+    if (!__all_sync(0xffffffffu, wait_for(&sh.rows_full, merges & 1u, sh, p.status))) return;
     ++merges;
     clear(r);
     const uint32_t parts = min(note.chunks, S::kWarps);
@@ -959,7 +1006,7 @@ __device__ void merge(const PagedDecodeParams& p, Shared<D, NT>& sh) {
             sh.job_tile = tile;
             arrive(&sh.job_full);
           }
-          if (!__all_sync(0xffffffffu, wait_on(&sh.job_done, jobs & 1u, sh, p.status))) return;
+          if (!__all_sync(0xffffffffu, wait_for(&sh.job_done, jobs & 1u, sh, p.status))) return;
           ++jobs;
         }
 #pragma unroll
@@ -1129,16 +1176,12 @@ EncodeFn encode_fn() {
 }
 
 template <uint32_t D, uint32_t NT, bool kBf16>
-cudaError_t launch(const PagedDecodeParams& p, const Maps& maps, uint32_t grid, cudaStream_t stream) {
+cudaError_t launch(const PagedDecodeParams& p, const Maps& maps, uint32_t grid, int dev, cudaStream_t stream) {
   constexpr size_t kSharedBytes = sizeof(Shared<D, NT>) + 128;
   static_assert(kSharedBytes <= 232448, "one CTA per SM");
   static bool ready[64] = {};  // the attribute is a property of the function on one device
-  int dev = 0;
-  cudaError_t e = cudaGetDevice(&dev);
-  if (e != cudaSuccess) return e;
-  if (dev < 0 || dev >= 64) return cudaErrorInvalidDevice;
   if (!ready[dev]) {
-    e = cudaFuncSetAttribute(paged_decode_kernel<D, NT, kBf16>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(kSharedBytes));
+    const cudaError_t e = cudaFuncSetAttribute(paged_decode_kernel<D, NT, kBf16>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(kSharedBytes));
     if (e != cudaSuccess) return e;
     ready[dev] = true;
   }
@@ -1147,9 +1190,9 @@ cudaError_t launch(const PagedDecodeParams& p, const Maps& maps, uint32_t grid, 
 }
 
 template <uint32_t D>
-cudaError_t launch_d(const PagedDecodeParams& p, const Maps& maps, uint32_t grid, cudaStream_t stream) {
-  if (p.dtype == 0) return p.rows <= 8 ? launch<D, 1, true>(p, maps, grid, stream) : launch<D, 2, true>(p, maps, grid, stream);
-  return p.rows <= 8 ? launch<D, 1, false>(p, maps, grid, stream) : launch<D, 2, false>(p, maps, grid, stream);
+cudaError_t launch_d(const PagedDecodeParams& p, const Maps& maps, uint32_t grid, int dev, cudaStream_t stream) {
+  if (p.dtype == 0) return p.rows <= 8 ? launch<D, 1, true>(p, maps, grid, dev, stream) : launch<D, 2, true>(p, maps, grid, dev, stream);
+  return p.rows <= 8 ? launch<D, 1, false>(p, maps, grid, dev, stream) : launch<D, 2, false>(p, maps, grid, dev, stream);
 }
 
 }  // namespace
@@ -1159,7 +1202,7 @@ size_t paged_workspace_bytes(uint32_t rows, uint32_t head_dim) {
   return kPagedCounterBytes + kPagedMaxParts * part;
 }
 
-cudaError_t launch_paged_decode(const PagedDecodeParams& p, int num_sms, cudaStream_t stream) {
+cudaError_t launch_paged_decode(const PagedDecodeParams& p, int dev, int num_sms, cudaStream_t stream) {
   if (p.nseq == 0) return cudaSuccess;
   const EncodeFn encode = encode_fn();
   if (!encode) return cudaErrorNotSupported;
@@ -1185,9 +1228,9 @@ cudaError_t launch_paged_decode(const PagedDecodeParams& p, int num_sms, cudaStr
   }
   const uint32_t sms = static_cast<uint32_t>(num_sms);
   const uint32_t grid = sms < kPagedMaxCtas ? sms : kPagedMaxCtas;
-  if (p.head_dim == 64) return launch_d<64>(p, maps, grid, stream);
-  if (p.head_dim == 128) return launch_d<128>(p, maps, grid, stream);
-  return launch_d<256>(p, maps, grid, stream);
+  if (p.head_dim == 64) return launch_d<64>(p, maps, grid, dev, stream);
+  if (p.head_dim == 128) return launch_d<128>(p, maps, grid, dev, stream);
+  return launch_d<256>(p, maps, grid, dev, stream);
 }
 
 }  // namespace ema

@@ -398,3 +398,78 @@ def test_a_serving_loop_of_all_calls_together():
             assert ok, (step, i, worst)
         lens = new
     assert free.tolist()[0] + free.tolist()[1] + sum(ceil_div(x, T) for x in lens) == 52
+
+
+FIRST_CALLS = """
+import torch
+from paper_2609_27040_b200 import binding as B
+i32, bf = torch.int32, torch.bfloat16
+dev = "cuda"
+gen = torch.Generator(device=dev).manual_seed(1)
+arena = torch.zeros((8, 2, 16, 2, 64), dtype=bf, device=dev)
+cache = B.PagedCache(arena)
+free, free_out, work = torch.tensor([8, 0], dtype=i32, device=dev), torch.zeros(2, dtype=i32, device=dev), torch.zeros(1, dtype=i32, device=dev)
+pool = B.PagedPool(torch.arange(8, dtype=i32, device=dev), None, free, free_out, work)
+lens, new = torch.zeros(2, dtype=i32, device=dev), torch.tensor([40, 3], dtype=i32, device=dev)
+tables, offsets = torch.full((2, 4), -1, dtype=i32, device=dev), torch.zeros(3, dtype=i32, device=dev)
+slots, positions = torch.zeros(50, dtype=torch.int64, device=dev), torch.zeros(50, dtype=i32, device=dev)
+k, v = (torch.randn((50, 2, 64), device=dev, generator=gen).to(bf) for _ in range(2))
+q, q2, lam = torch.randn((2, 4, 64), device=dev, generator=gen).to(bf), torch.randn((2, 8, 32), device=dev, generator=gen).to(bf), torch.full((4,), 0.3, device=dev)
+out, out2 = torch.zeros((2, 4, 64), dtype=bf, device=dev), torch.zeros((2, 4, 64), dtype=bf, device=dev)
+ws = torch.zeros(B.paged_decode_workspace(cache, 8), dtype=torch.uint8, device=dev)
+def step(stream):
+    assert B.paged_build_tables(pool, lens, new, 16, tables, offsets, slots, positions, stream=stream) == B.OK
+    assert B.paged_write_kv(cache, k, v, slots, stream=stream) == B.OK
+    assert B.paged_decode_tables(cache, tables, new, q, 0.125, out, ws, stream=stream) == B.OK
+    assert B.paged_decode_diff(cache, tables, new, q2, lam, 0.2, out2, ws, stream=stream) == B.OK
+torch.cuda.synchronize()
+s, g = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+with torch.cuda.graph(g, stream=s):
+    step(torch.cuda.current_stream())
+torch.cuda.synchronize()
+assert not out.any() and not arena.any()
+g.replay()
+torch.cuda.synchronize()
+got = out.clone(), out2.clone(), slots.clone(), arena.clone()
+assert out.any() and out2.any() and offsets.tolist() == [0, 40, 43]
+for t in (out, out2, slots, arena):
+    t.zero_()
+step(None)
+torch.cuda.synchronize()
+assert all(torch.equal(a, b) for a, b in zip(got, (out, out2, slots, arena)))
+print("the same")
+"""
+
+
+def test_the_very_first_calls_of_a_process_may_be_captured():
+    import subprocess
+    import sys
+    r = subprocess.run([sys.executable, "-c", FIRST_CALLS], capture_output=True, text=True, timeout=300)
+    assert r.returncode == 0 and "the same" in r.stdout, r.stderr[-2000:]
+
+
+def test_two_streams_at_once_with_workspaces_of_their_own():
+    cases = [Case([3000, 10, 700], 8, 4, 128, 16, BF, lent=0.4, seed=k) for k in range(2)]
+    alone = []
+    for c in cases:
+        c.run()
+        alone.append((c.out.clone(), c.lse.clone()))
+    streams = [torch.cuda.Stream() for _ in cases]
+    for _ in range(30):
+        for c, s in zip(cases, streams):
+            assert B.paged_decode_tables(c.cache, c.tables, c.lens_t, c.q, c.scale, c.out[:3], c.work, lse=c.lse[:3], status=c.status, stream=s) == B.OK
+    torch.cuda.synchronize()
+    for c, (o, l) in zip(cases, alone):
+        assert torch.equal(c.out, o) and torch.equal(c.lse, l) and int(c.status) == 0 and not c.work[:16384].any()
+
+
+def test_one_row_tables_and_queries_of_any_stride():
+    """A single sequence: the strides of dimensions of length one mean nothing."""
+    c = Case([77], 1, 1, 64, 16, BF, seed=1)
+    q = torch.empty((1, 1, 64), dtype=BF, device="cuda").as_strided((1, 1, 64), (7, 3, 1))
+    q.copy_(c.q)
+    c.q = q
+    c.tables = c.tables[:1].as_strided((1, c.width), (1, 1))
+    c.tables.copy_(torch.from_numpy(c.table_np).to(torch.int32))
+    c.run()
+    c.check()
