@@ -48,8 +48,9 @@ constexpr uint32_t kNotes = 16;                     // most pieces known to the 
 // Chunks of known pieces that no copy has been started of (an item that one warp takes alone counts as one chunk): 200 sequences
 // of at most 1000 attended tokens, 12 heads of 64: 92 us, with 3 95, with 24 112; 64 of up to 4095 tokens: 99 us with 3 to 24.
 constexpr uint32_t kAhead = 6;
-// Where pieces are many and this small on average, items of at most so many chunks are taken by one warp each, without the
-// merger: 1000 sequences of 10 to 260 tokens 119 us, with 4 (which leaves most of them to all warps) 183.
+// Items of at most two chunks are taken by one warp, which also writes them out (a merge takes longer than a chunk). Where
+// pieces are many and this small on average, items of so many chunks are, too: 1000 sequences of 10 to 260 tokens
+// 119 us, with 4 (which leaves most of them to all warps) 183.
 constexpr uint32_t kSolo = 8;
 constexpr uint32_t kFan = kPagedFan;                // pieces that meet at a time
 constexpr float kMinusInf = -INFINITY;
@@ -117,19 +118,18 @@ __device__ __forceinline__ void tma_box(uint32_t dst, const CUtensorMap* map, ui
       : "memory");
 }
 
-__device__ __forceinline__ void mma_f16_16816(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
-  asm volatile(
-      "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-      : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
-      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
-}
-
+// D(16x8, f32) += A(16x16, row) * B(16x8, col). Not volatile: products that do not depend on one another are to be
+// interleaved by the compiler (all uses are in code that whole warps run through together).
 template <bool kBf16>
 __device__ __forceinline__ void mma(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
   if constexpr (kBf16)
-    ptx::mma_bf16_16816(c, a, b0, b1);
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+        : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+        : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
   else
-    mma_f16_16816(c, a, b0, b1);
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+        : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+        : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 
 template <bool kBf16>
@@ -557,13 +557,20 @@ __device__ __forceinline__ uint32_t pieces_of(const Cut& c, uint32_t head) {
   return head < c.heads[0] ? c.pieces[0] : head < c.heads[1] ? c.pieces[1] : c.pieces[2];
 }
 
+// Tickets drawn at a time when so many pieces are left.
+__device__ __forceinline__ uint32_t batch_of(uint32_t pieces, uint32_t most) {
+  const uint32_t each = pieces / (gridDim.x * 4);
+  return each < 1 ? 1 : each < most ? each : most;
+}
+
 template <uint32_t D, uint32_t NT>
-__device__ void schedule(const PagedDecodeParams& p, Shared<D, NT>& sh, const Zones& zones, uint32_t pieces, uint32_t batch, bool many) {
+__device__ void schedule(const PagedDecodeParams& p, Shared<D, NT>& sh, const Zones& zones, uint32_t pieces, uint32_t batch, uint32_t most, bool many) {
   using S = Shape<D, NT>;
   constexpr uint32_t kTok = kHalf / (2 * D);
   const uint32_t lane = threadIdx.x & 31u;
   const uint32_t run = (p.nseq + S::kThreads - 1) / S::kThreads;
   uint32_t number = 0, turn = 0, tail = 0;    // chunks so far; whose turn it is; the oldest piece not known to be finished
+  const uint32_t first = gridDim.x * batch;   // tickets that are nobody's to draw: every CTA has a batch to begin with
   uint32_t ticket = blockIdx.x * batch, left = batch;
   // where the ticket is: sequence, head, piece of the item, and what was before the item
   uint32_t seq = 0, head = 0, index = 0, count = 0, parts = 0;
@@ -596,9 +603,12 @@ __device__ void schedule(const PagedDecodeParams& p, Shared<D, NT>& sh, const Zo
       ++tail;
     }
     if (left == 0) {
+      // A draw takes longer than a small piece: several at a time, fewer as the end comes nearer.
+      const uint32_t rest = pieces > ticket ? pieces - ticket : 0;
+      batch = batch_of(rest, most);
       uint32_t drawn = 0;
       if (lane == 0) drawn = atomicAdd(p.counters + kPagedTicket, batch);
-      ticket = gridDim.x * batch + __shfl_sync(0xffffffffu, drawn, 0);
+      ticket = first + __shfl_sync(0xffffffffu, drawn, 0);
       left = batch;
       found = false;
     }
@@ -681,7 +691,7 @@ __device__ void schedule(const PagedDecodeParams& p, Shared<D, NT>& sh, const Zo
     }
     const uint32_t a = static_cast<uint32_t>(static_cast<uint64_t>(span.chunks) * index / count);
     const uint32_t b = static_cast<uint32_t>(static_cast<uint64_t>(span.chunks) * (index + 1) / count);
-    const bool solo = many && count == 1 && b <= kSolo;
+    const bool solo = count == 1 && (b <= 2 || (many && b <= kSolo));
     if (lane == 0) {
       note.seq = seq;
       note.head = head;
@@ -1086,9 +1096,11 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) paged_decode_kernel
   // At least two chunks for every warp: a join costs what three take.
   constexpr uint32_t kLeast = 2 * S::kWarps;
   const bool finer = static_cast<unsigned long long>(p.nseq) * p.num_kv_heads >= 2 * gridDim.x;
-  zones.size[0] = max(static_cast<uint32_t>(share / kPagedCut0) + 1, kLeast);
-  zones.size[1] = max(static_cast<uint32_t>(share / (finer ? kPagedCut1 : kPagedCut0)) + 1, kLeast);
-  zones.size[2] = max(static_cast<uint32_t>(share / (finer ? kPagedCut2 : kPagedCut0)) + 1, kLeast);
+  // (If that leaves pieces of the least size, there would be somewhat more of them than CTAs: then one to a CTA.)
+  const uint32_t half = static_cast<uint32_t>(share / kPagedCut0) + 1, coarse = half >= kLeast ? half : max(static_cast<uint32_t>(share) + 1, kLeast);
+  zones.size[0] = coarse;
+  zones.size[1] = finer ? max(static_cast<uint32_t>(share / kPagedCut1) + 1, kLeast) : coarse;
+  zones.size[2] = finer ? max(static_cast<uint32_t>(share / kPagedCut2) + 1, kLeast) : coarse;
   uint2 cut = make_uint2(0, 0);
   {
     unsigned long long at = before;
@@ -1129,13 +1141,15 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) paged_decode_kernel
   sh.chunks_before[tid] = before;
   __syncthreads();
 
-  // Many small pieces are drawn several at a time: a draw takes longer than such a piece.
-  const uint32_t each = pieces / (gridDim.x * 16), batch = each < 1 ? 1 : each < 32 ? each : 32;
+  // Tickets to a draw: as many as two dozen chunks or so are.
+  const uint32_t mean = pieces ? static_cast<uint32_t>(min(total / pieces, 24ull)) : 24, most = 24 / max(mean, 1u), batch = batch_of(pieces, most);
+  // Items that one warp takes alone: only where every warp gets several of them.
+  const bool many = pieces >= 4 * S::kWarps * gridDim.x && total <= static_cast<unsigned long long>(pieces) * kSolo;
   if (static_cast<unsigned long long>(blockIdx.x) * batch < pieces) {
     if (warp < S::kWarps)
       consume<D, NT, kBf16>(p, maps, sh);
     else if (warp == S::kWarps)
-      schedule<D, NT>(p, sh, zones, pieces, batch, pieces >= 8 * gridDim.x && total <= static_cast<unsigned long long>(pieces) * kSolo);
+      schedule<D, NT>(p, sh, zones, pieces, batch, most, many);
     else
       merge<D, NT, kBf16>(p, sh);
   }
