@@ -621,7 +621,7 @@ int paged_write_kv(const paged_write_kv_t* args, void* stream);
 
 /* Bytes of workspace that the two calls below need for num_q_rows query rows per sequence (num_heads, or twice
  * that for the differential form), independent of batch and lengths. Before its first use the
- * workspace's first 16384 bytes must be 0; every call leaves them 0 (one that ended with SLICE_ETIMEOUT may not: clear them again). */
+ * workspace's first 32768 bytes must be 0; every call leaves them 0 (one that ended with SLICE_ETIMEOUT may not: clear them again). */
 int paged_decode_workspace(const paged_cache_t* cache, uint32_t num_q_rows, uint64_t* out_bytes);
 
 /* Attention of one new token per sequence: for query head h (KV head h / G, G = num_heads / num_kv_heads in 1..16)

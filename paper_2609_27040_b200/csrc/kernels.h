@@ -268,10 +268,10 @@ constexpr uint32_t kPagedZone0 = 7, kPagedZone1 = 12, kPagedCut0 = 2, kPagedCut1
 constexpr uint32_t kPagedMaxParts = kPagedMaxCtas * kPagedCut2;
 constexpr uint32_t kPagedFan = 16;              // pieces that are added at a time
 // Words at the start of the workspace, zero before and after: ticket counter, CTAs done, arrivals at every level of the
-// trees in which the pieces of cut items meet (three levels: 16^3 >= kPagedMaxParts).
+// trees in which the pieces of cut items meet (for two groups of columns, three levels: 16^3 >= kPagedMaxParts).
 constexpr uint32_t kPagedTicket = 0, kPagedDone = 1, kPagedTree = 32;
-constexpr uint32_t kPagedCounterBytes = 16384;
-static_assert((kPagedTree + 3 * kPagedMaxParts) * 4 <= kPagedCounterBytes, "counters");
+constexpr uint32_t kPagedCounterBytes = 32768;
+static_assert((kPagedTree + 2 * 3 * kPagedMaxParts) * 4 <= kPagedCounterBytes, "counters");
 static_assert(kPagedFan * kPagedFan * kPagedFan >= kPagedMaxParts, "levels");
 struct PagedDecodeParams {
   uint8_t* base[2];

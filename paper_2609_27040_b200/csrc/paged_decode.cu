@@ -55,18 +55,23 @@ constexpr uint32_t kSolo = 8;
 constexpr uint32_t kFan = kPagedFan;                // pieces that meet at a time
 constexpr float kMinusInf = -INFINITY;
 
-// Partial rows: [NT][D / 16][32 lanes] float4, then the columns' (maximum, sum) pairs.
-template <uint32_t D, uint32_t NT>
+// Partial rows of eight columns: [D / 16][32 lanes] float4, then the columns' (maximum, sum) pairs.
+template <uint32_t D>
 __host__ __device__ constexpr uint32_t part_floats() {
-  return NT * 8 * (D + 2);
+  return 8 * (D + 2);
 }
 
-// Consumer warps: as many as leave room for every consumer's partial rows beside its stages.
+// NT = 2: items of 9 to 16 columns are two groups of eight. Each group has consumer warps and a merger warp of its own; the
+// consumers of both take the same chunks from the same stages, which those of the first group fill. (One warp for both groups
+// needs 2 us a chunk: its matrix instructions follow one another every 33 cycles, whether or not they depend on one another;
+// five such warps to an SM, as many as the registers held, took no more than 40 KB/us together.)
+// Consumer warps of a group: as many as leave room for everybody's partial rows beside the stages, and registers.
 template <uint32_t D, uint32_t NT>
 struct Shape {
-  static constexpr uint32_t kPart = part_floats<D, NT>();
-  static constexpr uint32_t kWarps = kPart * 4 * 6 <= 26000 ? 6 : kPart * 4 * 5 <= 42000 ? 5 : 4;
-  static constexpr uint32_t kThreads = (kWarps + 2) * 32;
+  static constexpr uint32_t kPart = part_floats<D>();
+  static constexpr uint32_t kWarps = NT == 2 ? 4 : kPart * 4 * 6 <= 26000 ? 6 : 5;
+  static constexpr uint32_t kConsumers = kWarps * NT;
+  static constexpr uint32_t kThreads = (kConsumers + 1 + NT) * 32;
 };
 
 struct Maps {
@@ -92,15 +97,18 @@ template <uint32_t D, uint32_t NT>
 struct __align__(128) Shared {
   using S = Shape<D, NT>;
   uint8_t stage[S::kWarps][kDepth][kStageBytes];
-  float part[S::kWarps][S::kPart];
-  float joined[S::kPart];          // sum over parts of the workspace
+  float part[NT][S::kWarps][S::kPart];
+  float joined[NT][S::kPart];      // sum over parts of the workspace
   Note note[kNotes];
   uint64_t full[S::kWarps][kDepth];
+  uint64_t left[S::kWarps][kDepth];  // the second group has read the stage
   uint64_t note_full[kNotes], note_empty[kNotes];
-  uint64_t rows_full, rows_empty;  // the consumers' partial rows of a piece
-  uint64_t job_full, job_done;     // sums over parts that the consumers help with when they have nothing else to do
-  uint32_t job_slot, job_stride, job_count, job_tile;  // count 0: leave; tiles from job_tile on
-  uint32_t idle;
+  uint64_t rows_full[NT], rows_empty[NT];  // the consumers' partial rows of a piece
+  uint64_t job_full[NT], job_done[NT];     // sums over parts that the consumers help with when they have nothing else to do
+  struct Job {
+    uint32_t slot, stride, count, tile;    // count 0: leave; tiles from `tile` on
+  } job[NT];
+  uint32_t idle[NT];
   uint32_t started;                // chunks of the CTA's pieces that copies have been started of
   uint32_t dead;                   // a bounded wait ran out: no further waiting
   uint32_t warp_sum[S::kThreads / 32][2];
@@ -198,169 +206,154 @@ __device__ __forceinline__ bool ready(uint64_t* bar, uint32_t parity) {
 
 __device__ __forceinline__ void arrive(uint64_t* bar) { ptx::mbar_arrive(ptx::smem_u32(bar)); }
 
-// Rows of an item as a warp holds them: column nt * 8 + 2 * (lane % 4) + j, dims mt * 16 + lane / 4 and + 8; the columns'
-// maxima and sums (of all lanes).
-template <uint32_t D, uint32_t NT>
+// Eight columns (query rows) of an item as a warp holds them: column col0 + 2 * (lane % 4) + j, dims mt * 16 + lane / 4
+// and + 8; the columns' maxima and sums (of all lanes).
+template <uint32_t D>
 struct Rows {
-  float o[D / 16][NT][4];
-  float m[NT][2], l[NT][2];
+  float o[D / 16][4];
+  float m[2], l[2];
 };
 
 // Normalised, combined (differential form) and written.
-template <uint32_t D, uint32_t NT, bool kBf16>
-__device__ __forceinline__ void write_out(const PagedDecodeParams& p, Rows<D, NT>& r, uint32_t seq, uint32_t head) {
+template <uint32_t D, bool kBf16>
+__device__ __forceinline__ void write_out(const PagedDecodeParams& p, Rows<D>& r, uint32_t seq, uint32_t head, uint32_t col0) {
   const uint32_t lane = threadIdx.x & 31u, gid = lane >> 2, tig = lane & 3u;
   constexpr uint32_t kSteps = D / 16;
   const uint32_t G = p.lam ? p.rows / 2 : p.rows;
   uint8_t* out = p.out + static_cast<uint64_t>(seq) * p.out_stride + static_cast<uint64_t>(head) * G * D * 2;
   const uint64_t first_head = (static_cast<uint64_t>(seq) * p.num_kv_heads + head) * G;
+  float inv[2];
 #pragma unroll
-  for (uint32_t nt = 0; nt < NT; ++nt) {
-    float inv[2];
+  for (uint32_t j = 0; j < 2; ++j) {
+    const float s = r.l[j];
+    inv[j] = s > 0.f ? 1.f / s : s;  // no weight at all: a row of zeros; not a number stays one
+  }
+  if (!p.lam) {
 #pragma unroll
     for (uint32_t j = 0; j < 2; ++j) {
-      const float s = r.l[nt][j];
-      inv[j] = s > 0.f ? 1.f / s : s;  // no weight at all: a row of zeros; not a number stays one
+      const uint32_t g = col0 + 2 * tig + j;
+      if (p.lse && gid == 0 && g < G) p.lse[first_head + g] = (r.m[j] + log2f(r.l[j])) * 0.6931471805599453f;
     }
-    if (!p.lam) {
+    uint32_t* dst = reinterpret_cast<uint32_t*>(out + static_cast<uint64_t>(col0 + gid) * D * 2) + tig;
 #pragma unroll
-      for (uint32_t j = 0; j < 2; ++j) {
-        const uint32_t g = nt * 8 + 2 * tig + j;
-        if (p.lse && gid == 0 && g < G) p.lse[first_head + g] = (r.m[nt][j] + log2f(r.l[nt][j])) * 0.6931471805599453f;
+    for (uint32_t mt = 0; mt < kSteps; ++mt) {
+      const float(&v)[4] = r.o[mt];
+      // [dim][column] pairs become [column][dim] pairs
+      const uint32_t a = ptx::movmatrix_trans(pack<kBf16>(v[0] * inv[0], v[1] * inv[1]));
+      const uint32_t b = ptx::movmatrix_trans(pack<kBf16>(v[2] * inv[0], v[3] * inv[1]));
+      if (col0 + gid < G) {
+        dst[mt * 8] = a;
+        dst[mt * 8 + 4] = b;
       }
-      uint32_t* dst = reinterpret_cast<uint32_t*>(out + static_cast<uint64_t>(nt * 8 + gid) * D * 2) + tig;
+    }
+  } else {
+    const uint32_t g = col0 / 2 + tig;  // columns 2 tig and 2 tig + 1 are the two maps of this head
+    inv[1] *= g < G ? p.lam[head * G + g] : 0.f;
+    float sq = 0.f;
+#pragma unroll
+    for (uint32_t mt = 0; mt < kSteps; ++mt) {
+      float(&v)[4] = r.o[mt];
+      // two rounded products (not a fused one): equal maps with a weight of 1 leave exactly nothing
+      v[0] = __fsub_rn(__fmul_rn(v[0], inv[0]), __fmul_rn(v[1], inv[1]));
+      v[2] = __fsub_rn(__fmul_rn(v[2], inv[0]), __fmul_rn(v[3], inv[1]));
+      sq = fmaf(v[0], v[0], fmaf(v[2], v[2], sq));
+    }
+    float f = p.out_scale;
+    if (p.norm_weight) {
+#pragma unroll
+      for (int s = 4; s <= 16; s <<= 1) sq += __shfl_xor_sync(0xffffffffu, sq, s);
+      f *= rsqrtf(sq * (1.f / D) + p.eps);
 #pragma unroll
       for (uint32_t mt = 0; mt < kSteps; ++mt) {
-        const float(&v)[4] = r.o[mt][nt];
-        // [dim][column] pairs become [column][dim] pairs
-        const uint32_t a = ptx::movmatrix_trans(pack<kBf16>(v[0] * inv[0], v[1] * inv[1]));
-        const uint32_t b = ptx::movmatrix_trans(pack<kBf16>(v[2] * inv[0], v[3] * inv[1]));
-        if (nt * 8 + gid < G) {
-          dst[mt * 8] = a;
-          dst[mt * 8 + 4] = b;
-        }
+        r.o[mt][0] *= p.norm_weight[mt * 16 + gid];
+        r.o[mt][2] *= p.norm_weight[mt * 16 + 8 + gid];
       }
-    } else {
-      const uint32_t g = nt * 4 + tig;  // columns 2 tig and 2 tig + 1 are the two maps of this head
-      inv[1] *= g < G ? p.lam[head * G + g] : 0.f;
-      float sq = 0.f;
+    }
+    // pairs (dim, dim + 8) of head tig become, in lane 8 h + 4 half + t, dims 8 half + 2 t and + 1 of head h
+    uint32_t* dst = reinterpret_cast<uint32_t*>(out + static_cast<uint64_t>(col0 / 2 + (gid >> 1)) * D * 2) + (gid & 1u) * 4 + tig;
 #pragma unroll
-      for (uint32_t mt = 0; mt < kSteps; ++mt) {
-        float(&v)[4] = r.o[mt][nt];
-        // two rounded products (not a fused one): equal maps with a weight of 1 leave exactly nothing
-        v[0] = __fsub_rn(__fmul_rn(v[0], inv[0]), __fmul_rn(v[1], inv[1]));
-        v[2] = __fsub_rn(__fmul_rn(v[2], inv[0]), __fmul_rn(v[3], inv[1]));
-        sq = fmaf(v[0], v[0], fmaf(v[2], v[2], sq));
-      }
-      float f = p.out_scale;
-      if (p.norm_weight) {
-#pragma unroll
-        for (int s = 4; s <= 16; s <<= 1) sq += __shfl_xor_sync(0xffffffffu, sq, s);
-        f *= rsqrtf(sq * (1.f / D) + p.eps);
-#pragma unroll
-        for (uint32_t mt = 0; mt < kSteps; ++mt) {
-          r.o[mt][nt][0] *= p.norm_weight[mt * 16 + gid];
-          r.o[mt][nt][2] *= p.norm_weight[mt * 16 + 8 + gid];
-        }
-      }
-      // pairs (dim, dim + 8) of head tig become, in lane 8 h + 4 half + t, dims 8 half + 2 t and + 1 of head h
-      uint32_t* dst = reinterpret_cast<uint32_t*>(out + static_cast<uint64_t>(nt * 4 + (gid >> 1)) * D * 2) + (gid & 1u) * 4 + tig;
-#pragma unroll
-      for (uint32_t mt = 0; mt < kSteps; ++mt) {
-        const uint32_t a = ptx::movmatrix_trans(pack<kBf16>(r.o[mt][nt][0] * f, r.o[mt][nt][2] * f));
-        if (nt * 4 + (gid >> 1) < G) dst[mt * 8] = a;
-      }
+    for (uint32_t mt = 0; mt < kSteps; ++mt) {
+      const uint32_t a = ptx::movmatrix_trans(pack<kBf16>(r.o[mt][0] * f, r.o[mt][2] * f));
+      if (col0 / 2 + (gid >> 1) < G) dst[mt * 8] = a;
     }
   }
 }
 
 // Partial rows, as the lanes hold them. Lanes whose columns are padding neither store nor load.
-template <uint32_t D, uint32_t NT>
-__device__ __forceinline__ void store_part(const PagedDecodeParams& p, const Rows<D, NT>& r, float* part) {
+template <uint32_t D>
+__device__ __forceinline__ void store_part(const PagedDecodeParams& p, const Rows<D>& r, uint32_t col0, float* part) {
   const uint32_t lane = threadIdx.x & 31u, tig = lane & 3u;
   constexpr uint32_t kSteps = D / 16;
+  if (col0 + 2 * tig >= p.rows) return;
 #pragma unroll
-  for (uint32_t nt = 0; nt < NT; ++nt) {
-    if (nt * 8 + 2 * tig >= p.rows) continue;
-#pragma unroll
-    for (uint32_t mt = 0; mt < kSteps; ++mt)
-      reinterpret_cast<float4*>(part)[(nt * kSteps + mt) * 32 + lane] = make_float4(r.o[mt][nt][0], r.o[mt][nt][1], r.o[mt][nt][2], r.o[mt][nt][3]);
-    if (lane < 4)
-      reinterpret_cast<float4*>(part + NT * 8 * D)[nt * 4 + tig] = make_float4(r.m[nt][0], r.l[nt][0], r.m[nt][1], r.l[nt][1]);
-  }
+  for (uint32_t mt = 0; mt < kSteps; ++mt)
+    reinterpret_cast<float4*>(part)[mt * 32 + lane] = make_float4(r.o[mt][0], r.o[mt][1], r.o[mt][2], r.o[mt][3]);
+  if (lane < 4)
+    reinterpret_cast<float4*>(part + 8 * D)[tig] = make_float4(r.m[0], r.l[0], r.m[1], r.l[1]);
 }
 
 // r and the partial rows at `part` become the rows of both.
-template <uint32_t D, uint32_t NT>
-__device__ __forceinline__ void add_part(const PagedDecodeParams& p, Rows<D, NT>& r, const float* part) {
+template <uint32_t D>
+__device__ __forceinline__ void add_part(const PagedDecodeParams& p, Rows<D>& r, uint32_t col0, const float* part) {
   const uint32_t lane = threadIdx.x & 31u, tig = lane & 3u;
   constexpr uint32_t kSteps = D / 16;
+  if (col0 + 2 * tig >= p.rows) return;
+  const float4 ml = reinterpret_cast<const float4*>(part + 8 * D)[tig];
+  const float pm[2] = {ml.x, ml.z}, pl[2] = {ml.y, ml.w};
+  float mine[2], theirs[2];
 #pragma unroll
-  for (uint32_t nt = 0; nt < NT; ++nt) {
-    if (nt * 8 + 2 * tig >= p.rows) continue;
-    const float4 ml = reinterpret_cast<const float4*>(part + NT * 8 * D)[nt * 4 + tig];
-    const float pm[2] = {ml.x, ml.z}, pl[2] = {ml.y, ml.w};
-    float mine[2], theirs[2];
+  for (uint32_t j = 0; j < 2; ++j) {
+    const float top = fmaxf(r.m[j], pm[j]), safe = top == kMinusInf ? 0.f : top;
+    mine[j] = ptx::exp2_approx(r.m[j] - safe);
+    theirs[j] = ptx::exp2_approx(pm[j] - safe);
+    r.l[j] = r.l[j] * mine[j] + pl[j] * theirs[j];
+    r.m[j] = top;
+  }
 #pragma unroll
-    for (uint32_t j = 0; j < 2; ++j) {
-      const float top = fmaxf(r.m[nt][j], pm[j]), safe = top == kMinusInf ? 0.f : top;
-      mine[j] = ptx::exp2_approx(r.m[nt][j] - safe);
-      theirs[j] = ptx::exp2_approx(pm[j] - safe);
-      r.l[nt][j] = r.l[nt][j] * mine[j] + pl[j] * theirs[j];
-      r.m[nt][j] = top;
-    }
-#pragma unroll
-    for (uint32_t mt = 0; mt < kSteps; ++mt) {
-      const float4 v = reinterpret_cast<const float4*>(part)[(nt * kSteps + mt) * 32 + lane];
-      float(&o)[4] = r.o[mt][nt];
-      o[0] = o[0] * mine[0] + v.x * theirs[0];
-      o[1] = o[1] * mine[1] + v.y * theirs[1];
-      o[2] = o[2] * mine[0] + v.z * theirs[0];
-      o[3] = o[3] * mine[1] + v.w * theirs[1];
-    }
+  for (uint32_t mt = 0; mt < kSteps; ++mt) {
+    const float4 v = reinterpret_cast<const float4*>(part)[mt * 32 + lane];
+    float(&o)[4] = r.o[mt];
+    o[0] = o[0] * mine[0] + v.x * theirs[0];
+    o[1] = o[1] * mine[1] + v.y * theirs[1];
+    o[2] = o[2] * mine[0] + v.z * theirs[0];
+    o[3] = o[3] * mine[1] + v.w * theirs[1];
   }
 }
 
-template <uint32_t D, uint32_t NT>
-__device__ __forceinline__ void clear(Rows<D, NT>& r) {
+template <uint32_t D>
+__device__ __forceinline__ void clear(Rows<D>& r) {
+  r.m[0] = r.m[1] = kMinusInf;
+  r.l[0] = r.l[1] = 0.f;
 #pragma unroll
-  for (uint32_t nt = 0; nt < NT; ++nt) {
-    r.m[nt][0] = r.m[nt][1] = kMinusInf;
-    r.l[nt][0] = r.l[nt][1] = 0.f;
-#pragma unroll
-    for (uint32_t mt = 0; mt < D / 16; ++mt) r.o[mt][nt][0] = r.o[mt][nt][1] = r.o[mt][nt][2] = r.o[mt][nt][3] = 0.f;
-  }
+  for (uint32_t mt = 0; mt < D / 16; ++mt) r.o[mt][0] = r.o[mt][1] = r.o[mt][2] = r.o[mt][3] = 0.f;
 }
 
 // Query rows as the narrow operand: column n = row of the item, 16 dims per step. A scale below 0 is applied to the
 // signs here, a scale of 0 makes the rows zeros: the softmax sees a scale above 0.
-template <uint32_t D, uint32_t NT>
-__device__ __forceinline__ void load_q(const PagedDecodeParams& p, uint32_t seq, uint32_t head, uint32_t (&qf)[D / 16][NT][2]) {
+template <uint32_t D>
+__device__ __forceinline__ void load_q(const PagedDecodeParams& p, uint32_t seq, uint32_t head, uint32_t col0, uint32_t (&qf)[D / 16][2]) {
   const uint32_t lane = threadIdx.x & 31u, gid = lane >> 2, tig = lane & 3u;
   const bool diff = p.lam != nullptr;
   const uint32_t width = diff ? D / 2 : D;
   const uint8_t* q = p.q + static_cast<uint64_t>(seq) * p.q_stride + static_cast<uint64_t>(head) * p.rows * width * 2;
+  const uint32_t n = col0 + gid;
+  const uint32_t shift = diff && (n & 1u) ? D / 2 : 0;  // where the row's dims start in K
+  const uint8_t* row = q + static_cast<uint64_t>(n) * width * 2;
 #pragma unroll
-  for (uint32_t nt = 0; nt < NT; ++nt) {
-    const uint32_t n = nt * 8 + gid;
-    const uint32_t shift = diff && (n & 1u) ? D / 2 : 0;  // where the row's dims start in K
-    const uint8_t* row = q + static_cast<uint64_t>(n) * width * 2;
+  for (uint32_t ks = 0; ks < D / 16; ++ks)
 #pragma unroll
-    for (uint32_t ks = 0; ks < D / 16; ++ks)
-#pragma unroll
-      for (uint32_t hh = 0; hh < 2; ++hh) {
-        const uint32_t d = ks * 16 + hh * 8 + tig * 2;
-        qf[ks][nt][hh] = n < p.rows && d >= shift && d - shift < width
-                             ? (*reinterpret_cast<const uint32_t*>(row + (d - shift) * 2) & p.q_keep) ^ p.q_flip
-                             : 0u;
-      }
-  }
+    for (uint32_t hh = 0; hh < 2; ++hh) {
+      const uint32_t d = ks * 16 + hh * 8 + tig * 2;
+      qf[ks][hh] = n < p.rows && d >= shift && d - shift < width
+                           ? (*reinterpret_cast<const uint32_t*>(row + (d - shift) * 2) & p.q_keep) ^ p.q_flip
+                           : 0u;
+    }
 }
 
 // One chunk: scores, softmax, product with V. `tok0` = position of its first token. p.scale_log2 is above 0 (load_q).
-template <uint32_t D, uint32_t NT, bool kBf16>
+template <uint32_t D, bool kBf16>
 __device__ __forceinline__ void take_chunk(const PagedDecodeParams& p, uint32_t lo_tok, uint32_t end_tok, uint32_t tok0, const uint8_t* stage,
-                                           const uint32_t (&qf)[D / 16][NT][2], Rows<D, NT>& r) {
+                                           const uint32_t (&qf)[D / 16][2], Rows<D>& r) {
   constexpr uint32_t kTok = kHalf / (2 * D), kSub = kTok / 16, kSteps = D / 16;
   const uint32_t lane = threadIdx.x & 31u, gid = lane >> 2, tig = lane & 3u, mj = lane >> 3, mr = lane & 7u;
   const bool whole = tok0 >= lo_tok && tok0 + kTok <= end_tok;
@@ -371,124 +364,99 @@ __device__ __forceinline__ void take_chunk(const PagedDecodeParams& p, uint32_t 
   const uint32_t vaddr = ptx::smem_u32(stage) + kHalf + ((mj >> 1) * 8 + mr) * (2 * D) + (((mj & 1u) ^ mr) << 4);
 
   // A warp has few products at a time that do not depend on one another: the dims are summed in kChains parts.
-  constexpr uint32_t kChains = kSub * NT >= 4 ? 1 : 4 / (kSub * NT);
-  float s[kSub][NT][4], more[kChains][kSub][NT][4];
+  constexpr uint32_t kChains = kSub >= 4 ? 1 : 4 / kSub;
+  float s[kSub][4], more[kChains][kSub][4];
 #pragma unroll
   for (uint32_t ch = 0; ch < kChains; ++ch)
 #pragma unroll
     for (uint32_t sub = 0; sub < kSub; ++sub)
-#pragma unroll
-      for (uint32_t nt = 0; nt < NT; ++nt) more[ch][sub][nt][0] = more[ch][sub][nt][1] = more[ch][sub][nt][2] = more[ch][sub][nt][3] = 0.f;
+      more[ch][sub][0] = more[ch][sub][1] = more[ch][sub][2] = more[ch][sub][3] = 0.f;
 #pragma unroll
   for (uint32_t ks = 0; ks < kSteps; ++ks)
 #pragma unroll
     for (uint32_t sub = 0; sub < kSub; ++sub) {
       uint32_t f[4];
       ptx::ldmatrix_x4(f, (kaddr ^ ((ks & 3) << 5)) + (ks >> 2) * 128 + sub * 16 * 2 * D);
-#pragma unroll
-      for (uint32_t nt = 0; nt < NT; ++nt) mma<kBf16>(more[ks % kChains][sub][nt], f, qf[ks][nt][0], qf[ks][nt][1]);
+      mma<kBf16>(more[ks % kChains][sub], f, qf[ks][0], qf[ks][1]);
     }
 #pragma unroll
   for (uint32_t sub = 0; sub < kSub; ++sub)
 #pragma unroll
-    for (uint32_t nt = 0; nt < NT; ++nt)
+    for (uint32_t e = 0; e < 4; ++e) {
+      s[sub][e] = more[0][sub][e];
 #pragma unroll
-      for (uint32_t e = 0; e < 4; ++e) {
-        s[sub][nt][e] = more[0][sub][nt][e];
-#pragma unroll
-        for (uint32_t ch = 1; ch < kChains; ++ch) s[sub][nt][e] += more[ch][sub][nt][e];
-      }
+      for (uint32_t ch = 1; ch < kChains; ++ch) s[sub][e] += more[ch][sub][e];
+    }
   if (!whole) {
 #pragma unroll
     for (uint32_t sub = 0; sub < kSub; ++sub) {
       const uint32_t ta = tok0 + sub * 16 + gid, tb = ta + 8;
       const bool in_a = ta >= lo_tok && ta < end_tok, in_b = tb >= lo_tok && tb < end_tok;
-#pragma unroll
-      for (uint32_t nt = 0; nt < NT; ++nt) {
-        float(&x)[4] = s[sub][nt];
-        x[0] = in_a ? x[0] : kMinusInf;
-        x[1] = in_a ? x[1] : kMinusInf;
-        x[2] = in_b ? x[2] : kMinusInf;
-        x[3] = in_b ? x[3] : kMinusInf;
-      }
+      float(&x)[4] = s[sub];
+      x[0] = in_a ? x[0] : kMinusInf;
+      x[1] = in_a ? x[1] : kMinusInf;
+      x[2] = in_b ? x[2] : kMinusInf;
+      x[3] = in_b ? x[3] : kMinusInf;
     }
   }
-  float mx[NT][2];
+  float mx[2];
 #pragma unroll
-  for (uint32_t nt = 0; nt < NT; ++nt)
+  for (uint32_t j = 0; j < 2; ++j) {
+    mx[j] = fmaxf(s[0][j], s[0][2 + j]);
 #pragma unroll
-    for (uint32_t j = 0; j < 2; ++j) {
-      mx[nt][j] = fmaxf(s[0][nt][j], s[0][nt][2 + j]);
-#pragma unroll
-      for (uint32_t sub = 1; sub < kSub; ++sub) mx[nt][j] = fmaxf(mx[nt][j], fmaxf(s[sub][nt][j], s[sub][nt][2 + j]));
-    }
+    for (uint32_t sub = 1; sub < kSub; ++sub) mx[j] = fmaxf(mx[j], fmaxf(s[sub][j], s[sub][2 + j]));
+  }
 #pragma unroll
   for (int x = 4; x <= 16; x <<= 1)
 #pragma unroll
-    for (uint32_t nt = 0; nt < NT; ++nt)
-#pragma unroll
-      for (uint32_t j = 0; j < 2; ++j) mx[nt][j] = fmaxf(mx[nt][j], __shfl_xor_sync(0xffffffffu, mx[nt][j], x));
+    for (uint32_t j = 0; j < 2; ++j) mx[j] = fmaxf(mx[j], __shfl_xor_sync(0xffffffffu, mx[j], x));
   bool moved = false;
 #pragma unroll
-  for (uint32_t nt = 0; nt < NT; ++nt)
+  for (uint32_t j = 0; j < 2; ++j) {
+    mx[j] = fmaxf(r.m[j], mx[j] * p.scale_log2);
+    moved |= mx[j] != r.m[j];
+  }
+  if (__any_sync(0xffffffffu, moved)) {
+    float al[2];
 #pragma unroll
     for (uint32_t j = 0; j < 2; ++j) {
-      mx[nt][j] = fmaxf(r.m[nt][j], mx[nt][j] * p.scale_log2);
-      moved |= mx[nt][j] != r.m[nt][j];
+      al[j] = mx[j] == kMinusInf ? 1.f : ptx::exp2_approx(r.m[j] - mx[j]);
+      r.m[j] = mx[j];
+      r.l[j] *= al[j];
     }
-  if (__any_sync(0xffffffffu, moved)) {
-    float al[NT][2];
 #pragma unroll
-    for (uint32_t nt = 0; nt < NT; ++nt)
-#pragma unroll
-      for (uint32_t j = 0; j < 2; ++j) {
-        al[nt][j] = mx[nt][j] == kMinusInf ? 1.f : ptx::exp2_approx(r.m[nt][j] - mx[nt][j]);
-        r.m[nt][j] = mx[nt][j];
-        r.l[nt][j] *= al[nt][j];
-      }
-#pragma unroll
-    for (uint32_t mt = 0; mt < kSteps; ++mt)
-#pragma unroll
-      for (uint32_t nt = 0; nt < NT; ++nt) {
-        r.o[mt][nt][0] *= al[nt][0];
-        r.o[mt][nt][1] *= al[nt][1];
-        r.o[mt][nt][2] *= al[nt][0];
-        r.o[mt][nt][3] *= al[nt][1];
-      }
+    for (uint32_t mt = 0; mt < kSteps; ++mt) {
+      r.o[mt][0] *= al[0];
+      r.o[mt][1] *= al[1];
+      r.o[mt][2] *= al[0];
+      r.o[mt][3] *= al[1];
+    }
   }
 #pragma unroll
-  for (uint32_t nt = 0; nt < NT; ++nt)
-#pragma unroll
-    for (uint32_t j = 0; j < 2; ++j) mx[nt][j] = mx[nt][j] == kMinusInf ? 0.f : -mx[nt][j];  // no finite score so far: every weight is 0
+  for (uint32_t j = 0; j < 2; ++j) mx[j] = mx[j] == kMinusInf ? 0.f : -mx[j];  // no finite score so far: every weight is 0
 #pragma unroll
   for (uint32_t sub = 0; sub < kSub; ++sub) {
     const uint32_t t16 = tok0 + sub * 16;
     if (!whole && (t16 >= end_tok || t16 + 16 <= lo_tok)) continue;
-    uint32_t hi[NT][2], lo[NT][2];
-#pragma unroll
-    for (uint32_t nt = 0; nt < NT; ++nt) {
-      const float(&x)[4] = s[sub][nt];
-      const float p0 = ptx::exp2_approx(fmaf(x[0], p.scale_log2, mx[nt][0])), p1 = ptx::exp2_approx(fmaf(x[1], p.scale_log2, mx[nt][1]));
-      const float p2 = ptx::exp2_approx(fmaf(x[2], p.scale_log2, mx[nt][0])), p3 = ptx::exp2_approx(fmaf(x[3], p.scale_log2, mx[nt][1]));
-      r.l[nt][0] += p0 + p2;  // this lane's tokens; the lanes' sums are added at the end of the piece
-      r.l[nt][1] += p1 + p3;
-      const uint32_t h01 = pack<kBf16>(p0, p1), h23 = pack<kBf16>(p2, p3);
-      const float2 r01 = unpack<kBf16>(h01), r23 = unpack<kBf16>(h23);
-      hi[nt][0] = ptx::movmatrix_trans(h01);
-      hi[nt][1] = ptx::movmatrix_trans(h23);
-      lo[nt][0] = ptx::movmatrix_trans(pack<kBf16>(p0 - r01.x, p1 - r01.y));
-      lo[nt][1] = ptx::movmatrix_trans(pack<kBf16>(p2 - r23.x, p3 - r23.y));
-    }
+    uint32_t hi[2], lo[2];
+    const float(&x)[4] = s[sub];
+    const float p0 = ptx::exp2_approx(fmaf(x[0], p.scale_log2, mx[0])), p1 = ptx::exp2_approx(fmaf(x[1], p.scale_log2, mx[1]));
+    const float p2 = ptx::exp2_approx(fmaf(x[2], p.scale_log2, mx[0])), p3 = ptx::exp2_approx(fmaf(x[3], p.scale_log2, mx[1]));
+    r.l[0] += p0 + p2;  // this lane's tokens; the lanes' sums are added at the end of the piece
+    r.l[1] += p1 + p3;
+    const uint32_t h01 = pack<kBf16>(p0, p1), h23 = pack<kBf16>(p2, p3);
+    const float2 r01 = unpack<kBf16>(h01), r23 = unpack<kBf16>(h23);
+    hi[0] = ptx::movmatrix_trans(h01);
+    hi[1] = ptx::movmatrix_trans(h23);
+    lo[0] = ptx::movmatrix_trans(pack<kBf16>(p0 - r01.x, p1 - r01.y));
+    lo[1] = ptx::movmatrix_trans(pack<kBf16>(p2 - r23.x, p3 - r23.y));
     if (whole || (t16 >= lo_tok && t16 + 16 <= end_tok)) {
 #pragma unroll
       for (uint32_t mt = 0; mt < kSteps; ++mt) {
         uint32_t f[4];
         ptx::ldmatrix_x4_trans(f, (vaddr ^ ((mt & 3) << 5)) + (mt >> 2) * 128 + sub * 16 * 2 * D);
-#pragma unroll
-        for (uint32_t nt = 0; nt < NT; ++nt) {
-          mma<kBf16>(r.o[mt][nt], f, hi[nt][0], hi[nt][1]);
-          mma<kBf16>(r.o[mt][nt], f, lo[nt][0], lo[nt][1]);
-        }
+        mma<kBf16>(r.o[mt], f, hi[0], hi[1]);
+        mma<kBf16>(r.o[mt], f, lo[0], lo[1]);
       }
     } else {
       // Token pairs (2 tig, 2 tig + 1) and (+8, +9): rows of V outside [lo, end) are taken as zeros, whatever they hold.
@@ -504,11 +472,8 @@ __device__ __forceinline__ void take_chunk(const PagedDecodeParams& p, uint32_t 
         f[1] &= keep_lo;
         f[2] &= keep_hi;
         f[3] &= keep_hi;
-#pragma unroll
-        for (uint32_t nt = 0; nt < NT; ++nt) {
-          mma<kBf16>(r.o[mt][nt], f, hi[nt][0], hi[nt][1]);
-          mma<kBf16>(r.o[mt][nt], f, lo[nt][0], lo[nt][1]);
-        }
+        mma<kBf16>(r.o[mt], f, hi[0], hi[1]);
+        mma<kBf16>(r.o[mt], f, lo[0], lo[1]);
       }
     }
   }
@@ -716,12 +681,12 @@ __device__ void schedule(const PagedDecodeParams& p, Shared<D, NT>& sh, const Zo
 
 // A consumer warp's first chunk of a piece (none if that is not below note.chunks).
 template <uint32_t kWarps>
-__device__ __forceinline__ uint32_t first_chunk(const Note& note) {
-  const uint32_t warp = threadIdx.x >> 5, after = warp >= note.turn ? warp - note.turn : warp + kWarps - note.turn;
+__device__ __forceinline__ uint32_t first_chunk(const Note& note, uint32_t warp) {
+  const uint32_t after = warp >= note.turn ? warp - note.turn : warp + kWarps - note.turn;
   return note.solo && after ? ~0u - 64u : after;
 }
 
-// The copying side of a consumer warp: runs ahead of the work by up to kDepth chunks, into the next pieces as far as they
+// The copying side of a consumer warp (of the first group): runs ahead of the work by up to kDepth chunks, into the next pieces as far as they
 // are known. A chunk is 1, 2 or 4 copies of K and as many of V (blocks of at least its tokens: one); the lanes hold the
 // next 32 copies' blocks. (Every quantity that divides is a power of two and used as a shift: the integer divisions
 // were a fifth of all instructions.)
@@ -755,7 +720,7 @@ struct Feed {
     len = note.len;
     chunk = note.chunk;
     step = note.solo ? 1u : S::kWarps;
-    c = first_chunk<S::kWarps>(note);
+    c = first_chunk<S::kWarps>(note, threadIdx.x >> 5);
     k = 32;
   }
 
@@ -817,67 +782,68 @@ struct Feed {
   }
 };
 
-// Adds the parts of slots `slot`, slot + stride, .. (`count` of them, at most kFan) in that order: of the NT * D / 16 tiles
-// of a row, first, first + step, .. into sh.joined, and the columns' maxima and sums into m and l. `go_on` is asked
-// before each tile; returns the tile it stopped at.
+// A group's part of a slot of the workspace.
+template <uint32_t D, uint32_t NT>
+__device__ __forceinline__ float* part_of(const PagedDecodeParams& p, uint32_t slot, uint32_t group) {
+  return p.parts + (static_cast<uint64_t>(slot) * NT + group) * Shape<D, NT>::kPart;
+}
+
+// Adds the parts of slots `slot`, slot + stride, .. (`count` of them, at most kFan) in that order: of the D / 16 tiles of a
+// row, first, first + step, .. into sh.joined, and the columns' maxima and sums into m and l. `go_on` is asked before the
+// tiles, two at a time; returns the tile it stopped at.
 template <uint32_t D, uint32_t NT, typename GoOn>
-__device__ __forceinline__ uint32_t sum_parts(const PagedDecodeParams& p, Shared<D, NT>& sh, uint32_t slot, uint32_t stride, uint32_t count,
-                                              uint32_t first, uint32_t step, float (&m)[NT][2], float (&l)[NT][2], GoOn go_on) {
+__device__ __forceinline__ uint32_t sum_parts(const PagedDecodeParams& p, Shared<D, NT>& sh, uint32_t group, uint32_t slot, uint32_t stride,
+                                              uint32_t count, uint32_t first, uint32_t step, float (&m)[2], float (&l)[2], GoOn go_on) {
   const uint32_t lane = threadIdx.x & 31u, tig = lane & 3u;
-  constexpr uint32_t kSteps = D / 16, kPart = Shape<D, NT>::kPart;
-  float w[NT][kFan][2];
-#pragma unroll
-  for (uint32_t nt = 0; nt < NT; ++nt) {
-    const bool used = nt * 8 + 2 * tig < p.rows;
+  constexpr uint32_t kSteps = D / 16, kAtOnce = NT == 1 ? 2 : 1;  // tiles, as far as the registers go
+  const bool used = group * 8 + 2 * tig < p.rows;
+  float w[kFan][2];
+  {
     float4 ml[kFan];
 #pragma unroll
     for (uint32_t c = 0; c < kFan; ++c)
-      ml[c] = used && c < count ? __ldcg(reinterpret_cast<const float4*>(p.parts + static_cast<uint64_t>(slot + c * stride) * kPart + NT * 8 * D) + nt * 4 + tig)
+      ml[c] = used && c < count ? __ldcg(reinterpret_cast<const float4*>(part_of<D, NT>(p, slot + c * stride, group) + 8 * D) + tig)
                                 : make_float4(kMinusInf, 0.f, kMinusInf, 0.f);
-    m[nt][0] = m[nt][1] = kMinusInf;
-    l[nt][0] = l[nt][1] = 0.f;
+    m[0] = m[1] = kMinusInf;
+    l[0] = l[1] = 0.f;
 #pragma unroll
     for (uint32_t c = 0; c < kFan; ++c) {
-      m[nt][0] = fmaxf(m[nt][0], ml[c].x);
-      m[nt][1] = fmaxf(m[nt][1], ml[c].z);
+      m[0] = fmaxf(m[0], ml[c].x);
+      m[1] = fmaxf(m[1], ml[c].z);
     }
-    const float s0 = m[nt][0] == kMinusInf ? 0.f : m[nt][0], s1 = m[nt][1] == kMinusInf ? 0.f : m[nt][1];
+    const float s0 = m[0] == kMinusInf ? 0.f : m[0], s1 = m[1] == kMinusInf ? 0.f : m[1];
 #pragma unroll
     for (uint32_t c = 0; c < kFan; ++c) {
-      w[nt][c][0] = ptx::exp2_approx(ml[c].x - s0);
-      w[nt][c][1] = ptx::exp2_approx(ml[c].z - s1);
-      l[nt][0] = fmaf(ml[c].y, w[nt][c][0], l[nt][0]);
-      l[nt][1] = fmaf(ml[c].w, w[nt][c][1], l[nt][1]);
+      w[c][0] = ptx::exp2_approx(ml[c].x - s0);
+      w[c][1] = ptx::exp2_approx(ml[c].z - s1);
+      l[0] = fmaf(ml[c].y, w[c][0], l[0]);
+      l[1] = fmaf(ml[c].w, w[c][1], l[1]);
     }
   }
-  constexpr uint32_t kAtOnce = NT == 1 ? 2 : 1;  // tiles, as far as the registers go
   uint32_t tile = first;
 #pragma unroll 1
-  for (; tile < NT * kSteps && go_on(); tile += step * kAtOnce) {
+  for (; tile < kSteps && go_on(); tile += step * kAtOnce) {
     float4 v[kAtOnce][kFan];
 #pragma unroll
     for (uint32_t i = 0; i < kAtOnce; ++i) {
       const uint32_t x = tile + i * step;
-      const bool used = (x >= kSteps ? 8u : 0u) + 2 * tig < p.rows && x < NT * kSteps;
 #pragma unroll
       for (uint32_t c = 0; c < kFan; ++c)
-        v[i][c] = used && c < count ? __ldcg(reinterpret_cast<const float4*>(p.parts + static_cast<uint64_t>(slot + c * stride) * kPart) + x * 32 + lane)
-                                    : make_float4(0.f, 0.f, 0.f, 0.f);
+        v[i][c] = used && c < count && x < kSteps ? __ldcg(reinterpret_cast<const float4*>(part_of<D, NT>(p, slot + c * stride, group)) + x * 32 + lane)
+                                                  : make_float4(0.f, 0.f, 0.f, 0.f);
     }
 #pragma unroll
     for (uint32_t i = 0; i < kAtOnce; ++i) {
       const uint32_t x = tile + i * step;
-      const bool high = NT == 2 && x >= kSteps;
       float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
       for (uint32_t c = 0; c < kFan; ++c) {
-        const float w0 = high ? w[NT - 1][c][0] : w[0][c][0], w1 = high ? w[NT - 1][c][1] : w[0][c][1];
-        acc.x = fmaf(v[i][c].x, w0, acc.x);
-        acc.y = fmaf(v[i][c].y, w1, acc.y);
-        acc.z = fmaf(v[i][c].z, w0, acc.z);
-        acc.w = fmaf(v[i][c].w, w1, acc.w);
+        acc.x = fmaf(v[i][c].x, w[c][0], acc.x);
+        acc.y = fmaf(v[i][c].y, w[c][1], acc.y);
+        acc.z = fmaf(v[i][c].z, w[c][0], acc.z);
+        acc.w = fmaf(v[i][c].w, w[c][1], acc.w);
       }
-      if (x < NT * kSteps) reinterpret_cast<float4*>(sh.joined)[x * 32 + lane] = acc;
+      if (x < kSteps) reinterpret_cast<float4*>(sh.joined[group])[x * 32 + lane] = acc;
     }
   }
   return tile;
@@ -887,52 +853,72 @@ template <uint32_t D, uint32_t NT, bool kBf16>
 __device__ void consume(const PagedDecodeParams& p, const Maps& maps, Shared<D, NT>& sh) {
   using S = Shape<D, NT>;
   constexpr uint32_t kTok = kHalf / (2 * D), kSteps = D / 16;
-  const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31u;
+  const uint32_t lane = threadIdx.x & 31u, group = NT == 1 ? 0 : (threadIdx.x >> 5) / S::kWarps, warp = (threadIdx.x >> 5) - group * S::kWarps;
+  const uint32_t col0 = group * 8;
   const uint64_t policy = ptx::policy_evict_first();
   uint32_t merges = 0;              // pieces so far whose rows went to the merger
   uint32_t issued = 0, taken = 0;   // chunks of this warp
   bool alive = true;
   Feed<D, NT> feed;
   feed.init(p);
-  Rows<D, NT> r;
+  Rows<D> r;
+  // Copies on, as far as stages are free and chunks known. Of two groups both have to have read a stage: if the other one
+  // has not yet, its turn comes after the next chunk, unless there is none.
+  auto copy = [&] {
+    while (alive && issued - taken < kDepth) {
+      const uint32_t stage = issued % kDepth;
+      if (NT == 2 && issued >= kDepth) {
+        uint64_t* bar = &sh.left[warp][stage];
+        const uint32_t parity = (issued / kDepth - 1) & 1u;
+        if (!__all_sync(0xffffffffu, ready(bar, parity))) {
+          if (issued != taken) return;
+          alive = __all_sync(0xffffffffu, wait_for(bar, parity, sh, p.status));
+          if (!alive) return;
+        }
+      }
+      if (!feed.issue(p, maps, sh, stage, policy)) return;
+      ++issued;
+    }
+  };
   for (uint32_t j = 0; alive; ++j) {
     alive = __all_sync(0xffffffffu, wait_for(&sh.note_full[j % kNotes], j / kNotes & 1u, sh, p.status));
     if (!alive) break;
     const Note note = sh.note[j % kNotes];
     if (note.chunks == 0) break;
-    if (j == 0 || feed.j < j) feed.open(note, j);  // nothing of the pieces before is left to copy
-    const uint32_t c0 = first_chunk<S::kWarps>(note), step = note.solo ? 1u : S::kWarps;
+    if (group == 0 && (j == 0 || feed.j < j)) feed.open(note, j);  // nothing of the pieces before is left to copy
+    const uint32_t c0 = first_chunk<S::kWarps>(note, warp), step = note.solo ? 1u : S::kWarps;
     if (c0 < note.chunks) {
-      feed.prepare(p);
-      uint32_t qf[kSteps][NT][2];
-      load_q<D, NT>(p, note.seq, note.head, qf);
-      while (issued - taken < kDepth && feed.issue(p, maps, sh, issued % kDepth, policy)) ++issued;
+      if (group == 0) feed.prepare(p);
+      uint32_t qf[kSteps][2];
+      load_q<D>(p, note.seq, note.head, col0, qf);
+      if (group == 0) copy();
       clear(r);
-      for (uint32_t c = c0; c < note.chunks; c += step) {
+      for (uint32_t c = c0; c < note.chunks && alive; c += step) {
         const uint32_t stage = taken % kDepth;
         alive = __all_sync(0xffffffffu, wait_on(&sh.full[warp][stage], (taken / kDepth) & 1u, sh, p.status));
         if (!alive) break;
-        take_chunk<D, NT, kBf16>(p, note.lo, note.len, (note.chunk + c) * kTok, sh.stage[warp][stage], qf, r);
+        take_chunk<D, kBf16>(p, note.lo, note.len, (note.chunk + c) * kTok, sh.stage[warp][stage], qf, r);
         __syncwarp();  // every lane has read the stage
         ++taken;
-        while (issued - taken < kDepth && feed.issue(p, maps, sh, issued % kDepth, policy)) ++issued;
+        if (group == 0)
+          copy();
+        else if (lane == 0)
+          arrive(&sh.left[warp][stage]);
       }
       if (!alive) break;
 #pragma unroll
-      for (uint32_t nt = 0; nt < NT; ++nt)
+      for (uint32_t i = 0; i < 2; ++i)
 #pragma unroll
-        for (uint32_t i = 0; i < 2; ++i)
-#pragma unroll
-          for (int x = 4; x <= 16; x <<= 1) r.l[nt][i] += __shfl_xor_sync(0xffffffffu, r.l[nt][i], x);
+        for (int x = 4; x <= 16; x <<= 1) r.l[i] += __shfl_xor_sync(0xffffffffu, r.l[i], x);
     }
     if (note.solo || (note.chunks == 1 && note.count == 1)) {
-      if (c0 == 0) write_out<D, NT, kBf16>(p, r, note.seq, note.head);  // nobody else has rows of it
+      if (c0 == 0) write_out<D, kBf16>(p, r, note.seq, note.head, col0);  // nobody else has rows of it
     } else {
-      alive = __all_sync(0xffffffffu, wait_for(&sh.rows_empty, (merges & 1u) ^ 1u, sh, p.status));
+      alive = __all_sync(0xffffffffu, wait_for(&sh.rows_empty[group], (merges & 1u) ^ 1u, sh, p.status));
       if (!alive) break;
-      if (c0 < note.chunks) store_part<D, NT>(p, r, sh.part[warp]);
+      if (c0 < note.chunks) store_part<D>(p, r, col0, sh.part[group][warp]);
       __syncwarp();
-      if (lane == 0) arrive(&sh.rows_full);
+      if (lane == 0) arrive(&sh.rows_full[group]);
       ++merges;
     }
     __syncwarp();
@@ -945,24 +931,25 @@ __device__ void consume(const PagedDecodeParams& p, const Maps& maps, Shared<D, 
     return;
   }
   // Nothing left to stream: sums over parts go faster with all warps.
-  if (!__all_sync(0xffffffffu, wait_for(&sh.rows_empty, (merges & 1u) ^ 1u, sh, p.status))) return;
-  if (lane == 0) atomicAdd(&sh.idle, 1u);
+  if (!__all_sync(0xffffffffu, wait_for(&sh.rows_empty[group], (merges & 1u) ^ 1u, sh, p.status))) return;
+  if (lane == 0) atomicAdd(&sh.idle[group], 1u);
   for (uint32_t k = 0;; ++k) {
-    if (!__all_sync(0xffffffffu, wait_for(&sh.job_full, k & 1u, sh, p.status))) return;
-    if (sh.job_count == 0) return;
-    sum_parts<D, NT>(p, sh, sh.job_slot, sh.job_stride, sh.job_count, sh.job_tile + warp, S::kWarps, r.m, r.l, [] { return true; });
+    if (!__all_sync(0xffffffffu, wait_for(&sh.job_full[group], k & 1u, sh, p.status))) return;
+    const auto& job = sh.job[group];
+    if (job.count == 0) return;
+    sum_parts<D, NT>(p, sh, group, job.slot, job.stride, job.count, job.tile + warp, S::kWarps, r.m, r.l, [] { return true; });
     __syncwarp();
-    if (lane == 0) arrive(&sh.job_done);
+    if (lane == 0) arrive(&sh.job_done[group]);
   }
 }
 
 template <uint32_t D, uint32_t NT, bool kBf16>
-__device__ void merge(const PagedDecodeParams& p, Shared<D, NT>& sh) {
+__device__ void merge(const PagedDecodeParams& p, Shared<D, NT>& sh, uint32_t group) {
   using S = Shape<D, NT>;
-  constexpr uint32_t kSteps = D / 16, kPart = S::kPart;
-  const uint32_t lane = threadIdx.x & 31u;
+  constexpr uint32_t kSteps = D / 16;
+  const uint32_t lane = threadIdx.x & 31u, col0 = group * 8;
   uint32_t merges = 0, jobs = 0;
-  Rows<D, NT> r;
+  Rows<D> r;
   for (uint32_t j = 0;; ++j) {
     if (!__all_sync(0xffffffffu, wait_for(&sh.note_full[j % kNotes], j / kNotes & 1u, sh, p.status))) return;
     const Note note = sh.note[j % kNotes];
@@ -970,13 +957,13 @@ __device__ void merge(const PagedDecodeParams& p, Shared<D, NT>& sh) {
     __syncwarp();
     if (lane == 0) arrive(&sh.note_empty[j % kNotes]);  // read: the copy is what counts from here on
     if (note.solo || (note.chunks == 1 && note.count == 1)) continue;
-    if (!__all_sync(0xffffffffu, wait_for(&sh.rows_full, merges & 1u, sh, p.status))) return;
+    if (!__all_sync(0xffffffffu, wait_for(&sh.rows_full[group], merges & 1u, sh, p.status))) return;
     ++merges;
     clear(r);
     const uint32_t parts = min(note.chunks, S::kWarps);
-    for (uint32_t x = 0; x < parts; ++x) add_part<D, NT>(p, r, sh.part[(note.turn + x) % S::kWarps]);
+    for (uint32_t x = 0; x < parts; ++x) add_part<D>(p, r, col0, sh.part[group][(note.turn + x) % S::kWarps]);
     __syncwarp();
-    if (lane == 0) arrive(&sh.rows_empty);
+    if (lane == 0) arrive(&sh.rows_empty[group]);
 
     // Up the tree: store the rows, and where they are their group's last ones, take the group's sum on.
     uint32_t index = note.index, count = note.count, stride = 1;
@@ -984,10 +971,10 @@ __device__ void merge(const PagedDecodeParams& p, Shared<D, NT>& sh) {
     for (uint32_t level = 0; count > 1; ++level) {
       const uint32_t g = index / kFan, n = min(kFan, count - g * kFan);
       const uint32_t first = note.slot + g * kFan * stride;
-      store_part<D, NT>(p, r, p.parts + static_cast<uint64_t>(note.slot + index * stride) * kPart);
+      store_part<D>(p, r, col0, part_of<D, NT>(p, note.slot + index * stride, group));
       __threadfence();
       __syncwarp();
-      uint32_t* counter = p.counters + kPagedTree + level * kPagedMaxParts + first;
+      uint32_t* counter = p.counters + kPagedTree + (group * 3 + level) * kPagedMaxParts + first;
       uint32_t arrived = 0;
       if (lane == 0) {
         arrived = atomicAdd(counter, 1u);
@@ -1001,45 +988,40 @@ __device__ void merge(const PagedDecodeParams& p, Shared<D, NT>& sh) {
       __threadfence();
       if (n <= 4) {
         clear(r);
-        for (uint32_t c = 0; c < n; ++c) add_part<D, NT>(p, r, p.parts + static_cast<uint64_t>(first + c * stride) * kPart);
+        for (uint32_t c = 0; c < n; ++c) add_part<D>(p, r, col0, part_of<D, NT>(p, first + c * stride, group));
       } else {
-        // One warp has one tile of all parts in flight, 8 KB; as soon as the consumers have nothing else to do they take
+        // One warp has 8 or 16 KB of the parts in flight; as soon as the consumers have nothing else to do they take
         // the tiles that are left.
-        const uint32_t tile = sum_parts<D, NT>(p, sh, first, stride, n, 0, 1, r.m, r.l, [&] {
-          return __shfl_sync(0xffffffffu, *reinterpret_cast<volatile uint32_t*>(&sh.idle), 0) != S::kWarps;
+        const uint32_t tile = sum_parts<D, NT>(p, sh, group, first, stride, n, 0, 1, r.m, r.l, [&] {
+          return __shfl_sync(0xffffffffu, *reinterpret_cast<volatile uint32_t*>(&sh.idle[group]), 0) != S::kWarps;
         });
-        if (tile < NT * kSteps) {
+        if (tile < kSteps) {
           if (lane == 0) {
-            sh.job_slot = first;
-            sh.job_stride = stride;
-            sh.job_count = n;
-            sh.job_tile = tile;
-            arrive(&sh.job_full);
+            sh.job[group] = {first, stride, n, tile};
+            arrive(&sh.job_full[group]);
           }
-          if (!__all_sync(0xffffffffu, wait_for(&sh.job_done, jobs & 1u, sh, p.status))) return;
+          if (!__all_sync(0xffffffffu, wait_for(&sh.job_done[group], jobs & 1u, sh, p.status))) return;
           ++jobs;
         }
 #pragma unroll
-        for (uint32_t nt = 0; nt < NT; ++nt)
-#pragma unroll
-          for (uint32_t mt = 0; mt < kSteps; ++mt) {
-            const float4 v = reinterpret_cast<const float4*>(sh.joined)[(nt * kSteps + mt) * 32 + lane];
-            r.o[mt][nt][0] = v.x;
-            r.o[mt][nt][1] = v.y;
-            r.o[mt][nt][2] = v.z;
-            r.o[mt][nt][3] = v.w;
-          }
+        for (uint32_t mt = 0; mt < kSteps; ++mt) {
+          const float4 v = reinterpret_cast<const float4*>(sh.joined[group])[mt * 32 + lane];
+          r.o[mt][0] = v.x;
+          r.o[mt][1] = v.y;
+          r.o[mt][2] = v.z;
+          r.o[mt][3] = v.w;
+        }
       }
       __syncwarp();
       index = g;
       count = (count + kFan - 1) / kFan;
       stride *= kFan;
     }
-    if (mine) write_out<D, NT, kBf16>(p, r, note.seq, note.head);
+    if (mine) write_out<D, kBf16>(p, r, note.seq, note.head, col0);
   }
   if (lane == 0) {
-    sh.job_count = 0;
-    arrive(&sh.job_full);
+    sh.job[group].count = 0;
+    arrive(&sh.job_full[group]);
   }
 }
 
@@ -1052,19 +1034,25 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) paged_decode_kernel
   const uint32_t tid = threadIdx.x, warp = tid >> 5, lane = tid & 31u;
   if (tid == 0) {
     for (uint32_t x = 0; x < S::kWarps; ++x)
-      for (uint32_t s = 0; s < kDepth; ++s) ptx::mbar_init(ptx::smem_u32(&sh.full[x][s]), 1);
+      for (uint32_t s = 0; s < kDepth; ++s) {
+        ptx::mbar_init(ptx::smem_u32(&sh.full[x][s]), 1);
+        ptx::mbar_init(ptx::smem_u32(&sh.left[x][s]), 1);
+      }
     for (uint32_t s = 0; s < kNotes; ++s) {
       ptx::mbar_init(ptx::smem_u32(&sh.note_full[s]), 1);
-      ptx::mbar_init(ptx::smem_u32(&sh.note_empty[s]), S::kWarps + 1);
+      ptx::mbar_init(ptx::smem_u32(&sh.note_empty[s]), S::kConsumers + NT);
     }
-    ptx::mbar_init(ptx::smem_u32(&sh.rows_full), S::kWarps);
-    ptx::mbar_init(ptx::smem_u32(&sh.rows_empty), 1);
-    ptx::mbar_init(ptx::smem_u32(&sh.job_full), 1);
-    ptx::mbar_init(ptx::smem_u32(&sh.job_done), S::kWarps);
+    for (uint32_t g = 0; g < NT; ++g) {
+      ptx::mbar_init(ptx::smem_u32(&sh.rows_full[g]), S::kWarps);
+      ptx::mbar_init(ptx::smem_u32(&sh.rows_empty[g]), 1);
+      ptx::mbar_init(ptx::smem_u32(&sh.job_full[g]), 1);
+      ptx::mbar_init(ptx::smem_u32(&sh.job_done[g]), S::kWarps);
+      sh.idle[g] = 0;
+    }
     ptx::fence_barrier_init();
     asm volatile("prefetch.tensormap [%0];" ::"l"(&maps.m[0]));
     asm volatile("prefetch.tensormap [%0];" ::"l"(&maps.m[1]));
-    sh.dead = sh.idle = sh.started = 0;
+    sh.dead = sh.started = 0;
   }
 
   // How the work is cut: chunks before each thread's run of sequences, then pieces, and pieces of cut items.
@@ -1146,12 +1134,12 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) paged_decode_kernel
   // Items that one warp takes alone: only where every warp gets several of them.
   const bool many = pieces >= 4 * S::kWarps * gridDim.x && total <= static_cast<unsigned long long>(pieces) * kSolo;
   if (static_cast<unsigned long long>(blockIdx.x) * batch < pieces) {
-    if (warp < S::kWarps)
+    if (warp < S::kConsumers)
       consume<D, NT, kBf16>(p, maps, sh);
-    else if (warp == S::kWarps)
+    else if (warp == S::kConsumers)
       schedule<D, NT>(p, sh, zones, pieces, batch, most, many);
     else
-      merge<D, NT, kBf16>(p, sh);
+      merge<D, NT, kBf16>(p, sh, warp - S::kConsumers - 1);
   }
 
   // Sequences without tokens: zeros, and minus infinity for the log-sum-exp.

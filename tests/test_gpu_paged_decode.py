@@ -77,7 +77,7 @@ class Case:
         assert rc == B.OK
         torch.cuda.synchronize()
         assert int(self.status) == 0
-        assert not self.work[:16384].any()
+        assert not self.work[:32768].any()
 
     def check(self):
         eps = torch.finfo(self.dtype).eps
@@ -262,7 +262,7 @@ def test_a_captured_call_follows_tables_and_lengths():
         torch.cuda.synchronize()
         c.lens = lens
         c.check()
-        assert int(c.status) == 0 and not c.work[:16384].any()
+        assert int(c.status) == 0 and not c.work[:32768].any()
 
 
 def test_blocks_apart_and_offsets_beyond_32_bits():
@@ -460,7 +460,7 @@ def test_two_streams_at_once_with_workspaces_of_their_own():
             assert B.paged_decode_tables(c.cache, c.tables, c.lens_t, c.q, c.scale, c.out[:3], c.work, lse=c.lse[:3], status=c.status, stream=s) == B.OK
     torch.cuda.synchronize()
     for c, (o, l) in zip(cases, alone):
-        assert torch.equal(c.out, o) and torch.equal(c.lse, l) and int(c.status) == 0 and not c.work[:16384].any()
+        assert torch.equal(c.out, o) and torch.equal(c.lse, l) and int(c.status) == 0 and not c.work[:32768].any()
 
 
 def test_one_row_tables_and_queries_of_any_stride():

@@ -115,7 +115,7 @@ def test_bad_differential_arguments_are_refused():
 
 def test_workspace_too_small():
     need = C.c_uint64(0)
-    assert B.lib().paged_decode_workspace(C.byref(desc()), 32, C.byref(need)) == B.OK and need.value > 16384
+    assert B.lib().paged_decode_workspace(C.byref(desc()), 32, C.byref(need)) == B.OK and need.value > 32768
     assert decode(desc(), work_bytes=need.value - 1) == B.ESCRATCH
     more = C.c_uint64(0)
     assert B.lib().paged_decode_workspace(C.byref(desc()), 128, C.byref(more)) == B.OK and more.value > need.value
