@@ -644,7 +644,8 @@ int paged_decode_tables(const paged_decode_t* args, void* stream);
  *   out[i][h] = out_scale * x, or out_scale * x / sqrt(mean(x^2) + eps) * norm_weight when that is given.
  *   q        [nseq] rows of [2 * num_heads][d]; out [nseq] rows of [num_heads][D]
  *   lam      [num_heads] f32, norm_weight [D] f32 (device)
- * Everything else as in paged_decode_tables (zeros for an empty sequence). */
+ * Everything else as in paged_decode_tables (zeros for an empty sequence), but the rows of K that are attended to must be
+ * finite, too: an infinity in one map's half of a K row makes the other map's score not a number. */
 int paged_decode_diff(const paged_decode_t* args, void* stream);
 
 const char* slice_strerror(int code);

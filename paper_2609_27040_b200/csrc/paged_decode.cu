@@ -62,9 +62,10 @@ __host__ __device__ constexpr uint32_t part_floats() {
 }
 
 // NT = 2: items of 9 to 16 columns are two groups of eight. Each group has consumer warps and a merger warp of its own; the
-// consumers of both take the same chunks from the same stages, which those of the first group fill. (One warp for both groups
-// needs 2 us a chunk: its matrix instructions follow one another every 33 cycles, whether or not they depend on one another;
-// five such warps to an SM, as many as the registers held, took no more than 40 KB/us together.)
+// consumers of both take the same chunks from the same stages, which those of the first group fill. (A warp for all sixteen
+// columns took 2 us a chunk, 770 instructions at 6 cycles each, hardly anything else running on its scheduler, and registers and
+// partial rows left room for five of them: 40 sequences of up to 2000 tokens, 16 query heads to a KV head of 256, 141 us
+// against 119, differential with 8 heads 113 against 98. Two chunks at a time in one warp gained nothing.)
 // Consumer warps of a group: as many as leave room for everybody's partial rows beside the stages, and registers.
 template <uint32_t D, uint32_t NT>
 struct Shape {
