@@ -218,6 +218,24 @@ struct AppendParams {
 };
 cudaError_t launch_append(const AppendParams& p, cudaStream_t stream);
 
+// Launch of a kernel of the device-driven path: it may start while the kernel before it in the stream still runs. Its
+// threads wait for that one's end (ptx::grid_dependency_wait) before they touch global memory, and let the next one start
+// as soon as all CTAs have (ptx::launch_dependents), so that of a step's launches only the first one's latency shows.
+template <typename... Params, typename... Args>
+cudaError_t launch_early(void (*kernel)(Params...), unsigned grid, unsigned threads, size_t shared, cudaStream_t stream, const Args&... args) {
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = dim3(grid);
+  cfg.blockDim = dim3(threads);
+  cfg.dynamicSmemBytes = shared;
+  cfg.stream = stream;
+  cudaLaunchAttribute attr{};
+  attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr.val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = &attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, kernel, args...);
+}
+
 // paged_tables.cu: block tables and slot maps from request lengths (see paged_build_tables).
 struct BuildTablesParams {
   int32_t* ids[2];             // free stacks, top at the end

@@ -1055,6 +1055,8 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) paged_decode_kernel
     asm volatile("prefetch.tensormap [%0];" ::"l"(&maps.m[1]));
     sh.dead = sh.started = 0;
   }
+  ptx::launch_dependents();
+  ptx::grid_dependency_wait();
 
   // How the work is cut: chunks before each thread's run of sequences, then pieces, and pieces of cut items.
   const uint32_t run = (p.nseq + S::kThreads - 1) / S::kThreads;
@@ -1188,8 +1190,7 @@ cudaError_t launch(const PagedDecodeParams& p, const Maps& maps, uint32_t grid, 
     if (e != cudaSuccess) return e;
     ready[dev] = true;
   }
-  paged_decode_kernel<D, NT, kBf16><<<grid, Shape<D, NT>::kThreads, kSharedBytes, stream>>>(p, maps);
-  return cudaGetLastError();
+  return launch_early(paged_decode_kernel<D, NT, kBf16>, grid, Shape<D, NT>::kThreads, kSharedBytes, stream, p, maps);
 }
 
 template <uint32_t D>

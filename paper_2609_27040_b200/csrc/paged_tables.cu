@@ -162,6 +162,9 @@ __global__ void __launch_bounds__(kBuildThreads, 1) build_tables_kernel(const Bu
   const uint32_t tid = threadIdx.x, lane = tid & 31u, warp = tid >> 5;
   const uint32_t shift = p.block_shift;
 
+  ptx::launch_dependents();
+  ptx::grid_dependency_wait();
+
   // Every thread owns a run of requests.
   const uint32_t run = (p.nseq + kBuildThreads - 1) / kBuildThreads;
   const uint32_t r0 = min(tid * run, p.nseq), r1 = min(r0 + run, p.nseq);
@@ -346,6 +349,8 @@ constexpr uint32_t kWriteThreads = 256;
 
 template <uint32_t kRows, uint32_t kUnits>
 __global__ void __launch_bounds__(kWriteThreads) write_kv_kernel(const WriteKvParams p) {
+  ptx::launch_dependents();
+  ptx::grid_dependency_wait();
   const uint32_t lanes = 1u << p.lane_shift;
   const uint32_t sub = threadIdx.x & (lanes - 1);
   const uint32_t groups = kWriteThreads >> p.lane_shift, group = threadIdx.x >> p.lane_shift;
@@ -409,8 +414,7 @@ cudaError_t launch_build_tables(const BuildTablesParams& p, int num_sms, cudaStr
   const uint64_t steps = (static_cast<uint64_t>(p.max_tokens) + kBuildTokens - 1) / kBuildTokens;
   const uint64_t most = static_cast<uint64_t>(num_sms);
   const unsigned grid = static_cast<unsigned>(steps < 1 ? 1 : steps < most ? steps : most);
-  build_tables_kernel<<<grid, kBuildThreads, 0, stream>>>(p);
-  return cudaGetLastError();
+  return launch_early(build_tables_kernel, grid, kBuildThreads, 0, stream, p);
 }
 
 cudaError_t launch_write_kv(WriteKvParams p, cudaStream_t stream) {
@@ -420,11 +424,7 @@ cudaError_t launch_write_kv(WriteKvParams p, cudaStream_t stream) {
   const bool wide = p.units >= 3u << p.lane_shift;  // most of four units to a thread
   const uint32_t per_cta = (kWriteThreads >> p.lane_shift) * (wide ? 1 : 4);
   const unsigned grid = static_cast<unsigned>((static_cast<uint64_t>(p.ntok) + per_cta - 1) / per_cta);
-  if (wide)
-    write_kv_kernel<1, 4><<<grid, kWriteThreads, 0, stream>>>(p);
-  else
-    write_kv_kernel<4, 1><<<grid, kWriteThreads, 0, stream>>>(p);
-  return cudaGetLastError();
+  return wide ? launch_early(write_kv_kernel<1, 4>, grid, kWriteThreads, 0, stream, p) : launch_early(write_kv_kernel<4, 1>, grid, kWriteThreads, 0, stream, p);
 }
 
 }  // namespace ema
