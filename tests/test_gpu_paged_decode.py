@@ -473,3 +473,135 @@ def test_one_row_tables_and_queries_of_any_stride():
     c.tables.copy_(torch.from_numpy(c.table_np).to(torch.int32))
     c.run()
     c.check()
+
+
+@pytest.mark.parametrize("dtype", [BF, HF], ids=["bf16", "fp16"])
+@pytest.mark.parametrize("n", [700, 100001])
+def test_many_tiny_weights_beside_a_large_one(n, dtype):
+    """One token of score 17.53 (bf16: 17.5) and value 0, the others of score 0 (a weight of 2^-25.3 beside it) and value 1. All terms are positive: f32
+    sums of n of them are off by n 2^-23 of their size at most (numerator and denominator), a weight by 2^-16 (bf16's two numbers; and
+    2^-20 for the score), and the result is rounded once; what fp16 loses below 2^-40 of the largest weight is 2^-14 of the others'."""
+    T, D = 64, 64
+    local = torch.zeros((ceil_div(n, T), 2, T, 1, D), dtype=dtype, device="cuda")
+    local[:, 1] = 1.0
+    local[0, 1, 0] = 0.0
+    x = 17.53125 if dtype is HF else 17.5                        # as the type has it
+    local[0, 0, 0, 0, 0] = x
+    q = torch.zeros((1, 1, D), dtype=dtype, device="cuda")
+    q[..., 0] = 1.0
+    cache, tables = B.PagedCache(local), torch.arange(local.shape[0], dtype=torch.int32, device="cuda")[None]
+    work = torch.zeros(B.paged_decode_workspace(cache, 1), dtype=torch.uint8, device="cuda")
+    out, lse = torch.empty_like(q), torch.empty((1, 1), device="cuda")
+    torch.cuda.synchronize()
+    assert B.paged_decode_tables(cache, tables, gpu([n]), q, 1.0, out, work, lse=lse) == B.OK
+    w = (n - 1) * math.exp(-x)
+    ref = w / (1 + w)
+    rel = 2 * n * 2.0 ** -23 + 2.0 ** -14 + 2.0 ** -15 + torch.finfo(dtype).eps / 2
+    # fp16 below 2^-14 are multiples of 2^-24: there (n = 700, 1.7e-5) the rounding is off by up to 2^-25, whatever the value
+    least = 2.0 ** -25 if dtype is HF else 0.0
+    assert float((out.double() - ref).abs().max()) <= rel * ref + least, (float(out[0, 0, 0]), ref)
+    assert abs(float(lse) - (x + math.log1p(w))) <= lse_slack(n, D, x)
+
+
+@pytest.mark.parametrize("dtype", [BF, HF], ids=["bf16", "fp16"])
+@pytest.mark.parametrize("D,T", [(64, 16), (128, 16), (256, 64)])
+@pytest.mark.parametrize("n", [1, 100, 3000])
+def test_scores_beyond_what_f32_counts_in_ones(n, D, T, dtype):
+    """Scores around 2^38, apart by 2^30 and more: the largest has all the weight, exactly."""
+    rng = np.random.default_rng(n + D)
+    top = 2.0 ** 16 if dtype is BF else 2.0 ** 14
+    steps = rng.integers(1, 120, n)                              # of 128: both types have them
+    best, least = rng.permutation(n)[:2] if n > 1 else (0, 0)
+    steps[least], steps[best] = 0, 127
+    nb = ceil_div(n, T)
+    rows = torch.zeros(nb * T, dtype=torch.float64)
+    rows[:n] = torch.from_numpy(top * (1 + steps / 128))
+    local = torch.randn((nb, 2, T, 1, D), device="cuda").to(dtype)
+    local[:, 0] = rows.to("cuda").to(dtype).reshape(nb, T, 1, 1)
+    cache, tables = B.PagedCache(local), torch.arange(nb, dtype=torch.int32, device="cuda")[None]
+    v = logical_rows(local, None, np.arange(nb), n, T)[1]
+    q = torch.full((1, 2, D), top, dtype=dtype, device="cuda")
+    q[:, 1] = -top
+    work = torch.zeros(B.paged_decode_workspace(cache, 2), dtype=torch.uint8, device="cuda")
+    out, lse = torch.empty_like(q), torch.empty((1, 2), device="cuda")
+    if n == 1:
+        least = best
+    torch.cuda.synchronize()
+    for scale, heads in ((1.0, (best, least)), (-1.0, (least, best))):
+        assert B.paged_decode_tables(cache, tables, gpu([n]), q, scale, out, work, lse=lse) == B.OK
+        for h, t in enumerate(heads):
+            assert torch.equal(out[0, h].double(), v[t, 0])
+            score = (1 - 2 * h) * scale * D * top * float(rows[t])
+            assert abs(float(lse[0, h]) - score) <= 2.0 ** -21 * abs(score)   # log2(e), the product with it and with ln 2: a few roundings
+    half = D // 2
+    qd = torch.full((1, 2, half), top, dtype=dtype, device="cuda")
+    qd[:, 1] = -top
+    od, lam = torch.empty((1, 1, D), dtype=dtype, device="cuda"), torch.tensor([0.5], device="cuda")
+    torch.cuda.synchronize()
+    assert B.paged_decode_diff(cache, tables, gpu([n]), qd, lam, 1.0, od, work) == B.OK
+    ref = v[best, 0] - 0.5 * v[least, 0]                         # f32: a rounding of the difference, then the output's
+    assert bool(((od[0, 0].double() - ref).abs() <= (torch.finfo(dtype).eps / 2 + 2.0 ** -22) * ref.abs() + 2.0 ** -22 * v.abs().max()).all())
+
+
+def test_calls_behind_slow_kernels_copies_and_joined_streams():
+    """Every call waits for what comes before it, eager and captured: its inputs are written by a long kernel, by a copy, by another
+    stream, and what it wrote is read and overwritten right behind it."""
+    c = Case([600, 0, 1300], 4, 4, 128, 16, BF, lent=0.3, seed=2)
+    c.run()
+    want = c.out[:3].clone()
+    qs, lens = c.q.clone(), c.lens_t.clone()
+    q = torch.zeros_like(qs)
+    big = torch.ones(200_000_000, device="cuda")                 # a kernel of some 0.2 ms on it
+    out = torch.empty_like(want)
+    main, side = torch.cuda.Stream(), torch.cuda.Stream()
+
+    def step(results):
+        def decode():
+            assert B.paged_decode_tables(c.cache, c.tables, c.lens_t, q, c.scale, out, c.work, status=c.status, stream=torch.cuda.current_stream()) == B.OK
+        q.zero_()
+        c.lens_t.zero_()
+        big.mul_(1.0)
+        q.copy_(qs)                                              # a kernel or a copy
+        c.lens_t.copy_(lens)
+        decode()
+        results[0].copy_(out)
+        out.fill_(3.0)
+        q.zero_()
+        side.wait_stream(main)
+        with torch.cuda.stream(side):
+            big.mul_(1.0)
+            q.copy_(qs)
+        main.wait_stream(side)                                   # right behind another stream's work
+        decode()
+        decode()                                                 # and behind itself, with the same workspace
+        results[1].copy_(out)
+        side.wait_stream(main)                                   # work that overlaps with the next call on the other stream
+        with torch.cuda.stream(side):
+            big.mul_(1.0)
+        c.lens_t.zero_()
+        decode()
+        results[2].copy_(out)
+        c.lens_t.copy_(lens)
+        main.wait_stream(side)
+
+    results = [torch.zeros_like(want) for _ in range(3)]
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.stream(main):
+        step(results)
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph, stream=main):
+        step(results)
+    for k in range(6):
+        if k:
+            for r in results:
+                r.fill_(-1.0)
+            torch.cuda.synchronize()
+            if k % 2:
+                graph.replay()
+            else:
+                with torch.cuda.stream(main):
+                    step(results)
+            torch.cuda.synchronize()
+        assert torch.equal(results[0], want) and torch.equal(results[1], want) and not results[2].any()
+    assert int(c.status) == 0 and not c.work[:32768].any()
