@@ -91,7 +91,8 @@ struct Note {
   uint32_t chunk, chunks;       // first chunk (from the sequence's start), and how many
   uint32_t turn;                // warp of the first one; the next ones go to the next warps, in turn
   uint32_t solo;                // or all of them to the same warp, which also writes the rows out
-  uint32_t index, count, slot;  // piece `index` of the item's `count`, whose parts lie from `slot` on
+  uint32_t index, count;        // piece `index` of the item's `count`
+  uint32_t slot, step;          // piece i's part: slot + i * step; the first one's (step - 1) slots behind that
 };
 
 template <uint32_t D, uint32_t NT>
@@ -107,7 +108,7 @@ struct __align__(128) Shared {
   uint64_t rows_full[NT], rows_empty[NT];  // the consumers' partial rows of a piece
   uint64_t job_full[NT], job_done[NT];     // sums over parts that the consumers help with when they have nothing else to do
   struct Job {
-    uint32_t slot, stride, count, tile;    // count 0: leave; tiles from `tile` on
+    uint32_t slot, odd, stride, count, tile;  // count 0: leave; tiles from `tile` on
   } job[NT];
   uint32_t idle[NT];
   uint32_t started;                // chunks of the CTA's pieces that copies have been started of
@@ -537,6 +538,26 @@ __device__ __forceinline__ uint32_t pieces_of(const Cut& c, uint32_t head) {
   return head < c.heads[0] ? c.pieces[0] : head < c.heads[1] ? c.pieces[1] : c.pieces[2];
 }
 
+// Short work of few items (fewer than two to a CTA) is dealt out evenly instead: of the line of all chunks, CTA k takes chunks k * size
+// and on, up to the next one's. A cut that would leave less than `snap` chunks of an item on one side of it is moved to
+// that end of the item.
+struct Even {
+  uint32_t size, snap;          // size 0: not dealt out
+};
+
+// The item of chunks [at, at + chunks) of the line: it begins in CTA `owner`'s range, and goes on in that of the `cuts` next ones.
+struct Share {
+  uint32_t owner, cuts;
+};
+
+__device__ __forceinline__ Share share_of(const Even& even, unsigned long long at, uint32_t chunks) {
+  Share r;
+  r.owner = static_cast<uint32_t>((at + min(even.snap, chunks) + even.size - 1) / even.size) - 1;
+  const uint32_t last = static_cast<uint32_t>((at + chunks - min(even.snap, chunks)) / even.size);  // the last cut that is not moved to the item's end
+  r.cuts = chunks >= 2 * even.snap && last > r.owner ? last - r.owner : 0;
+  return r;
+}
+
 // Tickets drawn at a time when so many pieces are left.
 __device__ __forceinline__ uint32_t batch_of(uint32_t pieces, uint32_t most) {
   const uint32_t each = pieces / (gridDim.x * 4);
@@ -544,7 +565,7 @@ __device__ __forceinline__ uint32_t batch_of(uint32_t pieces, uint32_t most) {
 }
 
 template <uint32_t D, uint32_t NT>
-__device__ void schedule(const PagedDecodeParams& p, Shared<D, NT>& sh, const Zones& zones, uint32_t pieces, uint32_t batch, uint32_t most, bool many) {
+__device__ void schedule(const PagedDecodeParams& p, Shared<D, NT>& sh, const Zones& zones, const Even& even, uint32_t pieces, uint32_t batch, uint32_t most, bool many) {
   using S = Shape<D, NT>;
   constexpr uint32_t kTok = kHalf / (2 * D);
   const uint32_t lane = threadIdx.x & 31u;
@@ -563,7 +584,7 @@ __device__ void schedule(const PagedDecodeParams& p, Shared<D, NT>& sh, const Zo
     // have started copies of.
     uint64_t t0 = 0;
     uint32_t seen = 0;
-    for (uint32_t polls = 0; j; ++polls) {
+    for (uint32_t polls = 0; j && !even.size; ++polls) {
       const uint32_t started = *reinterpret_cast<volatile uint32_t*>(&sh.started);
       if (static_cast<int32_t>(number - started) < static_cast<int32_t>(kAhead)) break;
       if (*reinterpret_cast<volatile uint32_t*>(&sh.dead)) return;
@@ -582,6 +603,58 @@ __device__ void schedule(const PagedDecodeParams& p, Shared<D, NT>& sh, const Zo
       if (!__all_sync(0xffffffffu, wait_for(&sh.note_empty[tail % kNotes], tail / kNotes & 1u, sh, p.status))) return;
       ++tail;
     }
+    Note& note = sh.note[j % kNotes];
+    uint32_t a, b, slot, step;
+    if (even.size) {
+      const uint32_t me = blockIdx.x;
+      const unsigned long long from = static_cast<unsigned long long>(me) * even.size;
+      bool have = false;
+      Share share{};
+      while (!have) {
+        if (!found) {  // the item in which the range begins
+          uint32_t x = 0, n = S::kThreads;  // the last run of sequences that begins there or before
+          while (n > 1) {
+            const uint32_t half = n >> 1;
+            if (sh.chunks_before[x + half] <= from) x += half;
+            n -= half;
+          }
+          at = sh.chunks_before[x];
+          for (seq = x * run; seq < p.nseq; ++seq) {
+            span = span_of<kTok>(p, seq);
+            const unsigned long long all = static_cast<unsigned long long>(span.chunks) * p.num_kv_heads;
+            if (from < at + all) break;
+            at += all;
+          }
+          if (seq < p.nseq) head = static_cast<uint32_t>((from - at) / span.chunks);
+          found = true;
+        } else if (++head == p.num_kv_heads) {
+          head = 0;
+          at += static_cast<unsigned long long>(span.chunks) * p.num_kv_heads;
+          do {
+            ++seq;
+            if (seq < p.nseq) span = span_of<kTok>(p, seq);
+          } while (seq < p.nseq && span.chunks == 0);
+        }
+        if (seq >= p.nseq) break;
+        share = share_of(even, at + static_cast<unsigned long long>(head) * span.chunks, span.chunks);
+        if (share.owner > me) break;
+        index = me - share.owner;
+        have = index <= share.cuts;  // else its end was moved to where the range begins
+      }
+      if (!have) {
+        if (lane == 0) {
+          note.chunks = 0;
+          arrive(&sh.note_full[j % kNotes]);
+        }
+        return;
+      }
+      const unsigned long long start = at + static_cast<unsigned long long>(head) * span.chunks;
+      count = share.cuts + 1;
+      a = index ? static_cast<uint32_t>(from - start) : 0;
+      b = index < share.cuts ? static_cast<uint32_t>(from + even.size - start) : span.chunks;
+      slot = 2 * share.owner;  // of a CTA's two: the first one for an item that goes on there, the second one for one that begins there
+      step = 2;
+    } else {
     if (left == 0) {
       // A draw takes longer than a small piece: several at a time, fewer as the end comes nearer.
       const uint32_t rest = pieces > ticket ? pieces - ticket : 0;
@@ -592,7 +665,6 @@ __device__ void schedule(const PagedDecodeParams& p, Shared<D, NT>& sh, const Zo
       left = batch;
       found = false;
     }
-    Note& note = sh.note[j % kNotes];
     if (ticket >= pieces) {
       if (lane == 0) {
         note.chunks = 0;
@@ -661,7 +733,14 @@ __device__ void schedule(const PagedDecodeParams& p, Shared<D, NT>& sh, const Zo
       }
       count = pieces_of(cut, head);
     }
-    if (count > 1 && parts + count > kPagedMaxParts) {  // as above: never with lengths that stay as they are
+    a = static_cast<uint32_t>(static_cast<uint64_t>(span.chunks) * index / count);
+    b = static_cast<uint32_t>(static_cast<uint64_t>(span.chunks) * (index + 1) / count);
+    slot = parts;
+    step = 1;
+    ++ticket;
+    --left;
+    }
+    if (count > 1 && slot + count * step > kPagedMaxParts) {  // as above: never with lengths that stay as they are
       if (lane == 0) {
         ptx::report_status(p.status, kStatusInvalid);
         note.chunks = 0;
@@ -669,8 +748,6 @@ __device__ void schedule(const PagedDecodeParams& p, Shared<D, NT>& sh, const Zo
       }
       return;
     }
-    const uint32_t a = static_cast<uint32_t>(static_cast<uint64_t>(span.chunks) * index / count);
-    const uint32_t b = static_cast<uint32_t>(static_cast<uint64_t>(span.chunks) * (index + 1) / count);
     const bool solo = count == 1 && (b <= 2 || (many && b <= kSolo));
     if (lane == 0) {
       note.seq = seq;
@@ -683,14 +760,13 @@ __device__ void schedule(const PagedDecodeParams& p, Shared<D, NT>& sh, const Zo
       note.solo = solo;
       note.index = index;
       note.count = count;
-      note.slot = parts;
+      note.slot = slot;
+      note.step = step;
       arrive(&sh.note_full[j % kNotes]);
     }
     __syncwarp();
     number += solo ? 1 : b - a;
     turn = (turn + (solo ? 1 : b - a)) % S::kWarps;
-    ++ticket;
-    --left;
   }
 }
 
@@ -803,11 +879,11 @@ __device__ __forceinline__ float* part_of(const PagedDecodeParams& p, uint32_t s
   return p.parts + (static_cast<uint64_t>(slot) * NT + group) * Shape<D, NT>::kPart;
 }
 
-// Adds the parts of slots `slot`, slot + stride, .. (`count` of them, at most kFan) in that order: of the D / 16 tiles of a
+// Adds the parts of slots slot + odd, slot + stride, slot + 2 * stride, .. (`count` of them, at most kFan) in that order: of the D / 16 tiles of a
 // row, first, first + step, .. into sh.joined, and the columns' maxima and sums into m and l. `go_on` is asked before the
-// tiles, two at a time; returns the tile it stopped at.
+// tiles, two at a time.
 template <uint32_t D, uint32_t NT, typename GoOn>
-__device__ __forceinline__ uint32_t sum_parts(const PagedDecodeParams& p, Shared<D, NT>& sh, uint32_t group, uint32_t slot, uint32_t stride,
+__device__ __forceinline__ void sum_parts(const PagedDecodeParams& p, Shared<D, NT>& sh, uint32_t group, uint32_t slot, uint32_t odd, uint32_t stride,
                                               uint32_t count, uint32_t first, uint32_t step, float (&m)[2], float (&l)[2], GoOn go_on) {
   const uint32_t lane = threadIdx.x & 31u, tig = lane & 3u;
   constexpr uint32_t kSteps = D / 16, kAtOnce = NT == 1 ? 2 : 1;  // tiles, as far as the registers go
@@ -817,7 +893,7 @@ __device__ __forceinline__ uint32_t sum_parts(const PagedDecodeParams& p, Shared
     float4 ml[kFan];
 #pragma unroll
     for (uint32_t c = 0; c < kFan; ++c)
-      ml[c] = used && c < count ? __ldcg(reinterpret_cast<const float4*>(part_of<D, NT>(p, slot + c * stride, group) + 8 * D) + tig)
+      ml[c] = used && c < count ? __ldcg(reinterpret_cast<const float4*>(part_of<D, NT>(p, slot + (c ? c * stride : odd), group) + 8 * D) + tig)
                                 : make_float4(kMinusInf, 0.f, kMinusInf, 0.f);
     m[0] = m[1] = kMinusInf;
     l[0] = l[1] = 0.f;
@@ -837,14 +913,14 @@ __device__ __forceinline__ uint32_t sum_parts(const PagedDecodeParams& p, Shared
   }
   uint32_t tile = first;
 #pragma unroll 1
-  for (; tile < kSteps && go_on(); tile += step * kAtOnce) {
+  for (; tile < kSteps && go_on(tile); tile += step * kAtOnce) {
     float4 v[kAtOnce][kFan];
 #pragma unroll
     for (uint32_t i = 0; i < kAtOnce; ++i) {
       const uint32_t x = tile + i * step;
 #pragma unroll
       for (uint32_t c = 0; c < kFan; ++c)
-        v[i][c] = used && c < count && x < kSteps ? __ldcg(reinterpret_cast<const float4*>(part_of<D, NT>(p, slot + c * stride, group)) + x * 32 + lane)
+        v[i][c] = used && c < count && x < kSteps ? __ldcg(reinterpret_cast<const float4*>(part_of<D, NT>(p, slot + (c ? c * stride : odd), group)) + x * 32 + lane)
                                                   : make_float4(0.f, 0.f, 0.f, 0.f);
     }
 #pragma unroll
@@ -861,7 +937,51 @@ __device__ __forceinline__ uint32_t sum_parts(const PagedDecodeParams& p, Shared
       if (x < kSteps) reinterpret_cast<float4*>(sh.joined[group])[x * 32 + lane] = acc;
     }
   }
-  return tile;
+}
+
+// The consumers' rows of a piece, in the order of their chunks.
+template <uint32_t D, uint32_t NT>
+__device__ __forceinline__ void sum_rows(const PagedDecodeParams& p, const Shared<D, NT>& sh, uint32_t group, const Note& note, Rows<D>& r) {
+  constexpr uint32_t kWarps = Shape<D, NT>::kWarps, kSteps = D / 16;
+  const uint32_t lane = threadIdx.x & 31u, tig = lane & 3u;
+  clear(r);
+  if (group * 8 + 2 * tig >= p.rows) return;
+  const float* part[kWarps];
+  float w[kWarps][2], l[kWarps][2];
+#pragma unroll
+  for (uint32_t x = 0; x < kWarps; ++x) {
+    const uint32_t warp = note.turn + x < kWarps ? note.turn + x : note.turn + x - kWarps;
+    part[x] = sh.part[group][warp];
+    const float4 ml = x < note.chunks ? reinterpret_cast<const float4*>(part[x] + 8 * D)[tig] : make_float4(kMinusInf, 0.f, kMinusInf, 0.f);
+    w[x][0] = ml.x;
+    w[x][1] = ml.z;
+    l[x][0] = ml.y;
+    l[x][1] = ml.w;
+    r.m[0] = fmaxf(r.m[0], ml.x);
+    r.m[1] = fmaxf(r.m[1], ml.z);
+  }
+#pragma unroll
+  for (uint32_t j = 0; j < 2; ++j) {
+    const float safe = r.m[j] == kMinusInf ? 0.f : r.m[j];
+#pragma unroll
+    for (uint32_t x = 0; x < kWarps; ++x) {
+      w[x][j] = ptx::exp2_approx((w[x][j] - safe) * p.scale_log2);
+      r.l[j] = fmaf(l[x][j], w[x][j], r.l[j]);
+    }
+  }
+#pragma unroll
+  for (uint32_t x = 0; x < kWarps; ++x) {
+    if (x >= note.chunks) break;
+#pragma unroll
+    for (uint32_t mt = 0; mt < kSteps; ++mt) {
+      const float4 v = reinterpret_cast<const float4*>(part[x])[mt * 32 + lane];
+      float(&o)[4] = r.o[mt];
+      o[0] = fmaf(v.x, w[x][0], o[0]);
+      o[1] = fmaf(v.y, w[x][1], o[1]);
+      o[2] = fmaf(v.z, w[x][0], o[2]);
+      o[3] = fmaf(v.w, w[x][1], o[3]);
+    }
+  }
 }
 
 template <uint32_t D, uint32_t NT, bool kBf16>
@@ -946,13 +1066,12 @@ __device__ void consume(const PagedDecodeParams& p, const Maps& maps, Shared<D, 
     return;
   }
   // Nothing left to stream: sums over parts go faster with all warps.
-  if (!__all_sync(0xffffffffu, wait_for(&sh.rows_empty[group], (merges & 1u) ^ 1u, sh, p.status))) return;
   if (lane == 0) atomicAdd(&sh.idle[group], 1u);
   for (uint32_t k = 0;; ++k) {
     if (!__all_sync(0xffffffffu, wait_for(&sh.job_full[group], k & 1u, sh, p.status))) return;
     const auto& job = sh.job[group];
     if (job.count == 0) return;
-    sum_parts<D, NT>(p, sh, group, job.slot, job.stride, job.count, job.tile + warp, S::kWarps, r.m, r.l, [] { return true; });
+    sum_parts<D, NT>(p, sh, group, job.slot, job.odd, job.stride, job.count, job.tile + warp, S::kWarps, r.m, r.l, [](uint32_t) { return true; });
     __syncwarp();
     if (lane == 0) arrive(&sh.job_done[group]);
   }
@@ -974,22 +1093,20 @@ __device__ void merge(const PagedDecodeParams& p, Shared<D, NT>& sh, uint32_t gr
     if (note.solo || (note.chunks == 1 && note.count == 1)) continue;
     if (!__all_sync(0xffffffffu, wait_for(&sh.rows_full[group], merges & 1u, sh, p.status))) return;
     ++merges;
-    clear(r);
-    const uint32_t parts = min(note.chunks, S::kWarps);
-    for (uint32_t x = 0; x < parts; ++x) add_part<D>(p, r, col0, sh.part[group][(note.turn + x) % S::kWarps]);
+    sum_rows<D, NT>(p, sh, group, note, r);
     __syncwarp();
     if (lane == 0) arrive(&sh.rows_empty[group]);
 
     // Up the tree: store the rows, and where they are their group's last ones, take the group's sum on.
-    uint32_t index = note.index, count = note.count, stride = 1;
+    uint32_t index = note.index, count = note.count, stride = note.step;
     bool mine = true;
     for (uint32_t level = 0; count > 1; ++level) {
       const uint32_t g = index / kFan, n = min(kFan, count - g * kFan);
-      const uint32_t first = note.slot + g * kFan * stride;
-      store_part<D>(p, r, col0, part_of<D, NT>(p, note.slot + index * stride, group));
+      const uint32_t first = note.slot + g * kFan * stride, odd = g ? 0 : note.step - 1;
+      store_part<D>(p, r, col0, part_of<D, NT>(p, index ? note.slot + index * stride : note.slot + odd, group));
       __threadfence();
       __syncwarp();
-      uint32_t* counter = p.counters + kPagedTree + (group * 3 + level) * kPagedMaxParts + first;
+      uint32_t* counter = p.counters + kPagedTree + (group * 3 + level) * kPagedMaxParts + first + odd;
       uint32_t arrived = 0;
       if (lane == 0) {
         arrived = atomicAdd(counter, 1u);
@@ -1003,18 +1120,23 @@ __device__ void merge(const PagedDecodeParams& p, Shared<D, NT>& sh, uint32_t gr
       __threadfence();
       if (n <= 4) {
         clear(r);
-        for (uint32_t c = 0; c < n; ++c) add_part<D>(p, r, col0, part_of<D, NT>(p, first + c * stride, group));
+        for (uint32_t c = 0; c < n; ++c) add_part<D>(p, r, col0, part_of<D, NT>(p, first + (c ? c * stride : odd), group));
       } else {
         // One warp has 8 or 16 KB of the parts in flight; as soon as the consumers have nothing else to do they take
         // the tiles that are left.
-        const uint32_t tile = sum_parts<D, NT>(p, sh, group, first, stride, n, 0, 1, r.m, r.l, [&] {
-          return __shfl_sync(0xffffffffu, *reinterpret_cast<volatile uint32_t*>(&sh.idle[group]), 0) != S::kWarps;
-        });
-        if (tile < kSteps) {
+        bool given = false;
+        auto give = [&](uint32_t tile) {
+          if (__shfl_sync(0xffffffffu, *reinterpret_cast<volatile uint32_t*>(&sh.idle[group]), 0) != S::kWarps) return false;
           if (lane == 0) {
-            sh.job[group] = {first, stride, n, tile};
+            sh.job[group] = {first, odd, stride, n, tile};
             arrive(&sh.job_full[group]);
           }
+          given = true;
+          return true;
+        };
+        give(0);
+        sum_parts<D, NT>(p, sh, group, first, odd, stride, n, 0, 1, r.m, r.l, [&](uint32_t tile) { return !given && !give(tile); });
+        if (given) {
           if (!__all_sync(0xffffffffu, wait_for(&sh.job_done[group], jobs & 1u, sh, p.status))) return;
           ++jobs;
         }
@@ -1091,23 +1213,33 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) paged_decode_kernel
     if (x < warp) before += sh.warp_total[x];
     total += sh.warp_total[x];
   }
-  Zones zones;
+  constexpr uint32_t kLeast = 2 * S::kWarps;  // at least two chunks for every warp: a join costs what three take
   const unsigned long long share = total / gridDim.x;  // of a CTA
-  zones.end[0] = share * gridDim.x * kPagedZone0 / 16;
-  zones.end[1] = share * gridDim.x * kPagedZone1 / 16;
-  // Few items are all cut, and a join over many parts takes longer than uneven ends: two pieces to a CTA throughout (one
-  // sequence of 150000 tokens, 8 KV heads: 107 us, against 124 us with the finer cut; two items to a CTA and more the other
-  // way round: 64 sequences of up to 4095 tokens 99 us against 103, 48 of up to 6000 differential 102 against 109).
-  // At least two chunks for every warp: a join costs what three take.
-  constexpr uint32_t kLeast = 2 * S::kWarps;
-  const bool finer = static_cast<unsigned long long>(p.nseq) * p.num_kv_heads >= 2 * gridDim.x;
-  // (If that leaves pieces of the least size, there would be somewhat more of them than CTAs: then one to a CTA.)
-  const uint32_t half = static_cast<uint32_t>(share / kPagedCut0) + 1, coarse = half >= kLeast ? half : max(static_cast<uint32_t>(share) + 1, kLeast);
-  zones.size[0] = coarse;
-  zones.size[1] = finer ? max(static_cast<uint32_t>(share / kPagedCut1) + 1, kLeast) : coarse;
-  zones.size[2] = finer ? max(static_cast<uint32_t>(share / kPagedCut2) + 1, kLeast) : coarse;
-  uint2 cut = make_uint2(0, 0);
-  {
+  const bool few = static_cast<unsigned long long>(p.nseq) * p.num_kv_heads < 2 * gridDim.x;
+  Zones zones{};
+  Even even{};
+  uint32_t pieces = 0, most = 1, batch = 1;
+  bool many = false;
+  sh.chunks_before[tid] = before;
+  if (few && share < 8 * kLeast) {
+    // Short work: what comes after the last chunk, a merge and a join or two of 3 us each, is a good part of the time, and a
+    // CTA's first piece's join is in its second one's way. One sequence of 20000 tokens, 8 KV heads: 28 us against 36 in two
+    // pieces to a CTA; 16 of 3000 40 against 41.6; beyond, SMs that get less of HBM count for more: 5 of 100001 321 against 315.
+    even.size = max(static_cast<uint32_t>((total + gridDim.x - 1) / gridDim.x), kLeast);
+    even.snap = kLeast;
+    pieces = static_cast<uint32_t>((total + even.size - 1) / even.size);  // as many CTAs
+  } else {
+    zones.end[0] = share * gridDim.x * kPagedZone0 / 16;
+    zones.end[1] = share * gridDim.x * kPagedZone1 / 16;
+    // Few items are all cut, and a join over many parts takes longer than uneven ends: two pieces to a CTA throughout (one
+    // sequence of 150000 tokens, 8 KV heads: 107 us, against 124 us with the finer cut; two items to a CTA and more the other
+    // way round: 64 sequences of up to 4095 tokens 99 us against 103, 48 of up to 6000 differential 102 against 109).
+    // (If that leaves pieces of the least size, there would be somewhat more of them than CTAs: then one to a CTA.)
+    const uint32_t half = static_cast<uint32_t>(share / kPagedCut0) + 1, coarse = half >= kLeast ? half : max(static_cast<uint32_t>(share) + 1, kLeast);
+    zones.size[0] = coarse;
+    zones.size[1] = few ? coarse : max(static_cast<uint32_t>(share / kPagedCut1) + 1, kLeast);
+    zones.size[2] = few ? coarse : max(static_cast<uint32_t>(share / kPagedCut2) + 1, kLeast);
+    uint2 cut = make_uint2(0, 0);
     unsigned long long at = before;
     for (uint32_t i = i0; i < i1; ++i) {
       const uint32_t chunks = span_of<kTok>(p, i).chunks;
@@ -1116,45 +1248,45 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) paged_decode_kernel
       cut.y += c.parts;
       at += static_cast<unsigned long long>(chunks) * p.num_kv_heads;
     }
-  }
-  uint2 sum = cut;
+    uint2 sum = cut;
 #pragma unroll
-  for (int d = 1; d < 32; d <<= 1) {
-    const uint32_t a = __shfl_up_sync(0xffffffffu, sum.x, d), b = __shfl_up_sync(0xffffffffu, sum.y, d);
-    if (lane >= static_cast<uint32_t>(d)) {
-      sum.x += a;
-      sum.y += b;
+    for (int d = 1; d < 32; d <<= 1) {
+      const uint32_t a = __shfl_up_sync(0xffffffffu, sum.x, d), b = __shfl_up_sync(0xffffffffu, sum.y, d);
+      if (lane >= static_cast<uint32_t>(d)) {
+        sum.x += a;
+        sum.y += b;
+      }
     }
-  }
-  if (lane == 31) {
-    sh.warp_sum[warp][0] = sum.x;
-    sh.warp_sum[warp][1] = sum.y;
-  }
-  __syncthreads();
-  uint32_t pieces = 0;
-  sum.x -= cut.x;
-  sum.y -= cut.y;
-  for (uint32_t x = 0; x < kAllWarps; ++x) {
-    if (x < warp) {
-      sum.x += sh.warp_sum[x][0];
-      sum.y += sh.warp_sum[x][1];
+    if (lane == 31) {
+      sh.warp_sum[warp][0] = sum.x;
+      sh.warp_sum[warp][1] = sum.y;
     }
-    pieces += sh.warp_sum[x][0];
+    __syncthreads();
+    sum.x -= cut.x;
+    sum.y -= cut.y;
+    for (uint32_t x = 0; x < kAllWarps; ++x) {
+      if (x < warp) {
+        sum.x += sh.warp_sum[x][0];
+        sum.y += sh.warp_sum[x][1];
+      }
+      pieces += sh.warp_sum[x][0];
+    }
+    sh.pieces_before[tid] = sum.x;
+    sh.parts_before[tid] = sum.y;
+    // Tickets to a draw: as many as two dozen chunks or so are.
+    const uint32_t mean = pieces ? static_cast<uint32_t>(min(total / pieces, 24ull)) : 24;
+    most = 24 / max(mean, 1u);
+    batch = batch_of(pieces, most);
+    // Items that one warp takes alone: only where every warp gets several of them.
+    many = pieces >= 4 * S::kWarps * gridDim.x && total <= static_cast<unsigned long long>(pieces) * kSolo;
   }
-  sh.pieces_before[tid] = sum.x;
-  sh.parts_before[tid] = sum.y;
-  sh.chunks_before[tid] = before;
   __syncthreads();
 
-  // Tickets to a draw: as many as two dozen chunks or so are.
-  const uint32_t mean = pieces ? static_cast<uint32_t>(min(total / pieces, 24ull)) : 24, most = 24 / max(mean, 1u), batch = batch_of(pieces, most);
-  // Items that one warp takes alone: only where every warp gets several of them.
-  const bool many = pieces >= 4 * S::kWarps * gridDim.x && total <= static_cast<unsigned long long>(pieces) * kSolo;
   if (static_cast<unsigned long long>(blockIdx.x) * batch < pieces) {
     if (warp < S::kConsumers)
       consume<D, NT, kBf16>(p, maps, sh);
     else if (warp == S::kConsumers)
-      schedule<D, NT>(p, sh, zones, pieces, batch, most, many);
+      schedule<D, NT>(p, sh, zones, even, pieces, batch, most, many);
     else
       merge<D, NT, kBf16>(p, sh, warp - S::kConsumers - 1);
   }
