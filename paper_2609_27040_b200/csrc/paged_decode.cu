@@ -28,7 +28,7 @@
 //   * The differential form is the same pass: K heads 2g, 2g+1 of width D/2 lie side by side, so q1 is
 //     padded with zeros behind and q2 in front and the 2G rows of a head run over K and V of width D. The two
 //     maps of a head are neighbouring columns, which one thread holds.
-//   * A cut item's pieces meet in the workspace, sixteen at a time: whichever piece of a group arrives last adds
+//   * A cut item's pieces meet in the workspace, 16 or 32 at a time: whichever piece of a group arrives last adds
 //     the group's rows, in order, and is a piece of the next level. The result does not depend on who that is.
 #include <cuda.h>
 #include <cuda_bf16.h>
@@ -52,7 +52,8 @@ constexpr uint32_t kAhead = 6;
 // pieces are many and this small on average, items of so many chunks are, too: 1000 sequences of 10 to 260 tokens
 // 119 us, with 4 (which leaves most of them to all warps) 183.
 constexpr uint32_t kSolo = 8;
-constexpr uint32_t kFan = kPagedFan;                // pieces that meet at a time
+constexpr uint32_t kFan = kPagedFan;                // most pieces that meet at a time
+static_assert(kFan == 32, "sum_parts takes two times sixteen");
 constexpr float kMinusInf = -INFINITY;
 
 // Partial rows of eight columns: [D / 16][32 lanes] float4, then the columns' (maximum, sum) pairs.
@@ -879,64 +880,81 @@ __device__ __forceinline__ float* part_of(const PagedDecodeParams& p, uint32_t s
   return p.parts + (static_cast<uint64_t>(slot) * NT + group) * Shape<D, NT>::kPart;
 }
 
-// Adds the parts of slots slot + odd, slot + stride, slot + 2 * stride, .. (`count` of them, at most kFan) in that order: of the D / 16 tiles of a
-// row, first, first + step, .. into sh.joined, and the columns' maxima and sums into m and l. `go_on` is asked before the
-// tiles, two at a time.
+// Adds the parts of slots slot + odd, slot + stride, slot + 2 * stride, .. (`count` of them, at most kFan) in that order: of the
+// D / 16 tiles of a row, first, first + step, .. into sh.joined, and the columns' maxima and sums into m and l. `go_on` is asked
+// before the tiles, two at a time. A lane reads the maxima and sums of every eighth part; the first tiles are read meanwhile.
 template <uint32_t D, uint32_t NT, typename GoOn>
-__device__ __forceinline__ void sum_parts(const PagedDecodeParams& p, Shared<D, NT>& sh, uint32_t group, uint32_t slot, uint32_t odd, uint32_t stride,
-                                              uint32_t count, uint32_t first, uint32_t step, float (&m)[2], float (&l)[2], GoOn go_on) {
-  const uint32_t lane = threadIdx.x & 31u, tig = lane & 3u;
-  constexpr uint32_t kSteps = D / 16, kAtOnce = NT == 1 ? 2 : 1;  // tiles, as far as the registers go
+__device__ __forceinline__ void sum_parts(const PagedDecodeParams& p, Shared<D, NT>& sh, uint32_t group, uint32_t slot, uint32_t odd,
+                                          uint32_t stride, uint32_t count, uint32_t first, uint32_t step, float (&m)[2], float (&l)[2], GoOn go_on) {
+  const uint32_t lane = threadIdx.x & 31u, gid = lane >> 2, tig = lane & 3u;
+  constexpr uint32_t kSteps = D / 16, kOwn = kFan / 8, kTiles = NT == 1 ? 2 : 1;  // as far as the registers go
   const bool used = group * 8 + 2 * tig < p.rows;
-  float w[kFan][2];
-  {
-    float4 ml[kFan];
+  auto part = [&](uint32_t c) { return reinterpret_cast<const float4*>(part_of<D, NT>(p, slot + (c ? c * stride : odd), group)); };
+  float4 ml[kOwn];
 #pragma unroll
-    for (uint32_t c = 0; c < kFan; ++c)
-      ml[c] = used && c < count ? __ldcg(reinterpret_cast<const float4*>(part_of<D, NT>(p, slot + (c ? c * stride : odd), group) + 8 * D) + tig)
-                                : make_float4(kMinusInf, 0.f, kMinusInf, 0.f);
+  for (uint32_t i = 0; i < kOwn; ++i)
+    ml[i] = used && gid + 8 * i < count ? __ldcg(part(gid + 8 * i) + 2 * D + tig) : make_float4(kMinusInf, 0.f, kMinusInf, 0.f);
+  float w[kOwn][2];
+  auto weigh = [&] {
     m[0] = m[1] = kMinusInf;
     l[0] = l[1] = 0.f;
 #pragma unroll
-    for (uint32_t c = 0; c < kFan; ++c) {
-      m[0] = fmaxf(m[0], ml[c].x);
-      m[1] = fmaxf(m[1], ml[c].z);
+    for (uint32_t i = 0; i < kOwn; ++i) {
+      m[0] = fmaxf(m[0], ml[i].x);
+      m[1] = fmaxf(m[1], ml[i].z);
     }
+#pragma unroll
+    for (int x = 4; x <= 16; x <<= 1)
+#pragma unroll
+      for (uint32_t j = 0; j < 2; ++j) m[j] = fmaxf(m[j], __shfl_xor_sync(0xffffffffu, m[j], x));
     const float s0 = m[0] == kMinusInf ? 0.f : m[0], s1 = m[1] == kMinusInf ? 0.f : m[1];
 #pragma unroll
-    for (uint32_t c = 0; c < kFan; ++c) {
-      w[c][0] = ptx::exp2_approx((ml[c].x - s0) * p.scale_log2);
-      w[c][1] = ptx::exp2_approx((ml[c].z - s1) * p.scale_log2);
-      l[0] = fmaf(ml[c].y, w[c][0], l[0]);
-      l[1] = fmaf(ml[c].w, w[c][1], l[1]);
+    for (uint32_t i = 0; i < kOwn; ++i) {
+      w[i][0] = ptx::exp2_approx((ml[i].x - s0) * p.scale_log2);
+      w[i][1] = ptx::exp2_approx((ml[i].z - s1) * p.scale_log2);
+      l[0] = fmaf(ml[i].y, w[i][0], l[0]);
+      l[1] = fmaf(ml[i].w, w[i][1], l[1]);
     }
-  }
+#pragma unroll
+    for (int x = 4; x <= 16; x <<= 1)
+#pragma unroll
+      for (uint32_t j = 0; j < 2; ++j) l[j] += __shfl_xor_sync(0xffffffffu, l[j], x);
+  };
   uint32_t tile = first;
 #pragma unroll 1
-  for (; tile < kSteps && go_on(tile); tile += step * kAtOnce) {
-    float4 v[kAtOnce][kFan];
+  for (; tile < kSteps && go_on(tile); tile += step * kTiles) {
+    float4 acc[kTiles];
 #pragma unroll
-    for (uint32_t i = 0; i < kAtOnce; ++i) {
-      const uint32_t x = tile + i * step;
+    for (uint32_t i = 0; i < kTiles; ++i) acc[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 1
+    for (uint32_t c0 = 0; c0 < count; c0 += 16) {
+      float4 v[kTiles][16];
 #pragma unroll
-      for (uint32_t c = 0; c < kFan; ++c)
-        v[i][c] = used && c < count && x < kSteps ? __ldcg(reinterpret_cast<const float4*>(part_of<D, NT>(p, slot + (c ? c * stride : odd), group)) + x * 32 + lane)
-                                                  : make_float4(0.f, 0.f, 0.f, 0.f);
-    }
+      for (uint32_t i = 0; i < kTiles; ++i) {
+        const uint32_t x = tile + i * step;
 #pragma unroll
-    for (uint32_t i = 0; i < kAtOnce; ++i) {
-      const uint32_t x = tile + i * step;
-      float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-      for (uint32_t c = 0; c < kFan; ++c) {
-        acc.x = fmaf(v[i][c].x, w[c][0], acc.x);
-        acc.y = fmaf(v[i][c].y, w[c][1], acc.y);
-        acc.z = fmaf(v[i][c].z, w[c][0], acc.z);
-        acc.w = fmaf(v[i][c].w, w[c][1], acc.w);
+        for (uint32_t c = 0; c < 16; ++c)
+          v[i][c] = used && c0 + c < count && x < kSteps ? __ldcg(part(c0 + c) + x * 32 + lane) : make_float4(0.f, 0.f, 0.f, 0.f);
       }
-      if (x < kSteps) reinterpret_cast<float4*>(sh.joined[group])[x * 32 + lane] = acc;
+      if (tile == first && c0 == 0) weigh();
+#pragma unroll
+      for (uint32_t c = 0; c < 16; ++c) {
+        const uint32_t from = (c & 7u) * 4 + tig, k = c >> 3;
+        const float w0 = __shfl_sync(0xffffffffu, c0 ? w[k + 2][0] : w[k][0], from), w1 = __shfl_sync(0xffffffffu, c0 ? w[k + 2][1] : w[k][1], from);
+#pragma unroll
+        for (uint32_t i = 0; i < kTiles; ++i) {
+          acc[i].x = fmaf(v[i][c].x, w0, acc[i].x);
+          acc[i].y = fmaf(v[i][c].y, w1, acc[i].y);
+          acc[i].z = fmaf(v[i][c].z, w0, acc[i].z);
+          acc[i].w = fmaf(v[i][c].w, w1, acc[i].w);
+        }
+      }
     }
+#pragma unroll
+    for (uint32_t i = 0; i < kTiles; ++i)
+      if (tile + i * step < kSteps) reinterpret_cast<float4*>(sh.joined[group])[(tile + i * step) * 32 + lane] = acc[i];
   }
+  if (tile == first) weigh();
 }
 
 // The consumers' rows of a piece, in the order of their chunks.
@@ -1099,10 +1117,13 @@ __device__ void merge(const PagedDecodeParams& p, Shared<D, NT>& sh, uint32_t gr
 
     // Up the tree: store the rows, and where they are their group's last ones, take the group's sum on.
     uint32_t index = note.index, count = note.count, stride = note.step;
+    // Dealt-out work: a join comes at the end, with all warps (one level for 17 to 32 parts: one sequence of 20000 tokens, 8 KV
+    // heads, 26.4 us against 28.2). By tickets it is mostly this warp's alone, between pieces: one of 80000 67 us against 71.
+    const uint32_t fan = note.step == 1 ? kFan / 2 : kFan;
     bool mine = true;
     for (uint32_t level = 0; count > 1; ++level) {
-      const uint32_t g = index / kFan, n = min(kFan, count - g * kFan);
-      const uint32_t first = note.slot + g * kFan * stride, odd = g ? 0 : note.step - 1;
+      const uint32_t g = index / fan, n = min(fan, count - g * fan);
+      const uint32_t first = note.slot + g * fan * stride, odd = g ? 0 : note.step - 1;
       store_part<D>(p, r, col0, part_of<D, NT>(p, index ? note.slot + index * stride : note.slot + odd, group));
       __threadfence();
       __syncwarp();
@@ -1151,8 +1172,8 @@ __device__ void merge(const PagedDecodeParams& p, Shared<D, NT>& sh, uint32_t gr
       }
       __syncwarp();
       index = g;
-      count = (count + kFan - 1) / kFan;
-      stride *= kFan;
+      count = (count + fan - 1) / fan;
+      stride *= fan;
     }
     if (mine) write_out<D, kBf16>(p, r, note.seq, note.head, col0);
   }
