@@ -605,3 +605,37 @@ def test_calls_behind_slow_kernels_copies_and_joined_streams():
             torch.cuda.synchronize()
         assert torch.equal(results[0], want) and torch.equal(results[1], want) and not results[2].any()
     assert int(c.status) == 0 and not c.work[:32768].any()
+
+
+@pytest.mark.parametrize("diff", [False, True], ids=["plain", "diff"])
+@pytest.mark.parametrize("lens,Hkv,G,D,T", [
+    ([20000], 1, 2, 128, 16),                                    # one item in dozens of parts: more than one level of sums
+    ([9000], 3, 8, 64, 64),
+    ([3000, 50, 4000, 1, 700, 0, 2500, 390], 1, 3, 128, 32),     # items that end where others begin
+    ([384, 385, 383, 400, 767, 768, 769, 1, 5], 2, 1, 128, 16),  # around the least piece and twice that
+    ([6000, 40, 5000], 2, 7, 256, 16),
+    ([700, 1500, 20, 2600, 0, 0, 1100, 333, 64], 7, 1, 64, 16),
+    ([14000, 13000], 8, 1, 256, 64),                             # few items, but long ones: by tickets
+])
+def test_few_items(lens, Hkv, G, D, T, diff):
+    c = Case(lens, Hkv, G, D, T, BF, lent=0.3, seed=sum(lens) % 97, diff=diff, stray=float("nan"))
+    c.run()
+    c.check()
+    again = c.out.clone()
+    for _ in range(3):
+        c.run()
+        assert torch.equal(c.out, again)
+    c.run(window=1000)
+    c.check()
+
+
+@pytest.mark.parametrize("seed", range(12))
+def test_random_batches_of_few_items(seed):
+    rng = np.random.default_rng(1000 + seed)
+    n, Hkv = int(rng.integers(1, 25)), int(rng.choice([1, 2, 5, 8]))
+    lens = [int(x) for x in rng.integers(0, int(rng.choice([40, 600, 3000, 9000])), n)]
+    D, T, diff = int(rng.choice([64, 128, 256])), int(rng.choice([16, 32, 64])), bool(rng.integers(2))
+    G = int(rng.integers(1, 9 if diff else 17))
+    c = Case(lens, Hkv, G, D, T, [BF, HF][seed % 2], lent=0.25, seed=seed, diff=diff, stray=float("inf"))
+    c.run()
+    c.check()
