@@ -6,14 +6,15 @@
 //
 // Every K and V byte is needed once and used for a handful of query rows: the kernel is bound by HBM,
 // and what it does is keep enough copies in flight on every SM while the arithmetic stays hidden. Measured
-// (B200, 6.45 TB/s copy rate): 64 sequences of 512 to 4095 tokens, 32/8 heads of 128: 99 us, 6.1 TB/s; 5 of 60000
-// to 100001, 64/8 heads: 250 us, 6.6 TB/s; 200 with a window of 1000, 12 heads of 64: 92 us, 6.0 TB/s; differential,
-// 8 of 9000 to 40000, 16/4 heads of 256: 133 us, 6.0 TB/s; one of 500 tokens: 12 us (launch, one read of the lengths, of a
-// table cell, of the cache, one merge, each a trip to L2 or HBM).
+// (B200, 6.45 TB/s copy rate): 64 sequences of 512 to 4095 tokens, 32/8 heads of 128: 101 us, 6.0 TB/s; 5 of 60000
+// to 100001, 64/8 heads: 252 us, 6.5 TB/s; 200 with a window of 1000, 12 heads of 64: 95 us, 5.8 TB/s; differential,
+// 8 of 9000 to 40000, 16/4 heads of 256: 134 us, 6.0 TB/s; one of 20000, 32/8 heads: 26 us; one of 500: 10.8 us (launch,
+// one read of the lengths, of a table cell, of the cache, one merge, each a trip to L2 or HBM).
 //   * Work is cut into pieces, runs of chunks of one (sequence, KV head), an item; a chunk is 16 KB of it (64 /
-//     32 / 16 tokens of K and V for head_dim 64 / 128 / 256). How items are cut (cut_of) depends on the lengths
-//     alone; who computes a piece is settled by a ticket counter, because the SMs do not get equal shares of
-//     HBM: with equal static ranges the first CTA had its data at 81 us, the last at 95.
+//     32 / 16 tokens of K and V for head_dim 64 / 128 / 256). How items are cut (cut_of, share_of) depends on the
+//     lengths alone; who computes a piece is settled by a ticket counter, because the SMs do not get equal shares of
+//     HBM: with equal static ranges the first CTA had its data at 81 us, the last at 95. (Short work of few items is
+//     dealt out, one range to a CTA: what counts there is that nobody's last rows wait for another join.)
 //   * In a CTA, a scheduler warp draws tickets, a little ahead of the work. Consumer warps take the chunks of a
 //     piece in turn, each through its own online softmax; each copies its own chunks, two at a time, into stages
 //     of its own (tiled bulk copies of [tokens][head] boxes, the format's swizzled rows as they are: one warp that
@@ -46,7 +47,8 @@ constexpr uint32_t kHalf = kStageBytes / 2;
 constexpr uint32_t kDepth = 2;                      // stages of a consumer warp
 constexpr uint32_t kNotes = 16;                     // most pieces known to the consumers at a time
 // Chunks of known pieces that no copy has been started of (an item that one warp takes alone counts as one chunk): 200 sequences
-// of at most 1000 attended tokens, 12 heads of 64: 92 us, with 3 95, with 24 112; 64 of up to 4095 tokens: 99 us with 3 to 24.
+// of at most 1000 attended tokens, 12 heads of 64: 92 us, with 3 95, with 24 112; 64 of up to 4095 tokens: 99 us with 3 to 24 (both before the sums of
+// a piece's rows and the weights took their present forms).
 constexpr uint32_t kAhead = 6;
 // Items of at most two chunks are taken by one warp, which also writes them out (a merge takes longer than a chunk). Where
 // pieces are many and this small on average, items of so many chunks are, too: 1000 sequences of 10 to 260 tokens

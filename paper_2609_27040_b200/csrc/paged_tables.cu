@@ -12,8 +12,8 @@
 // entry. Only the stacks' new tops and the blocks that shrinking requests give back must wait until every
 // CTA has read the old ones: the CTA that draws the last ticket does both.
 // Bound by latency: launch, one read of the lengths, the block-wide scan, one read of a table or
-// stack entry, the stores. One new token for each of 256 requests: 4.0 us a launch back to back; 550 000 new tokens of
-// 1000 requests: 8.9 us (6.9 MB to write, 1.1 us at the copy rate; each CTA fills two steps of 2048).
+// stack entry, the stores. One new token for each of 256 requests: 3.9 us a launch back to back; 550 000 new tokens of
+// 1000 requests: 8.4 us (6.9 MB to write, 1.1 us at the copy rate; each CTA fills two steps of 2048).
 #include "kernels.h"
 #include "ptx.cuh"
 
@@ -344,7 +344,7 @@ __global__ void __launch_bounds__(kBuildThreads, 1) build_tables_kernel(const Bu
 // r is stored at unit u ^ (r & 7) of its 128 bytes. `lanes` (8, 16 or 32) neighbouring threads take a
 // token together. A thread has kRows * kUnits independent loads of K and as many of V in flight: four units of
 // one token where rows are long enough, else one unit of each of four tokens. Bound by HBM: the rows are read
-// and written once (131071 tokens of 8 heads of 128: 178 us, 6.0 TB/s, 93 % of a plain copy's rate).
+// and written once (131071 tokens of 8 heads of 128: 164 us, 6.55 TB/s, a plain copy's rate).
 constexpr uint32_t kWriteThreads = 256;
 
 template <uint32_t kRows, uint32_t kUnits>
