@@ -9,7 +9,6 @@ from __future__ import annotations
 
 import ctypes as C
 import os
-import struct as _struct
 from typing import Optional, Sequence
 
 import numpy as np
@@ -145,7 +144,7 @@ def lib() -> C.CDLL:
         L.slice_copy_blocks.argtypes = [vp, vp, vp, vp, u32, u64, u32, u32, vp]
         L.slice_copy_blocks_series.argtypes = [vp, u32, u64, vp, vp, u64, u32, u64, i32, u32, u32, vp]
         for name in ("paged_build_tables", "paged_write_kv", "paged_decode_tables", "paged_decode_diff"):
-            getattr(L, name).argtypes = [C.c_char_p, vp]              # a packed argument struct, the stream
+            getattr(L, name).argtypes = [C.c_char_p, vp]              # an argument struct's bytes, the stream
         L.paged_decode_workspace.argtypes = [C.POINTER(PagedCacheDesc), u32, C.POINTER(u64)]
         L.slice_strerror.argtypes = [C.c_int]
         L.slice_strerror.restype = C.c_char_p
@@ -444,21 +443,36 @@ def slice_schedule_gll(slices) -> int:
 
 
 # -- device-driven path: torch tensors in, one launch per call ---------------------------------------
-# On a small batch the host's part of a call takes longer than the kernel: the checks read as little of a tensor as they
-# can and build their messages only when they fail, and the argument structs of the C ABI are packed in one go (ctypes
-# takes 2 us to convert 18 arguments one by one, 0.6 us this way).
+# On a small batch the host's part of a call takes longer than the kernel: tensors are checked, and the argument structs of
+# the C ABI filled in, by an extension module (csrc/torch_calls.cpp: 0.3 us a call, 3 to 5 us in Python). What does not fit is
+# a ValueError; what the C entry point refuses comes back as its code.
 
-_BUILD = _struct.Struct("=9Q4I")                       # paged_build_tables_t
-_WRITE = _struct.Struct("=7QI4x")                      # paged_write_kv_t
-_DECODE = _struct.Struct("=14Q4I3f4x")                 # paged_decode_t
+_calls = None
 
-_I32 = _I64 = _F32 = None                             # torch's dtypes, once a cache or a pool has been made
+
+def _torch_calls():
+    global _calls
+    if _calls is None:
+        L = lib()
+        import torch  # noqa: F401  (its libraries have to be there first)
+        try:
+            from . import _torch_calls as x
+        except ImportError as e:
+            raise RuntimeError("the _torch_calls extension is missing or was built for another torch: build it with "
+                               "paper_2609_27040_b200/build.py") from e
+        x.bind(*(C.cast(getattr(L, name), C.c_void_p).value
+                 for name in ("paged_build_tables", "paged_write_kv", "paged_decode_tables", "paged_decode_diff")))
+        _calls = x
+    return _calls
+
+
+_I32 = None                                           # torch's, once a cache or a pool has been made
 
 
 def _torch_types():
-    global _I32, _I64, _F32
+    global _I32
     import torch
-    _I32, _I64, _F32 = torch.int32, torch.int64, torch.float32
+    _I32 = torch.int32
     return {torch.bfloat16: 0, torch.float16: 1}
 
 
@@ -467,21 +481,11 @@ def _refuse(what: str):
 
 
 def _words(t, name: str, dev: int, dtype, shape=None) -> int:
-    """Address of a dense array of whole numbers (or f32) on device number `dev` (-1: host memory)."""
+    """Address of a dense array on device number `dev` (-1: host memory)."""
     if t.dtype is not dtype or t.get_device() != dev or not t.is_contiguous() or (shape is not None and t.shape != shape):
         _refuse(f"{name}: expected a contiguous {dtype} tensor on device {dev}" + (f" of shape {shape}" if shape is not None else "")
                 + f", got {tuple(t.shape)} of {t.dtype} on {t.device}")
     return t.data_ptr()
-
-
-def _row_stride(t, name: str, dev: int, dtype, n: int, rows: int, cols: int) -> int:
-    """Byte stride between the entries of an [n][rows][cols] tensor whose inner two dimensions are dense."""
-    if t.dtype is not dtype or t.get_device() != dev or t.shape != (n, rows, cols):
-        _refuse(f"{name}: expected [{n}][{rows}][{cols}] of {dtype} on device {dev}, got {tuple(t.shape)} of {t.dtype} on {t.device}")
-    s0, s1, s2 = t.stride()
-    if (s2 != 1 and cols > 1) or (s1 != cols and rows > 1):
-        _refuse(f"{name}: the inner two dimensions have to be contiguous, got strides {t.stride()}")
-    return (s0 if n > 1 else rows * cols) * 2
 
 
 class PagedCache:
@@ -532,34 +536,14 @@ class PagedPool:
         self._keep = (local_ids, lent_ids, free, free_out, work)
 
 
-def _table(t, n: int, dev: int):
-    """Address, entries from a row to the next, and width of the tables."""
-    shape, strides = t.shape, t.stride()
-    if len(shape) != 2 or t.dtype is not _I32 or t.get_device() != dev or shape[0] != n or (strides[1] != 1 and shape[1] > 1):
-        _refuse(f"tables: expected int32 [{n}][max_blocks] on device {dev}, rows contiguous, got {tuple(shape)} of {t.dtype} on {t.device}")
-    return t.data_ptr(), (strides[0] if n > 1 else shape[1]), shape[1]
-
-
-def _status(t, dev: int) -> int:
-    return 0 if t is None else _words(t, "status", dev, _I32, (1,))
-
-
 def paged_build_tables(pool: PagedPool, lens, new_lens, block_tokens: int, tables, offsets, slots, positions, status=None,
                        stream=None) -> int:
-    dev, n, room = pool._dev, lens.numel(), slots.numel()
-    tab, stride, width = _table(tables, n, dev)
-    args = _BUILD.pack(pool._addr, _words(lens, "lens", dev, _I32), _words(new_lens, "new_lens", dev, _I32, (n,)), tab, stride,
-                       _words(offsets, "offsets", dev, _I32, (n + 1,)), _words(slots, "slots", dev, _I64),
-                       _words(positions, "positions", dev, _I32, (room,)), _status(status, dev), n, block_tokens, width, room)
-    return (_lib or lib()).paged_build_tables(args, stream if stream is None or isinstance(stream, int) else stream.cuda_stream)
+    return (_calls or _torch_calls()).build(pool._addr, pool._dev, lens, new_lens, block_tokens, tables, offsets, slots, positions, status,
+                                            stream)
 
 
 def paged_write_kv(cache: PagedCache, k, v, slots, status=None, stream=None) -> int:
-    dev, n = cache._dev, slots.numel()
-    ks = _row_stride(k, "k", dev, cache.dtype, n, cache.num_kv_heads, cache.head_dim)
-    vs = _row_stride(v, "v", dev, cache.dtype, n, cache.num_kv_heads, cache.head_dim)
-    args = _WRITE.pack(cache._addr, k.data_ptr(), v.data_ptr(), ks, vs, _words(slots, "slots", dev, _I64), _status(status, dev), n)
-    return (_lib or lib()).paged_write_kv(args, stream if stream is None or isinstance(stream, int) else stream.cuda_stream)
+    return (_calls or _torch_calls()).write(cache._addr, cache._dev, k, v, slots, status, stream)
 
 
 def paged_decode_workspace(cache: PagedCache, num_q_rows: int) -> int:
@@ -572,38 +556,12 @@ def paged_decode_workspace(cache: PagedCache, num_q_rows: int) -> int:
     return int(out.value)
 
 
-def _workspace(work, dev: int):
-    if not work.is_contiguous() or work.get_device() != dev:
-        _refuse("workspace: a contiguous tensor on the cache's device")
-    return work.data_ptr(), work.nbytes
-
-
 def paged_decode_tables(cache: PagedCache, tables, lens, q, sm_scale: float, out, workspace, lse=None, window: int = 0, status=None,
                         stream=None) -> int:
-    dev, n, heads, d = cache._dev, lens.numel(), q.shape[1], cache.head_dim
-    if window < 0:
-        _refuse("a window is 0 (none) or more")
-    tab, stride, width = _table(tables, n, dev)
-    ws, wb = _workspace(workspace, dev)
-    args = _DECODE.pack(cache._addr, tab, stride, _words(lens, "lens", dev, _I32),
-                        q.data_ptr(), _row_stride(q, "q", dev, cache.dtype, n, heads, d),
-                        out.data_ptr(), _row_stride(out, "out", dev, cache.dtype, n, heads, d),
-                        0 if lse is None else _words(lse, "lse", dev, _F32, (n, heads)), 0, 0, ws, wb, _status(status, dev),
-                        n, width, heads, window, sm_scale, 0.0, 1.0)
-    return (_lib or lib()).paged_decode_tables(args, stream if stream is None or isinstance(stream, int) else stream.cuda_stream)
+    return (_calls or _torch_calls()).decode(cache._addr, cache._dev, tables, lens, q, sm_scale, out, workspace, window, status, stream, lse)
 
 
 def paged_decode_diff(cache: PagedCache, tables, lens, q, lam, sm_scale: float, out, workspace, norm_weight=None, eps: float = 1e-5,
                       out_scale: float = 1.0, window: int = 0, status=None, stream=None) -> int:
-    dev, n, heads, d = cache._dev, lens.numel(), out.shape[1], cache.head_dim
-    if window < 0:
-        _refuse("a window is 0 (none) or more")
-    tab, stride, width = _table(tables, n, dev)
-    ws, wb = _workspace(workspace, dev)
-    args = _DECODE.pack(cache._addr, tab, stride, _words(lens, "lens", dev, _I32),
-                        q.data_ptr(), _row_stride(q, "q", dev, cache.dtype, n, 2 * heads, d // 2),
-                        out.data_ptr(), _row_stride(out, "out", dev, cache.dtype, n, heads, d),
-                        0, _words(lam, "lam", dev, _F32, (heads,)),
-                        0 if norm_weight is None else _words(norm_weight, "norm_weight", dev, _F32, (d,)), ws, wb, _status(status, dev),
-                        n, width, heads, window, sm_scale, eps, out_scale)
-    return (_lib or lib()).paged_decode_diff(args, stream if stream is None or isinstance(stream, int) else stream.cuda_stream)
+    return (_calls or _torch_calls()).diff(cache._addr, cache._dev, tables, lens, q, sm_scale, out, workspace, window, status, stream, lam,
+                                           norm_weight, eps, out_scale)

@@ -1,9 +1,12 @@
-"""Builds libemaslice.so in-tree with nvcc for sm_100a (cross-compiles without a GPU)."""
+"""Builds in-tree: libemaslice.so with nvcc for sm_100a (cross-compiles without a GPU), and the extension module that fills in
+the device-driven calls' arguments from torch tensors, with the host compiler."""
 from __future__ import annotations
 
+import importlib.util
 import os
 import subprocess
 import sys
+import sysconfig
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
@@ -19,18 +22,43 @@ def _nvcc() -> str:
     return "nvcc"
 
 
-def needs_build() -> bool:
-    if not os.path.exists(LIB):
+TORCH_CALLS = os.path.join(HERE, "_torch_calls.so")
+TORCH_SOURCES = ["torch_calls.cpp"]
+
+
+def _older(product: str, sources) -> bool:
+    if not os.path.exists(product):
         return True
-    t = os.path.getmtime(LIB)
-    deps = [os.path.join(CSRC, f) for f in SOURCES + HEADERS] + [os.path.abspath(__file__)]
-    return any(os.path.getmtime(d) > t for d in deps)
+    t = os.path.getmtime(product)
+    return any(os.path.getmtime(d) > t for d in [os.path.join(CSRC, f) for f in sources] + [os.path.abspath(__file__)])
+
+
+def needs_build() -> bool:
+    return _older(LIB, SOURCES + HEADERS)
+
+
+def build_torch_calls(force: bool = False, verbose: bool = False) -> str:
+    if not force and not _older(TORCH_CALLS, TORCH_SOURCES + HEADERS[-1:]):
+        return TORCH_CALLS
+    torch = importlib.util.find_spec("torch").submodule_search_locations[0]
+    # nvcc's host compiler, with the C++ runtime that torch's libraries use (a compiler set to link its own in does not do).
+    cmd = ["g++", "-std=c++17", "-O2", "-fPIC", "-shared", "-Wall", "-I" + sysconfig.get_paths()["include"],
+           "-isystem", os.path.join(torch, "include"), "-isystem", os.path.join(torch, "include", "torch", "csrc", "api", "include")]
+    cmd += [os.path.join(CSRC, f) for f in TORCH_SOURCES]
+    cmd += ["-o", TORCH_CALLS, "-L" + os.path.join(torch, "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10"]
+    res = subprocess.run(cmd, capture_output=True, text=True)
+    if verbose or res.returncode != 0:
+        sys.stderr.write(res.stdout + res.stderr)
+    if res.returncode != 0:
+        raise RuntimeError("the host compiler failed building _torch_calls.so")
+    return TORCH_CALLS
 
 
 RESOURCES = os.path.join(HERE, "libemaslice.resources.txt")   # ptxas' report of the last build (git-ignored)
 
 
 def build(force: bool = False, verbose: bool = False) -> str:
+    build_torch_calls(force, verbose)
     if not force and not needs_build() and os.path.exists(RESOURCES):
         return LIB
     cmd = [_nvcc(), "-std=c++17", "-O3", "-lineinfo", "-gencode", "arch=compute_100a,code=sm_100a",

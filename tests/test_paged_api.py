@@ -71,11 +71,90 @@ def write(cache, **kw):
     return call("paged_write_kv", Write(**a))
 
 
-def test_packed_arguments_are_the_headers_structs():
-    for fmt, cls in ((B._BUILD, Build), (B._WRITE, Write), (B._DECODE, Decode)):
-        assert fmt.size == C.sizeof(cls)
-        values = [float(i) if t is F32 else i + 1 for i, (_, t) in enumerate(cls._fields_)]
-        assert fmt.pack(*values) == bytes(cls(*values))
+class Caught:
+    """Stands in for the library's entry points: keeps the structs that the binding hands over."""
+
+    def __enter__(self):
+        self.calls, self.refs = B._torch_calls(), []
+        for cls in (Build, Write, Decode, Decode):
+            def entry(args, stream, cls=cls):
+                self.args, self.stream = cls.from_buffer_copy(C.string_at(args, C.sizeof(cls))), stream
+                return 17
+            self.refs.append(C.CFUNCTYPE(C.c_int, VP, VP)(entry))
+        self.calls.bind(*(C.cast(f, VP).value for f in self.refs))
+        return self
+
+    def __exit__(self, *_):
+        B._calls = None                                            # bound to the library again by the next call
+
+
+def test_every_argument_reaches_its_field():
+    bf, i32, i64 = torch.bfloat16, torch.int32, torch.int64
+    arena = torch.zeros((4, 2, 32, 2, 64), dtype=bf)
+    c = B.PagedCache(arena)
+    ids, free, free_out, work = torch.zeros(9, dtype=i32), torch.zeros(2, dtype=i32), torch.zeros(2, dtype=i32), torch.zeros(1, dtype=i32)
+    pool = B.PagedPool(ids, None, free, free_out, work)
+    lens, new, offsets = (torch.zeros(x, dtype=i32) for x in (3, 3, 4))
+    tables = torch.zeros((3, 11), dtype=i32)[:, :7]
+    slots, positions, status = torch.zeros(5, dtype=i64), torch.zeros(5, dtype=i32), torch.zeros(1, dtype=i32)
+
+    class Stream:
+        cuda_stream = 0x7f0012345678
+
+    def fields(a):
+        return {name: getattr(a, name) for name, _ in a._fields_}
+
+    with Caught() as got:
+        assert B.paged_build_tables(pool, lens, new, 32, tables, offsets, slots, positions, status, stream=Stream()) == 17
+        assert fields(got.args) == dict(pool=C.addressof(pool.desc), lens=lens.data_ptr(), new=new.data_ptr(), tables=tables.data_ptr(), stride=11,
+                                        offsets=offsets.data_ptr(), slots=slots.data_ptr(), positions=positions.data_ptr(),
+                                        status=status.data_ptr(), n=3, T=32, width=7, tokens=5)
+        assert got.stream == Stream.cuda_stream
+        k, v = torch.zeros((5, 4, 64), dtype=bf)[:, :2], torch.zeros((5, 2, 64), dtype=bf)
+        assert B.paged_write_kv(c, k, v, slots) == 17
+        assert fields(got.args) == dict(cache=C.addressof(c.desc), k=k.data_ptr(), v=v.data_ptr(), ks=512, vs=256, slots=slots.data_ptr(), status=None,
+                                        ntok=5)
+        assert got.stream is None
+        q, out = torch.zeros((3, 9, 64), dtype=bf)[:, 1:7], torch.zeros((3, 6, 64), dtype=bf)
+        lse, ws, lam, weight = torch.zeros((3, 6)), torch.zeros(77), torch.zeros(6), torch.zeros(64)
+        assert B.paged_decode_tables(c, tables, lens, q, 0.25, out, ws, lse=lse, window=9, status=status, stream=5) == 17
+        common = dict(cache=C.addressof(c.desc), tables=tables.data_ptr(), table_stride=11, lens=lens.data_ptr(), out=out.data_ptr(), out_stride=768,
+                      work=ws.data_ptr(), work_bytes=308, nseq=3, max_blocks=7, heads=6)
+        assert fields(got.args) == dict(common, q=q.data_ptr(), q_stride=1152, lse=lse.data_ptr(), lam=None, norm=None, status=status.data_ptr(),
+                                        window=9, scale=0.25, eps=0.0, out_scale=1.0)
+        assert got.stream == 5
+        qd = torch.zeros((3, 12, 32), dtype=bf)
+        assert B.paged_decode_diff(c, tables, lens, qd, lam, -2, out, ws, norm_weight=weight, eps=0.5, out_scale=3, window=1) == 17
+        assert fields(got.args) == dict(common, q=qd.data_ptr(), q_stride=768, lse=None, lam=lam.data_ptr(), norm=weight.data_ptr(), status=None, window=1,
+                                        scale=-2.0, eps=0.5, out_scale=3.0)
+        # one sequence, none: strides of such dimensions mean nothing
+        one = torch.zeros((1, 6, 64), dtype=bf).as_strided((1, 6, 64), (8, 64, 1))
+        assert B.paged_decode_tables(c, tables[:1], lens[:1], one, 1.0, out[:1], ws) == 17
+        assert (got.args.q_stride, got.args.out_stride, got.args.table_stride, got.args.window, got.args.lse) == (768, 768, 7, 0, None)
+        assert B.paged_decode_tables(c, tables[:0], lens[:0], out[:0], 1.0, out[:0], ws) == 17 and got.args.nseq == 0
+
+
+def test_arguments_that_are_no_tensors_or_numbers():
+    bf, i64 = torch.bfloat16, torch.int64
+    c = B.PagedCache(torch.zeros((4, 2, 16, 2, 64), dtype=bf))
+    k, slots = torch.zeros((5, 2, 64), dtype=bf), torch.zeros(5, dtype=i64)
+    for a in ((None, k, slots), (k, 3, slots), (k, k, [1, 2]), (k, k, slots, 0), (k.to_sparse(), k, slots), (k.to("meta"), k, slots),
+              (k[0], k, slots)):
+        with pytest.raises(ValueError):
+            B.paged_write_kv(c, *a)
+    with pytest.raises((TypeError, AttributeError)):
+        B.paged_write_kv(c, k, k, slots, stream="main")
+    q, ws = torch.zeros((3, 4, 64), dtype=bf), torch.zeros(9)
+    tables, lens = torch.zeros((3, 5), dtype=torch.int32), torch.zeros(3, dtype=torch.int32)
+    with pytest.raises(TypeError):
+        B.paged_decode_tables(c, tables, lens, q, "1", q, ws)
+    for kw in (dict(window=-1), dict(window=1 << 40)):
+        with pytest.raises(ValueError):
+            B.paged_decode_tables(c, tables, lens, q, 1.0, q, ws, **kw)
+    with pytest.raises(TypeError):
+        B.paged_decode_tables(c, tables, lens, q, 1.0, q, ws, window=1.5)
+    with pytest.raises((ValueError, OverflowError)):
+        B.paged_decode_tables(c, tables, lens, q, 1.0, q, ws, window=1 << 70)
 
 
 def test_no_arguments_at_all():
