@@ -541,23 +541,29 @@ __device__ __forceinline__ uint32_t pieces_of(const Cut& c, uint32_t head) {
   return head < c.heads[0] ? c.pieces[0] : head < c.heads[1] ? c.pieces[1] : c.pieces[2];
 }
 
-// Short work of few items (fewer than two to a CTA) is dealt out evenly instead: of the line of all chunks, CTA k takes chunks k * size
-// and on, up to the next one's. A cut that would leave less than `snap` chunks of an item on one side of it is moved to
-// that end of the item.
+// Short work of few items (fewer than two to a CTA) is dealt out evenly instead. On the line of all chunks an item takes `least`
+// at least: a CTA is rather given one short item than several, each of which costs a round of its own (16 sequences of 1 to 600
+// tokens, 8 KV heads: 13.6 us against 16.3; one of 30 7.3 against 13.2). CTA k takes what lies from k * size on, up to the next
+// one's. A cut that would leave less than `least` chunks of an item on one side of it is moved to that end of the item.
 struct Even {
-  uint32_t size, snap;          // size 0: not dealt out
+  uint32_t size, least;         // size 0: not dealt out
 };
 
-// The item of chunks [at, at + chunks) of the line: it begins in CTA `owner`'s range, and goes on in that of the `cuts` next ones.
+__device__ __forceinline__ uint32_t room_of(uint32_t chunks, uint32_t least) { return chunks ? max(chunks, least) : 0; }
+
+// The item of `chunks` chunks that begins at `at` of the line: it begins in CTA `owner`'s range, and goes on in that of the `cuts` next ones.
 struct Share {
   uint32_t owner, cuts;
 };
 
 __device__ __forceinline__ Share share_of(const Even& even, unsigned long long at, uint32_t chunks) {
   Share r;
-  r.owner = static_cast<uint32_t>((at + min(even.snap, chunks) + even.size - 1) / even.size) - 1;
-  const uint32_t last = static_cast<uint32_t>((at + chunks - min(even.snap, chunks)) / even.size);  // the last cut that is not moved to the item's end
-  r.cuts = chunks >= 2 * even.snap && last > r.owner ? last - r.owner : 0;
+  r.owner = static_cast<uint32_t>((at + even.least + even.size - 1) / even.size) - 1;
+  r.cuts = 0;
+  if (chunks >= 2 * even.least) {
+    const uint32_t last = static_cast<uint32_t>((at + chunks - even.least) / even.size);  // the last cut that is not moved to the item's end
+    if (last > r.owner) r.cuts = last - r.owner;
+  }
   return r;
 }
 
@@ -611,6 +617,7 @@ __device__ void schedule(const PagedDecodeParams& p, Shared<D, NT>& sh, const Zo
     if (even.size) {
       const uint32_t me = blockIdx.x;
       const unsigned long long from = static_cast<unsigned long long>(me) * even.size;
+      unsigned long long start = 0;
       bool have = false;
       Share share{};
       while (!have) {
@@ -624,22 +631,23 @@ __device__ void schedule(const PagedDecodeParams& p, Shared<D, NT>& sh, const Zo
           at = sh.chunks_before[x];
           for (seq = x * run; seq < p.nseq; ++seq) {
             span = span_of<kTok>(p, seq);
-            const unsigned long long all = static_cast<unsigned long long>(span.chunks) * p.num_kv_heads;
+            const unsigned long long all = static_cast<unsigned long long>(room_of(span.chunks, even.least)) * p.num_kv_heads;
             if (from < at + all) break;
             at += all;
           }
-          if (seq < p.nseq) head = static_cast<uint32_t>((from - at) / span.chunks);
+          if (seq < p.nseq) head = static_cast<uint32_t>((from - at) / room_of(span.chunks, even.least));
           found = true;
         } else if (++head == p.num_kv_heads) {
           head = 0;
-          at += static_cast<unsigned long long>(span.chunks) * p.num_kv_heads;
+          at += static_cast<unsigned long long>(room_of(span.chunks, even.least)) * p.num_kv_heads;
           do {
             ++seq;
             if (seq < p.nseq) span = span_of<kTok>(p, seq);
           } while (seq < p.nseq && span.chunks == 0);
         }
         if (seq >= p.nseq) break;
-        share = share_of(even, at + static_cast<unsigned long long>(head) * span.chunks, span.chunks);
+        start = at + static_cast<unsigned long long>(head) * room_of(span.chunks, even.least);
+        share = share_of(even, start, span.chunks);
         if (share.owner > me) break;
         index = me - share.owner;
         have = index <= share.cuts;  // else its end was moved to where the range begins
@@ -651,7 +659,6 @@ __device__ void schedule(const PagedDecodeParams& p, Shared<D, NT>& sh, const Zo
         }
         return;
       }
-      const unsigned long long start = at + static_cast<unsigned long long>(head) * span.chunks;
       count = share.cuts + 1;
       a = index ? static_cast<uint32_t>(from - start) : 0;
       b = index < share.cuts ? static_cast<uint32_t>(from + even.size - start) : span.chunks;
@@ -1221,7 +1228,9 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) paged_decode_kernel
   const uint32_t run = (p.nseq + S::kThreads - 1) / S::kThreads;
   const uint32_t i0 = min(tid * run, p.nseq), i1 = min(i0 + run, p.nseq);
   unsigned long long mine = 0;
-  for (uint32_t i = i0; i < i1; ++i) mine += span_of<kTok>(p, i).chunks;
+  constexpr uint32_t kLeast = 2 * S::kWarps;  // at least two chunks for every warp: a join costs what three take
+  const bool few = static_cast<unsigned long long>(p.nseq) * p.num_kv_heads < 2 * gridDim.x;
+  for (uint32_t i = i0; i < i1; ++i) mine += room_of(span_of<kTok>(p, i).chunks, few ? kLeast : 1);
   mine *= p.num_kv_heads;
   unsigned long long inc = mine;
 #pragma unroll
@@ -1236,9 +1245,7 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) paged_decode_kernel
     if (x < warp) before += sh.warp_total[x];
     total += sh.warp_total[x];
   }
-  constexpr uint32_t kLeast = 2 * S::kWarps;  // at least two chunks for every warp: a join costs what three take
   const unsigned long long share = total / gridDim.x;  // of a CTA
-  const bool few = static_cast<unsigned long long>(p.nseq) * p.num_kv_heads < 2 * gridDim.x;
   Zones zones{};
   Even even{};
   uint32_t pieces = 0, most = 1, batch = 1;
@@ -1249,7 +1256,7 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) paged_decode_kernel
     // CTA's first piece's join is in its second one's way. One sequence of 20000 tokens, 8 KV heads: 28 us against 36 in two
     // pieces to a CTA; 16 of 3000 40 against 41.6; beyond, SMs that get less of HBM count for more: 5 of 100001 321 against 315.
     even.size = max(static_cast<uint32_t>((total + gridDim.x - 1) / gridDim.x), kLeast);
-    even.snap = kLeast;
+    even.least = kLeast;
     pieces = static_cast<uint32_t>((total + even.size - 1) / even.size);  // as many CTAs
   } else {
     zones.end[0] = share * gridDim.x * kPagedZone0 / 16;

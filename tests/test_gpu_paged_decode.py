@@ -639,3 +639,13 @@ def test_random_batches_of_few_items(seed):
     c = Case(lens, Hkv, G, D, T, [BF, HF][seed % 2], lent=0.25, seed=seed, diff=diff, stray=float("inf"))
     c.run()
     c.check()
+
+
+@pytest.mark.parametrize("Hkv,n", [(1, 250), (2, 147), (8, 18), (64, 4), (37, 3)])
+def test_short_items_on_ctas_of_their_own(Hkv, n):
+    rng = np.random.default_rng(n)
+    lens = [int(x) for x in rng.integers(0, 300, n)]
+    lens[n // 2] = 1600
+    c = Case(lens, Hkv, 1, 64, 16, HF, lent=0.2, seed=n, stray=float("nan"))
+    c.run()
+    c.check()
