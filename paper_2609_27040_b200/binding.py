@@ -508,6 +508,8 @@ class PagedCache:
                 _refuse("arenas: [blocks][2][block_tokens][num_kv_heads][head_dim], bf16 or fp16, alike in both")
             if not t[0].is_contiguous():
                 _refuse("arenas: blocks have to be dense")
+            if t.shape[0] > 1 and t.stride(0) < t[0].numel():  # expanded along its blocks (stride 0, the descriptor's "dense"), or overlapping
+                _refuse(f"arenas: blocks have to lie apart, got a first stride of {t.stride(0)} for blocks of {t[0].numel()} elements")
             d.blocks[j], d.base[j] = t.shape[0], t.data_ptr()
             d.block_stride[j] = t.stride(0) * 2 if t.shape[0] > 1 else 0
         d.dtype, d.block_tokens, d.num_kv_heads, d.head_dim = kinds[ref.dtype], ref.shape[2], ref.shape[3], ref.shape[4]

@@ -291,3 +291,19 @@ def test_memory_that_no_gpu_can_reach_is_refused():
     i32 = torch.int32
     assert B.paged_decode_tables(c, torch.zeros((3, 5), dtype=i32), torch.zeros(3, dtype=i32), q, 1.0, q.clone(),
                                  torch.zeros(B.paged_decode_workspace(c, 4), dtype=torch.uint8)) in (B.EINVAL, B.ECUDA)
+
+
+def test_arenas_whose_blocks_share_memory_are_refused():
+    """A first stride of 0 would be the descriptor's "dense": blocks far behind the tensor. Smaller than a block: blocks over one another."""
+    one = torch.zeros((1, 2, 16, 2, 64), dtype=torch.bfloat16)
+    size = one.numel()
+    flat = torch.zeros(4 * size, dtype=torch.bfloat16)
+    for bad in (one.expand(64, -1, -1, -1, -1), flat.as_strided((3, 2, 16, 2, 64), (size - 8,) + one.stride()[1:]),
+                flat.as_strided((3, 2, 16, 2, 64), (8,) + one.stride()[1:])):
+        assert bad[0].is_contiguous()
+        with pytest.raises(ValueError):
+            B.PagedCache(bad)
+        with pytest.raises(ValueError):
+            B.PagedCache(one, bad)
+    c = B.PagedCache(one.expand(1, -1, -1, -1, -1), flat.as_strided((3, 2, 16, 2, 64), (size + 8,) + one.stride()[1:]))
+    assert list(c.desc.blocks) == [1, 3] and list(c.desc.block_stride) == [0, 2 * (size + 8)]
