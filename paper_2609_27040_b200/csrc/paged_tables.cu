@@ -390,8 +390,8 @@ __global__ void __launch_bounds__(kWriteThreads) write_kv_kernel(const WriteKvPa
         const uint32_t u = u0 + i * lanes;
         if (dst[j] && u < p.units) {
           const uint64_t t = t0 + static_cast<uint64_t>(j) * groups;
-          k[j][i] = ptx::ld_stream_v4(p.k + t * p.k_stride + u * 16);
-          v[j][i] = ptx::ld_stream_v4(p.v + t * p.v_stride + u * 16);
+          k[j][i] = ptx::ld_once_v4(p.k + t * p.k_stride + u * 16);
+          v[j][i] = ptx::ld_once_v4(p.v + t * p.v_stride + u * 16);
         }
       }
 #pragma unroll

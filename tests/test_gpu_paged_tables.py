@@ -256,3 +256,115 @@ def test_slots_outside_the_cache_are_skipped_and_reported():
     assert B.paged_write_kv(B.PagedCache(arenas[0]), k, k, gpu([~0, 5, NO_SLOT, 47], torch.int64), status) == B.OK   # no second arena
     torch.cuda.synchronize()
     assert int(status) == B.EINVAL and float(arenas[0].float().sum()) == 2 * 2 * 2 * 64
+
+
+def test_tables_and_rows_behind_slow_kernels_and_one_another():
+    """Every call waits for what comes before it, eager and captured: inputs are written by a long kernel or a copy right before the
+    call, or by a call that lets its successor start early (slots by the tables, rows by attention), and are overwritten right behind it."""
+    n, T, Hkv, D, width = 150, 16, 4, 128, 12
+    rng = np.random.default_rng(3)
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    old, new = rng.integers(0, 90, n), rng.integers(90, 180, n)
+    room = int((new - old).sum()) + 9
+    blocks = int((-(-new // T)).sum())
+    bf, i32 = torch.bfloat16, torch.int32
+    arena = torch.zeros((blocks + 5, 2, T, Hkv, D), dtype=bf, device="cuda")
+    cache = B.PagedCache(arena)
+    held = int((-(-old // T)).sum())
+    ids = rng.permutation(blocks + 5)
+    first = np.full((n, width), -1)
+    first[np.arange(width)[None] < (-(-old // T))[:, None]] = ids[:held]
+    first, spare = gpu(first.tolist()), gpu(ids[held:].tolist() + [0] * held)
+    olds, news, ks, vs = gpu(old.tolist()), gpu(new.tolist()), *(torch.randn((room, Hkv, D), device="cuda", generator=gen).to(bf) for _ in range(2))
+    qs = torch.randn((n, Hkv, D), device="cuda", generator=gen).to(bf)
+    lens, want = torch.zeros_like(olds), torch.zeros_like(news)
+    tables, stack, free, work, status = first.clone(), spare.clone(), gpu([0, 0]), gpu([0]), gpu([0])
+    pool = B.PagedPool(stack, None, free, free, work)
+    offsets, slots, positions = torch.zeros(n + 1, dtype=i32, device="cuda"), torch.zeros(room, dtype=torch.int64, device="cuda"), torch.zeros(room, dtype=i32, device="cuda")
+    k, v, q, out = torch.zeros_like(ks), torch.zeros_like(vs), torch.zeros_like(qs), torch.zeros_like(qs)
+    ws = torch.zeros(B.paged_decode_workspace(cache, Hkv), dtype=torch.uint8, device="cuda")
+    last = gpu([0], torch.int64).expand(n).contiguous()
+    big = torch.ones(100_000_000, device="cuda")                 # a kernel of some 0.1 ms on it
+    results = [torch.zeros_like(x) for x in (tables, slots, positions, offsets, free, arena, out, arena)]
+
+    def step():
+        s = torch.cuda.current_stream()
+        arena.zero_()
+        tables.copy_(first)
+        stack.copy_(spare)
+        lens.fill_(-1)                                           # what a call that came too soon would see: refused
+        want.fill_(-1)
+        slots.fill_(1 << 40)
+        free.copy_(torch_free)
+        big.mul_(1.0)
+        lens.copy_(olds)
+        want.copy_(news)
+        assert B.paged_build_tables(pool, lens, want, T, tables, offsets, slots, positions, status, s) == B.OK
+        lens.fill_(-1)
+        want.fill_(-1)
+        k.fill_(9.0)
+        v.fill_(9.0)
+        big.mul_(1.0)
+        k.copy_(ks)
+        v.copy_(vs)
+        assert B.paged_write_kv(cache, k, v, slots, status, s) == B.OK
+        k.fill_(9.0)
+        v.fill_(9.0)
+        for r, x in zip(results[:6], (tables, slots, positions, offsets, free, arena)):
+            r.copy_(x)
+        # tables, rows, attention and rows again, back to back: each reads what the one before it writes
+        arena.zero_()
+        tables.copy_(first)
+        free.copy_(torch_free)
+        lens.copy_(olds)
+        want.copy_(news)
+        k.copy_(ks)
+        v.copy_(vs)
+        q.copy_(qs)
+        assert B.paged_build_tables(pool, lens, want, T, tables, offsets, slots, positions, status, s) == B.OK
+        assert B.paged_write_kv(cache, k, v, slots, status, s) == B.OK
+        assert B.paged_decode_tables(cache, tables, want, q, 0.1, out, ws, status=status, stream=s) == B.OK
+        assert B.paged_write_kv(cache, out, out, last, status, s) == B.OK
+        results[6].copy_(out)
+        results[7].copy_(arena)
+        out.fill_(5.0)
+
+    torch_free = gpu([len(ids) - held, 0])
+    model = PoolModel(ids[held:].tolist(), [])
+    model.width = width
+    rows = [dict(enumerate(first[i, :ceil_div(int(old[i]), T)].tolist())) for i in range(n)]
+    st, o, sl, po = model.step(T, old.tolist(), new.tolist(), rows, room)
+    last.copy_(gpu([int(sl[o[i + 1] - 1]) for i in range(n)], torch.int64))   # each request's last token, distinct
+    main = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(main):
+        step()
+    torch.cuda.synchronize()
+    assert st == 0 and int(status) == 0
+    assert results[3].tolist() == o and results[1].tolist() == sl and results[2].tolist() == po and results[4].tolist() == [len(model.stacks[0]), 0]
+    at = np.array(sl[:o[n]])
+    place = torch.from_numpy(np.stack([stored_place(r, Hkv * D) for r in range(T)])).cuda()
+
+    def rows_at(x, where):
+        where = torch.from_numpy(np.asarray(where)).cuda()
+        return x[where // T, :, where % T].reshape(-1, 2, Hkv * D).gather(2, place[where % T][:, None].expand(-1, 2, -1)).reshape(-1, 2, Hkv, D)
+
+    for j, x in enumerate((ks, vs)):
+        assert torch.equal(rows_at(results[5], at)[:, j], x[:o[n]])
+        assert torch.equal(rows_at(results[7], last.cpu().numpy())[:, j], results[6])
+    assert results[6].any()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=main):
+        step()
+    good = [r.clone() for r in results]
+    for rep in range(6):
+        for r in results:
+            r.fill_(3)
+        torch.cuda.synchronize()
+        if rep % 2:
+            with torch.cuda.stream(main):
+                step()
+        else:
+            graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(results, good)) and int(status) == 0 and int(work) == 0

@@ -307,3 +307,21 @@ def test_arenas_whose_blocks_share_memory_are_refused():
             B.PagedCache(one, bad)
     c = B.PagedCache(one.expand(1, -1, -1, -1, -1), flat.as_strided((3, 2, 16, 2, 64), (size + 8,) + one.stride()[1:]))
     assert list(c.desc.blocks) == [1, 3] and list(c.desc.block_stride) == [0, 2 * (size + 8)]
+
+
+def test_kernels_that_start_early_read_through_coherent_loads():
+    """A kernel launched with programmatic serialisation is there while its inputs are still being written: loads of the read-only path
+    (ld.global.nc, __ldg) are for data that does not change as long as the kernel lives."""
+    import os
+    import re
+    with open(os.path.join(build_mod.CSRC, "ptx.cuh")) as f:
+        wrappers = set(re.findall(r"__forceinline__ \w+ (\w+)\([^{]*\{[^}]*ld\.global\.nc", f.read()))
+    assert "ld_stream_v4" in wrappers
+    seen = 0
+    for name in os.listdir(build_mod.CSRC):
+        with open(os.path.join(build_mod.CSRC, name)) as f:
+            text = f.read()
+        if "launch_early(" in text and name.endswith(".cu"):
+            seen += 1
+            assert not re.search(r"ld\.global\.nc|__ldg\(|\b(%s)\(" % "|".join(wrappers), text), name
+    assert seen == 2
