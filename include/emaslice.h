@@ -623,7 +623,7 @@ int paged_write_kv(const paged_write_kv_t* args, void* stream);
 
 /* Bytes of workspace that the two calls below need for num_q_rows query rows per sequence (num_heads, or twice
  * that for the differential form), independent of batch and lengths. Before its first use the
- * workspace's first 32768 bytes must be 0; every call leaves them 0 (one that ended with SLICE_ETIMEOUT may not: clear them again). */
+ * workspace's first 32768 bytes must be 0; every call leaves them 0, whatever its status. */
 int paged_decode_workspace(const paged_cache_t* cache, uint32_t num_q_rows, uint64_t* out_bytes);
 
 /* Attention of one new token per sequence: for query head h (KV head h / G, G = num_heads / num_kv_heads in 1..16)
@@ -634,7 +634,8 @@ int paged_decode_workspace(const paged_cache_t* cache, uint32_t num_q_rows, uint
  * A sequence of length 0 gets zeros and minus infinity. What block tails hold does not matter; the rows of V that are
  * attended to must be finite. Arithmetic: 16-bit products, f32 accumulation and softmax, result rounded once.
  * The result does not depend on timing. Status: EINVAL (length below 0 or above max_blocks * block_tokens: zeros, like
- * an empty sequence; an entry outside its arena: reads as zeros, the row is not meaningful).
+ * an empty sequence; an entry outside its arena: reads as zeros, the row is not meaningful; lengths seen to change during the call: no row of it
+ * is), ETIMEOUT (a copy or a warp did not come within seconds: rows are missing).
  * Returns EINVAL, ESCRATCH (workspace too small), ECUDA. */
 int paged_decode_tables(const paged_decode_t* args, void* stream);
 

@@ -285,10 +285,12 @@ constexpr uint32_t kPagedZone0 = 7, kPagedZone1 = 12, kPagedCut0 = 2, kPagedCut1
 // items that begin in the first zone may reach to the end, and so on.
 constexpr uint32_t kPagedMaxParts = kPagedMaxCtas * kPagedCut2;
 constexpr uint32_t kPagedFan = 32;              // most pieces that are added at a time, and twice the other number
-// Words at the start of the workspace, zero before and after: ticket counter, CTAs done, arrivals at every level of the
+// Words at the start of the workspace, zero before and after: ticket counter, CTAs done (two words: their number in the lowest 8
+// bits, above them arrivals that no complete group accounts for), arrivals at every level of the
 // trees in which the pieces of cut items meet (for two groups of columns, three levels: 16^3 >= kPagedMaxParts).
-constexpr uint32_t kPagedTicket = 0, kPagedDone = 1, kPagedTree = 32;
+constexpr uint32_t kPagedTicket = 0, kPagedDone = 2, kPagedTree = 32;
 constexpr uint32_t kPagedCounterBytes = 32768;
+static_assert(kPagedMaxCtas < 256, "CTAs done");
 static_assert((kPagedTree + 2 * 3 * kPagedMaxParts) * 4 <= kPagedCounterBytes, "counters");
 static_assert(kPagedFan / 2 * (kPagedFan / 2) * (kPagedFan / 2) >= kPagedMaxParts, "levels");
 struct PagedDecodeParams {

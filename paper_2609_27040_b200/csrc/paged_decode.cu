@@ -116,6 +116,7 @@ struct __align__(128) Shared {
   uint32_t idle[NT];
   uint32_t started;                // chunks of the CTA's pieces that copies have been started of
   uint32_t dead;                   // a bounded wait ran out: no further waiting
+  int32_t open[NT];                // the mergers' arrivals, less the sizes of the groups that they found complete
   uint32_t warp_sum[S::kThreads / 32][2];
   unsigned long long warp_total[S::kThreads / 32];
   uint32_t pieces_before[S::kThreads], parts_before[S::kThreads];  // before the threads' runs of sequences
@@ -703,6 +704,7 @@ __device__ void schedule(const PagedDecodeParams& p, Shared<D, NT>& sh, const Zo
       }
       if (seq == p.nseq) {  // only if the lengths have changed since they were added up: no more is read
         if (lane == 0) {
+          ptx::report_status(p.status, kStatusInvalid);
           note.chunks = 0;
           arrive(&sh.note_full[j % kNotes]);
         }
@@ -734,6 +736,7 @@ __device__ void schedule(const PagedDecodeParams& p, Shared<D, NT>& sh, const Zo
         } while (span.chunks == 0);  // there is one: the ticket exists
         if (seq == p.nseq) {
           if (lane == 0) {
+            ptx::report_status(p.status, kStatusInvalid);
             note.chunks = 0;
             arrive(&sh.note_full[j % kNotes]);
           }
@@ -750,7 +753,7 @@ __device__ void schedule(const PagedDecodeParams& p, Shared<D, NT>& sh, const Zo
     ++ticket;
     --left;
     }
-    if (count > 1 && slot + count * step > kPagedMaxParts) {  // as above: never with lengths that stay as they are
+    if (count > 1 && (slot > kPagedMaxParts || count > (kPagedMaxParts - slot) / step)) {  // as above: never with lengths that stay as they are
       if (lane == 0) {
         ptx::report_status(p.status, kStatusInvalid);
         note.chunks = 0;
@@ -1140,7 +1143,9 @@ __device__ void merge(const PagedDecodeParams& p, Shared<D, NT>& sh, uint32_t gr
       uint32_t arrived = 0;
       if (lane == 0) {
         arrived = atomicAdd(counter, 1u);
-        if (arrived == n - 1) *counter = 0;
+        const bool complete = arrived == n - 1;
+        if (complete) *counter = 0;
+        sh.open[group] += complete ? 1 - static_cast<int32_t>(n) : 1;
       }
       arrived = __shfl_sync(0xffffffffu, arrived, 0);
       if (arrived != n - 1) {
@@ -1215,6 +1220,7 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) paged_decode_kernel
       ptx::mbar_init(ptx::smem_u32(&sh.job_full[g]), 1);
       ptx::mbar_init(ptx::smem_u32(&sh.job_done[g]), S::kWarps);
       sh.idle[g] = 0;
+      sh.open[g] = 0;
     }
     ptx::fence_barrier_init();
     asm volatile("prefetch.tensormap [%0];" ::"l"(&maps.m[0]));
@@ -1333,10 +1339,23 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) paged_decode_kernel
     if (tid == 0 && (n < 0 || static_cast<uint32_t>(n) > p.max_blocks * p.block_tokens)) ptx::report_status(p.status, kStatusInvalid);
   }
 
+  // The CTA that is done last resets the ticket and done words: every CTA has drawn its last ticket and made its last arrival (each
+  // got the word's old value back before it came here). The words of the trees are 0 again if every group was complete, which is
+  // when arrivals and complete groups balance over all CTAs; if not (a wait ran out, or lengths changed under the call and CTAs did
+  // not cut the work alike), all are cleared. (Always clearing them: one sequence of 500 10.8 -> 11.1 us.)
   __syncthreads();
-  if (tid == 0 && atomicAdd(p.counters + kPagedDone, 1u) == gridDim.x - 1) {  // every CTA has drawn its last ticket
-    p.counters[kPagedTicket] = 0;
-    p.counters[kPagedDone] = 0;
+  if (tid == 0) {
+    long long open = 0;
+    for (uint32_t g = 0; g < NT; ++g) open += sh.open[g];
+    const unsigned long long mine = 1 + (static_cast<unsigned long long>(open) << 8);
+    auto* done = reinterpret_cast<unsigned long long*>(p.counters + kPagedDone);
+    const unsigned long long all = atomicAdd(done, mine) + mine;
+    if ((all & 255u) == gridDim.x) {
+      p.counters[kPagedTicket] = 0;
+      *done = 0;
+      if (all != gridDim.x)
+        for (uint32_t x = kPagedTree; x < kPagedTree + NT * 3 * kPagedMaxParts; ++x) p.counters[x] = 0;
+    }
   }
 }
 

@@ -649,3 +649,32 @@ def test_short_items_on_ctas_of_their_own(Hkv, n):
     c = Case(lens, Hkv, 1, 64, 16, HF, lent=0.2, seed=n, stray=float("nan"))
     c.run()
     c.check()
+
+
+@pytest.mark.parametrize("lens,Hkv", [([3000] * 5, 4), ([4000] * 60 + [100, 0, 3900], 8), ([300000, 200000], 4)], ids=str)
+def test_a_workspace_is_whole_again_after_lengths_that_changed_under_a_call(lens, Hkv):
+    """What such a call answers means nothing (its CTAs may have cut the work differently), but every access stays in bounds, every
+    wait ends, and the next call is right. The lengths change around the time at which the CTAs read them."""
+    n = len(lens)
+    c = Case(lens, Hkv, 1, 128, 16, BF, seed=n)
+    c.run()
+    good = c.out[:n].clone(), c.lse[:n].clone()
+    then = gpu([x // 2 + x // 5 * (i % 3) for i, x in enumerate(lens)])
+    lens_t, side = c.lens_t.clone(), torch.cuda.Stream()
+    hit = 0
+    for k in range(300):
+        c.lens_t.copy_(lens_t)
+        torch.cuda.synchronize()
+        with torch.cuda.stream(side):
+            torch.cuda._sleep(k * 240)                           # 0 to some 40 us
+            c.lens_t.copy_(then)
+        assert B.paged_decode_tables(c.cache, c.tables, c.lens_t, c.q, c.scale, c.out[:n], c.work, lse=c.lse[:n], status=c.status) == B.OK
+        torch.cuda.synchronize()
+        assert int(c.status) in (0, B.EINVAL)
+        hit += not torch.equal(c.out[:n], good[0])
+        c.status.zero_()
+        assert not c.work[:32768].any(), k
+        c.lens_t.copy_(lens_t)
+        c.run()
+        assert torch.equal(c.out[:n], good[0]) and torch.equal(c.lse[:n], good[1])
+    assert hit                                                   # the lengths did change before or under some of the calls
