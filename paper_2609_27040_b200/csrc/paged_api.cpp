@@ -30,25 +30,29 @@ bool cache_ok(const paged_cache_t* c, uint64_t (&stride)[2]) {
   return true;
 }
 
+// A failure's code. The runtime keeps it until it is asked for, and the library's other launches would report it as theirs.
+int failed(int code) {
+  cudaGetLastError();
+  return code;
+}
+
 // The call's memory has to be reachable from the current device: memory of another one is refused.
 int device_ok(const void* p, int* sms, int* device = nullptr) {
   static int sms_of[64] = {};
   int dev = 0;
-  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return SLICE_ECUDA;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return failed(SLICE_ECUDA);
   cudaPointerAttributes at{};
-  if (cudaPointerGetAttributes(&at, p) != cudaSuccess) {
-    cudaGetLastError();
-    return SLICE_EINVAL;
-  }
+  if (cudaPointerGetAttributes(&at, p) != cudaSuccess) return failed(SLICE_EINVAL);
   if (at.type == cudaMemoryTypeDevice && at.device != dev) return SLICE_EINVAL;
   if (at.type == cudaMemoryTypeUnregistered) return SLICE_EINVAL;
-  if (!sms_of[dev] && cudaDeviceGetAttribute(&sms_of[dev], cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) return SLICE_ECUDA;
+  if (!sms_of[dev] && cudaDeviceGetAttribute(&sms_of[dev], cudaDevAttrMultiProcessorCount, dev) != cudaSuccess)
+    return failed(SLICE_ECUDA);
   *sms = sms_of[dev];
   if (device) *device = dev;
   return SLICE_OK;
 }
 
-int launched(cudaError_t e) { return e == cudaSuccess ? SLICE_OK : SLICE_ECUDA; }
+int launched(cudaError_t e) { return e == cudaSuccess ? SLICE_OK : failed(SLICE_ECUDA); }
 
 int decode(const paged_decode_t* a, bool diff, void* stream) {
   if (!a) return SLICE_EINVAL;

@@ -368,3 +368,44 @@ def test_tables_and_rows_behind_slow_kernels_and_one_another():
             graph.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(results, good)) and int(status) == 0 and int(work) == 0
+
+
+def test_a_call_that_could_not_be_launched_leaves_no_error_to_the_next_one():
+    """A stream whose capture has become invalid takes no launch: the call says so, and what the library launches next does not."""
+    import ctypes as C
+    arena = torch.zeros((3, 2, 16, 2, 64), dtype=torch.bfloat16, device="cuda")
+    cache, k, slots = B.PagedCache(arena), torch.ones((1, 2, 64), dtype=torch.bfloat16, device="cuda"), gpu([5], torch.int64)
+    tables, lens, q = gpu([[0, 1, 2]]), gpu([20]), torch.ones((1, 2, 64), dtype=torch.bfloat16, device="cuda")
+    ws, out = torch.zeros(B.paged_decode_workspace(cache, 4), dtype=torch.uint8, device="cuda"), torch.zeros_like(q)
+    b = Bench(1, 16, 4, 3, 0, 1)
+    args = (gpu([0]), gpu([17]), 16, b.tables, gpu([0, 0]), torch.zeros(17, dtype=torch.int64, device="cuda"), gpu([0] * 17))
+    src, dst = torch.arange(64, dtype=torch.int32, device="cuda"), torch.zeros(64, dtype=torch.int32, device="cuda")
+    torch.cuda.synchronize()
+    driver, stream = C.CDLL("libcuda.so.1"), C.c_void_p()
+
+    def calls(s):
+        yield B.paged_write_kv(cache, k, k, slots, stream=s)
+        yield B.paged_decode_tables(cache, tables, lens, q, 0.1, out, ws, stream=s)
+        yield B.paged_decode_diff(cache, tables, lens, q.view(1, 4, 32), torch.ones(2, device="cuda"), 0.1, out, ws, stream=s)
+        yield B.paged_build_tables(b.pool(), *args, stream=s)
+
+    assert driver.cuStreamCreate(C.byref(stream), 1) == 0
+    try:
+        for which in range(4):
+            assert driver.cuStreamBeginCapture_v2(stream, 2) == 0
+            assert driver.cuStreamSynchronize(stream) != 0       # not allowed there: the capture is invalid
+            for i, rc in enumerate(calls(stream.value)):
+                if i == which:
+                    assert rc == B.ECUDA
+                    break
+            graph = C.c_void_p()
+            assert driver.cuStreamEndCapture(stream, C.byref(graph)) != 0
+            dst.zero_()
+            torch.cuda.synchronize()
+            assert B.lib().slice_copy_blocks(dst.data_ptr(), None, src.data_ptr(), None, 1, 256, 1, 1, None) == B.OK
+            torch.cuda.synchronize()
+            assert torch.equal(src, dst)
+    finally:
+        driver.cuStreamDestroy_v2(stream)
+    assert [rc for rc in calls(None)] == [B.OK] * 4
+    torch.cuda.synchronize()
