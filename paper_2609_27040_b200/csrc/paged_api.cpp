@@ -3,6 +3,8 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include <atomic>
+
 #include "../../include/emaslice.h"
 #include "kernels.h"
 
@@ -38,16 +40,18 @@ int failed(int code) {
 
 // The call's memory has to be reachable from the current device: memory of another one is refused.
 int device_ok(const void* p, int* sms, int* device = nullptr) {
-  static int sms_of[64] = {};
+  static std::atomic<int> sms_of[64] = {};  // several threads may call at a time
   int dev = 0;
   if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return failed(SLICE_ECUDA);
   cudaPointerAttributes at{};
   if (cudaPointerGetAttributes(&at, p) != cudaSuccess) return failed(SLICE_EINVAL);
   if (at.type == cudaMemoryTypeDevice && at.device != dev) return SLICE_EINVAL;
   if (at.type == cudaMemoryTypeUnregistered) return SLICE_EINVAL;
-  if (!sms_of[dev] && cudaDeviceGetAttribute(&sms_of[dev], cudaDevAttrMultiProcessorCount, dev) != cudaSuccess)
-    return failed(SLICE_ECUDA);
-  *sms = sms_of[dev];
+  *sms = sms_of[dev].load(std::memory_order_relaxed);
+  if (!*sms) {
+    if (cudaDeviceGetAttribute(sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) return failed(SLICE_ECUDA);
+    sms_of[dev].store(*sms, std::memory_order_relaxed);
+  }
   if (device) *device = dev;
   return SLICE_OK;
 }

@@ -35,6 +35,8 @@
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
+#include <atomic>
+
 #include "kernels.h"
 #include "ptx.cuh"
 
@@ -1379,11 +1381,11 @@ template <uint32_t D, uint32_t NT, bool kBf16>
 cudaError_t launch(const PagedDecodeParams& p, const Maps& maps, uint32_t grid, int dev, cudaStream_t stream) {
   constexpr size_t kSharedBytes = sizeof(Shared<D, NT>) + 128;
   static_assert(kSharedBytes <= 232448, "one CTA per SM");
-  static bool ready[64] = {};  // the attribute is a property of the function on one device
-  if (!ready[dev]) {
+  static std::atomic<bool> ready[64] = {};  // the attribute is a property of the function on one device; several threads may launch
+  if (!ready[dev].load(std::memory_order_acquire)) {
     const cudaError_t e = cudaFuncSetAttribute(paged_decode_kernel<D, NT, kBf16>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(kSharedBytes));
     if (e != cudaSuccess) return e;
-    ready[dev] = true;
+    ready[dev].store(true, std::memory_order_release);
   }
   return launch_early(paged_decode_kernel<D, NT, kBf16>, grid, Shape<D, NT>::kThreads, kSharedBytes, stream, p, maps);
 }
