@@ -1423,9 +1423,18 @@ cudaError_t launch_paged_decode(const PagedDecodeParams& p, int dev, int num_sms
     const cuuint64_t strides[2] = {dims[0] * 2, p.block_stride[a]};
     const cuuint32_t box[3] = {p.head_dim, box_rows, 1};
     const cuuint32_t elem[3] = {1, 1, 1};
-    if (encode(&maps.m[j], CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, p.base[a], dims, strides, box, elem, CU_TENSOR_MAP_INTERLEAVE_NONE,
-               CU_TENSOR_MAP_SWIZZLE_NONE, promotion, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
-      return cudaErrorInvalidValue;
+    auto make = [&] {
+      return encode(&maps.m[j], CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, p.base[a], dims, strides, box, elem, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                    CU_TENSOR_MAP_SWIZZLE_NONE, promotion, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    };
+    CUresult r = make();
+    // A thread that has not used the GPU yet: the runtime would make its device's context current at the launch, the driver's call needs it now.
+    if (r == CUDA_ERROR_INVALID_CONTEXT || r == CUDA_ERROR_NOT_INITIALIZED) {
+      const cudaError_t e = cudaSetDevice(dev);
+      if (e != cudaSuccess) return e;
+      r = make();
+    }
+    if (r != CUDA_SUCCESS) return cudaErrorInvalidValue;
   }
   const uint32_t sms = static_cast<uint32_t>(num_sms);
   const uint32_t grid = sms < kPagedMaxCtas ? sms : kPagedMaxCtas;

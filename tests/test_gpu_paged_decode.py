@@ -678,3 +678,60 @@ def test_a_workspace_is_whole_again_after_lengths_that_changed_under_a_call(lens
         c.run()
         assert torch.equal(c.out[:n], good[0]) and torch.equal(c.lse[:n], good[1])
     assert hit                                                   # the lengths did change before or under some of the calls
+
+
+FIRST_CALLS_OF_THREADS = """
+import threading, torch
+from tests.test_gpu_paged_decode import B, BF, Case
+cases = [Case([900, 33, 0, 700], 2, 3, 128, 16, BF, lent=0.4, seed=k % 2, diff=k % 4 >= 2) for k in range(8)]
+streams = [torch.cuda.Stream() for _ in cases]
+gate = threading.Barrier(len(cases))
+torch.cuda.synchronize()
+codes = []
+def call(c, s):
+    gate.wait()
+    for _ in range(20):
+        if c.diff:
+            codes.append(B.paged_decode_diff(c.cache, c.tables, c.lens_t, c.q, c.lam, c.scale, c.out[:4], c.work, status=c.status, stream=s))
+        else:
+            codes.append(B.paged_decode_tables(c.cache, c.tables, c.lens_t, c.q, c.scale, c.out[:4], c.work, status=c.status, stream=s))
+threads = [threading.Thread(target=call, args=x) for x in zip(cases, streams)]
+[t.start() for t in threads]
+[t.join() for t in threads]
+torch.cuda.synchronize()
+assert codes == [B.OK] * (20 * len(cases))
+for k, c in enumerate(cases):
+    assert torch.equal(c.out[:4], cases[k % 4].out[:4]) and c.out[:2].any() and int(c.status) == 0
+print("the same")
+"""
+
+
+def test_the_first_calls_of_several_threads():
+    import subprocess
+    import sys
+    r = subprocess.run([sys.executable, "-c", FIRST_CALLS_OF_THREADS], capture_output=True, text=True, timeout=300)
+    assert r.returncode == 0 and "the same" in r.stdout, r.stderr[-2000:]
+
+
+@pytest.mark.parametrize("diff", [False, True], ids=["plain", "diff"])
+def test_a_thread_whose_first_use_of_the_gpu_is_the_call(diff):
+    import threading
+    c = Case([900, 33, 0, 700], 2, 3, 128, 16, BF, lent=0.4, seed=1, diff=diff)
+    c.run(norm=False)
+    want = c.out[:4].clone()
+    c.out.fill_(7.0)
+    torch.cuda.synchronize()
+    codes = []
+
+    def call():
+        for _ in range(2):
+            if diff:
+                codes.append(B.paged_decode_diff(c.cache, c.tables, c.lens_t, c.q, c.lam, c.scale, c.out[:4], c.work, out_scale=c.out_scale, status=c.status))
+            else:
+                codes.append(B.paged_decode_tables(c.cache, c.tables, c.lens_t, c.q, c.scale, c.out[:4], c.work, status=c.status))
+
+    t = threading.Thread(target=call)
+    t.start()
+    t.join()
+    torch.cuda.synchronize()
+    assert codes == [B.OK, B.OK] and torch.equal(c.out[:4], want) and int(c.status) == 0
