@@ -455,11 +455,15 @@ def _torch_calls():
     if _calls is None:
         L = lib()
         import torch  # noqa: F401  (its libraries have to be there first)
+        from . import build
+        built, wanted = build.torch_calls_built_for(), build.torch_calls_wanted()
+        if built != wanted:                           # its classes are laid out as that torch has them: not to be tried with another one
+            raise RuntimeError(f"the _torch_calls extension was built for {built or 'nothing yet'}, this is {wanted}: build it with "
+                               "paper_2609_27040_b200/build.py")
         try:
             from . import _torch_calls as x
         except ImportError as e:
-            raise RuntimeError("the _torch_calls extension is missing or was built for another torch: build it with "
-                               "paper_2609_27040_b200/build.py") from e
+            raise RuntimeError("the _torch_calls extension cannot be loaded: build it with paper_2609_27040_b200/build.py") from e
         x.bind(*(C.cast(getattr(L, name), C.c_void_p).value
                  for name in ("paged_build_tables", "paged_write_kv", "paged_decode_tables", "paged_decode_diff")))
         _calls = x

@@ -1,9 +1,10 @@
 """Builds in-tree: libemaslice.so with nvcc for sm_100a (cross-compiles without a GPU), and the extension module that fills in
-the device-driven calls' arguments from torch tensors, with the host compiler."""
+the device-driven calls' arguments from torch tensors, with the host compiler. The library needs neither torch nor the extension."""
 from __future__ import annotations
 
 import importlib.util
 import os
+import re
 import subprocess
 import sys
 import sysconfig
@@ -23,6 +24,7 @@ def _nvcc() -> str:
 
 
 TORCH_CALLS = os.path.join(HERE, "_torch_calls.so")
+TORCH_CALLS_FOR = os.path.join(HERE, "_torch_calls.for.txt")   # the Python and the torch it was built for (git-ignored)
 TORCH_SOURCES = ["torch_calls.cpp"]
 
 
@@ -37,28 +39,58 @@ def needs_build() -> bool:
     return _older(LIB, SOURCES + HEADERS)
 
 
+def _torch_dir():
+    """Where torch is installed (it is not imported), or None."""
+    spec = importlib.util.find_spec("torch")
+    return spec.submodule_search_locations[0] if spec and spec.submodule_search_locations else None
+
+
+def torch_calls_wanted() -> str:
+    """The Python and the torch that the extension has to be built for here."""
+    with open(os.path.join(_torch_dir(), "version.py")) as f:
+        version = re.search(r"__version__ = '([^']+)'", f.read())
+    return f"{sysconfig.get_config_var('SOABI')} torch {version.group(1) if version else 'unknown'}"
+
+
+def torch_calls_built_for() -> str:
+    """And those that it was built for; empty if that is not known."""
+    if not os.path.exists(TORCH_CALLS_FOR):
+        return ""
+    with open(TORCH_CALLS_FOR) as f:
+        return f.read().strip()
+
+
 def build_torch_calls(force: bool = False, verbose: bool = False) -> str:
-    if not force and not _older(TORCH_CALLS, TORCH_SOURCES + HEADERS[-1:]):
+    torch = _torch_dir()
+    if torch is None:
+        raise RuntimeError("torch is not installed: the device-driven calls on tensors need it (the library itself does not)")
+    wanted = torch_calls_wanted()
+    if not force and not _older(TORCH_CALLS, TORCH_SOURCES + HEADERS[-1:]) and torch_calls_built_for() == wanted:
         return TORCH_CALLS
-    torch = importlib.util.find_spec("torch").submodule_search_locations[0]
     # nvcc's host compiler, with the C++ runtime that torch's libraries use (a compiler set to link its own in does not do).
     cmd = ["g++", "-std=c++17", "-O2", "-fPIC", "-shared", "-Wall", "-I" + sysconfig.get_paths()["include"],
            "-isystem", os.path.join(torch, "include"), "-isystem", os.path.join(torch, "include", "torch", "csrc", "api", "include")]
     cmd += [os.path.join(CSRC, f) for f in TORCH_SOURCES]
     cmd += ["-o", TORCH_CALLS, "-L" + os.path.join(torch, "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10"]
-    res = subprocess.run(cmd, capture_output=True, text=True)
+    if os.path.exists(TORCH_CALLS_FOR):
+        os.remove(TORCH_CALLS_FOR)
+    try:
+        res = subprocess.run(cmd, capture_output=True, text=True)
+    except OSError as e:
+        raise RuntimeError(f"the host compiler cannot be run for _torch_calls.so: {e}") from e
     if verbose or res.returncode != 0:
         sys.stderr.write(res.stdout + res.stderr)
     if res.returncode != 0:
         raise RuntimeError("the host compiler failed building _torch_calls.so")
+    with open(TORCH_CALLS_FOR, "w") as f:
+        f.write(wanted + "\n")
     return TORCH_CALLS
 
 
 RESOURCES = os.path.join(HERE, "libemaslice.resources.txt")   # ptxas' report of the last build (git-ignored)
 
 
-def build(force: bool = False, verbose: bool = False) -> str:
-    build_torch_calls(force, verbose)
+def build_library(force: bool = False, verbose: bool = False) -> str:
     if not force and not needs_build() and os.path.exists(RESOURCES):
         return LIB
     cmd = [_nvcc(), "-std=c++17", "-O3", "-lineinfo", "-gencode", "arch=compute_100a,code=sm_100a",
@@ -74,14 +106,24 @@ def build(force: bool = False, verbose: bool = False) -> str:
     return LIB
 
 
+def build(force: bool = False, verbose: bool = False) -> str:
+    """Both. Without the extension the library is of use all the same, so that what keeps that one from being built is told, and
+    raised by the first call that needs it (or by build_torch_calls)."""
+    build_library(force, verbose)
+    try:
+        build_torch_calls(force, verbose)
+    except RuntimeError as e:
+        sys.stderr.write(f"the device-driven calls on tensors are not available: {e}\n")
+    return LIB
+
+
 def kernel_resources() -> dict:
     """What ptxas reported for every kernel of the last build: registers per thread, bytes of stack
     frame, bytes of spill stores and loads, keyed by the kernel's (mangled) name. The layer kernel runs
     352 threads per CTA at the register limit of one CTA per SM; a change that makes it spill, or
     that makes the compiler keep a copy of its 1 KB parameter block on every thread's stack, costs
     several per cent of its bandwidth, and this report is where that shows without a GPU."""
-    import re
-    build()
+    build_library()
     out, name = {}, None
     with open(RESOURCES) as f:
         for line in f:
