@@ -18,8 +18,9 @@ def ceil_div(a, b):
 class PoolModel:
     """Two stacks (lists, top at the end) and the calls' effect on tables, stated one block at a time."""
 
-    def __init__(self, ids0, ids1, capacity=None):
+    def __init__(self, ids0, ids1, capacity=(math.inf, math.inf)):
         self.stacks = [list(ids0), list(ids1)]
+        self.capacity = capacity
 
     def step(self, T, lens, new_lens, tables, max_tokens):
         """tables: list of dicts {block: entry}, changed in place. Returns (status, offsets, slots, positions)."""
@@ -44,11 +45,16 @@ class PoolModel:
             offsets.append(len(slots))
         slots += [NO_SLOT] * (max_tokens - len(slots))
         positions += [-1] * (max_tokens - len(positions))
+        status = 0
         for i in reversed(range(n)):
             for j in reversed(range(ceil_div(new_lens[i], T), ceil_div(lens[i], T))):
                 e = tables[i][j]
-                self.stacks[0 if e >= 0 else 1].append(e if e >= 0 else ~e)
-        return 0, offsets, slots, positions
+                k = 0 if e >= 0 else 1
+                if len(self.stacks[k]) < self.capacity[k]:
+                    self.stacks[k].append(e if e >= 0 else ~e)
+                else:
+                    status = EINVAL
+        return status, offsets, slots, positions
 
 
 def stored_place(row, width):

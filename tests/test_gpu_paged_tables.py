@@ -409,3 +409,115 @@ def test_a_call_that_could_not_be_launched_leaves_no_error_to_the_next_one():
         driver.cuStreamDestroy_v2(stream)
     assert [rc for rc in calls(None)] == [B.OK] * 4
     torch.cuda.synchronize()
+
+
+class Guarded:
+    """Arrays that lie in larger ones: what is before and behind them has to stay as it is."""
+
+    def __init__(self):
+        self.all = []
+
+    def __call__(self, values, dtype=torch.int32, before=4, behind=600):
+        big = torch.full((before + len(values) + behind,), 0x5a5a5a, dtype=dtype, device="cuda")
+        part = big[before:before + len(values)]
+        part.copy_(gpu(values, dtype))
+        self.all.append((big, before, len(values), behind))
+        return part
+
+    def untouched(self):
+        return all((big[:a] == 0x5a5a5a).all() and (big[a + n:] == 0x5a5a5a).all() for big, a, n, _ in self.all)
+
+
+@pytest.mark.parametrize("n,T,hi,room,capacity", [
+    (1, 16, 128, 1, (3, 2)),                                      # one request gives back more than there is room for
+    (7, 16, 100, 333, (9, 5)),
+    (40, 32, 900, 2049, (50, 700)),                               # more than one CTA; more blocks than threads come back
+    (700, 64, 300, 4097, (1, 800)),
+    (300, 16, 200, 60001, (2600, 1)),
+    (2100, 16, 40, 2048, (4000, 2000))])                          # more requests than a step lists
+def test_nothing_is_written_outside_the_arrays(n, T, hi, room, capacity):
+    """Requests grow, and others give back blocks that never came from this pool: those that the stacks have no room for are dropped."""
+    rng = np.random.default_rng(n + room)
+    width = ceil_div(hi, T)
+    guard = Guarded()
+    lens = rng.integers(0, hi + 1, n)
+    lens[0] = hi
+    model = PoolModel(rng.integers(0, 1000, capacity[0] * 2 // 3).tolist(), rng.integers(0, 1000, capacity[1] * 2 // 3).tolist(), capacity)
+    model.width = width
+    seen = set()
+    for kind in ("back", "all back", "grow"):
+        if kind == "grow":                                        # as far as the free blocks and the room go
+            lens = np.zeros(n, np.int64)
+            free = sum(map(len, model.stacks))
+            new = np.minimum(rng.integers(0, hi + 1, n), (free // n) * T)
+            new[np.cumsum(new) > room] = 0
+        else:
+            new = np.where(rng.random(n) < 0.5, lens // 3, lens) if kind == "back" else lens * 0
+            new[0] = 0
+        rows = [{j: int(rng.integers(0, 1000)) if rng.random() < 0.6 else ~int(rng.integers(0, 1000)) for j in range(ceil_div(int(x), T))} for x in lens]
+        cells = np.full((n, width + 2), 0x5a5a5a)
+        for i, row in enumerate(rows):
+            for j, e in row.items():
+                cells[i, j] = e
+        tables = guard(cells.reshape(-1).tolist())
+        tables2 = tables.view(n, width + 2)[:, :width]
+        ids = [guard(s + [-7] * (c - len(s))) for s, c in zip(model.stacks, capacity)]
+        free, out, work, status = guard([len(s) for s in model.stacks]), guard([-1, -1]), guard([0]), guard([0])
+        offsets, slots, positions = guard([-5] * (n + 1)), guard([5] * room, torch.int64), guard([5] * room)
+        before = [x.tolist() for x in ids]
+        for pool_out in (out, free):
+            status.zero_()
+            pool = B.PagedPool(ids[0], ids[1], free, pool_out, work)
+            a, b = gpu(lens.tolist()), gpu(new.tolist())
+            torch.cuda.synchronize()
+            if pool_out is free:                                  # again, from the same state
+                tables.copy_(gpu(cells.reshape(-1).tolist()))
+                for x, y in zip(ids, before):
+                    x.copy_(gpu(y))
+            assert B.paged_build_tables(pool, a, b, T, tables2, offsets, slots, positions, status) == B.OK
+            torch.cuda.synchronize()
+            if pool_out is out:
+                st, o, sl, po = model.step(T, lens.tolist(), new.tolist(), rows, room)
+                seen.add(st)
+            assert (int(status), offsets.tolist(), slots.tolist(), positions.tolist(), int(work)) == (st, o, sl, po, 0)
+            assert pool_out.tolist() == [len(s) for s in model.stacks]
+            for x, s, y in zip(ids, model.stacks, before):
+                assert x[:len(s)].tolist() == s and x[len(s):].tolist() == y[len(s):]
+            want = cells.copy()
+            for i, row in enumerate(rows):
+                for j, e in row.items():
+                    want[i, j] = e
+            assert (tables.cpu().numpy().reshape(n, width + 2) == want).all()
+            assert guard.untouched()
+        lens = new
+    assert seen == {0, B.EINVAL}
+
+
+def test_a_pool_with_room_to_spare():
+    """Stacks whose capacity is above their blocks: the cells behind the tops are left alone."""
+    b = Bench(30, 16, 9, 60, 80, 4, extra=50)
+    rng = np.random.default_rng(8)
+    for _ in range(6):
+        assert b.step(rng.integers(0, 80, 30).tolist(), 3000) in (0, B.ENOSPC)
+        assert all((x[-50:] == -7).all() for x in b.ids)
+
+
+def test_rows_that_are_not_written_keep_what_they_hold():
+    """Every row of the arenas that no slot names, and what lies behind them."""
+    Hkv, D, T, blocks = 3, 64, 16, 5
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    size = 2 * T * Hkv * D
+    bigs = [torch.randn(size * (blocks + 2), device="cuda", generator=gen).to(torch.bfloat16) for _ in range(2)]
+    before = [x.clone() for x in bigs]
+    arenas = [x[size:-size].view(blocks, 2, T, Hkv, D) for x in bigs]
+    k, v = (torch.randn((2, Hkv, D), device="cuda", generator=gen).to(torch.bfloat16) for _ in range(2))
+    slots = gpu([blocks * T - 1, ~0], torch.int64)
+    torch.cuda.synchronize()
+    assert B.paged_write_kv(B.PagedCache(*arenas), k, v, slots) == B.OK
+    torch.cuda.synchronize()
+    for x, y, block, row in zip(bigs, before, (blocks, 1), (T - 1, 0)):
+        for plane in range(2):
+            at = block * size + (plane * T + row) * Hkv * D
+            assert not torch.equal(x[at:at + Hkv * D], y[at:at + Hkv * D])
+            y[at:at + Hkv * D] = x[at:at + Hkv * D]
+        assert torch.equal(x, y)
