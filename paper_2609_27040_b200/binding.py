@@ -187,12 +187,13 @@ def _seqs(seqs) -> np.ndarray:
 def kv_block_swizzle(x):
     """Converts KV rows between canonical order and the block format's storage order (and back: the
     permutation is its own inverse). `x` is a numpy array or torch tensor of 16-bit elements whose
-    last three dimensions are [16 token rows][num_kv_heads][128]; within every 128 bytes of token
-    row r, the 16-byte unit u moves to unit u ^ (r & 7). Returns a new array."""
+    last three dimensions are [token rows][num_kv_heads][head_dim] (slices: 16 and 128; PagedCache: 16, 32 or
+    64 rows, heads of 64, 128 or 256); within every 128 bytes of token row r, the 16-byte unit u moves to
+    unit u ^ (r & 7). Returns a new array."""
     shape = tuple(x.shape)
-    if len(shape) < 3 or shape[-3] != 16 or shape[-1] != 128:
-        raise ValueError(f"expected [..., 16, num_kv_heads, 128], got {shape}")
-    v = x.reshape(shape[:-3] + (16, shape[-2] * 2, 8, 8))
+    if len(shape) < 3 or shape[-3] not in (16, 32, 64) or shape[-1] not in (64, 128, 256):
+        raise ValueError(f"expected [..., 16 / 32 / 64, num_kv_heads, 64 / 128 / 256], got {shape}")
+    v = x.reshape(shape[:-2] + (shape[-2] * shape[-1] // 64, 8, 8))
     out = v.copy() if isinstance(v, np.ndarray) else v.clone()
     for k in range(1, 8):
         perm = [u ^ k for u in range(8)]

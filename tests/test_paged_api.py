@@ -325,3 +325,17 @@ def test_kernels_that_start_early_read_through_coherent_loads():
             seen += 1
             assert not re.search(r"ld\.global\.nc|__ldg\(|\b(%s)\(" % "|".join(wrappers), text), name
     assert seen == 2
+
+
+@pytest.mark.parametrize("T,Hkv,D", [(16, 3, 64), (32, 1, 64), (64, 5, 128), (16, 2, 256), (32, 4, 256), (16, 8, 128)])
+def test_the_block_formats_converter_takes_every_cache(T, Hkv, D):
+    """Unit u of 8 elements of token row r lies at unit u ^ (r & 7) of its 64 elements; its own inverse, for arrays and tensors."""
+    from tests.paged_helpers import stored_place
+    x = torch.arange(3 * 2 * T * Hkv * D).to(torch.int16).view(3, 2, T, Hkv, D)
+    y = B.kv_block_swizzle(x)
+    for r in range(T):
+        assert torch.equal(y[:, :, r].reshape(3, 2, -1)[..., torch.from_numpy(stored_place(r, Hkv * D))], x[:, :, r].reshape(3, 2, -1))
+    assert torch.equal(B.kv_block_swizzle(y), x) and (B.kv_block_swizzle(x.numpy()) == y.numpy()).all()
+    for bad in (x[:, :, :8], x[..., :32], x[0, 0, 0]):
+        with pytest.raises(ValueError):
+            B.kv_block_swizzle(bad)
