@@ -515,7 +515,8 @@ int slice_copy_blocks_series(void* ring_base, uint32_t ring_slots, uint64_t slot
  *     the launch fails). What only the kernel can see is written to `status`, a device word that may be
  *     NULL: SLICE_EINVAL, SLICE_ENOSPC or SLICE_ETIMEOUT. The kernels never write 0 there: the caller
  *     clears the word, and reads it when it likes.
- *   - The device of the call's memory must be current, and `stream` belong to it (EINVAL / ECUDA).
+ *   - The device of all of a call's memory must be current, and `stream` (NULL: the legacy default stream) belong to it. The calls look
+ *     at one array only (out, offsets, the slots of paged_write_kv: EINVAL where it is another device's or plain host memory).
  *   - Strides: bytes for rows of elements, multiples of 16; entries for tables, at least max_blocks. Pointers to
  *     elements (arenas, q, k, v, out, workspace) are 16-byte aligned.
  *   - What a call writes overlaps nothing that it reads (free_out may be free_in; k and v of paged_write_kv lie outside the
@@ -524,9 +525,10 @@ int slice_copy_blocks_series(void* ring_base, uint32_t ring_slots, uint64_t slot
  *     two captured graphs that may run together, need one each); calls in stream order may share one.
  *   - Ids of a pool that are taken from a slice_t belong to a sequence of that slice which the caller
  *     allocated for the purpose (slice_alloc_blocks); slice_reclaim rewrites that sequence's host table only,
- *     so hand the ids back first. */
+ *     so hand the ids back first. A staged copy of a lent block (prefetch_layer) does not follow paged_write_kv as it
+ *     follows slice_append_kv: rows of sequences that both paths read are written before their blocks are staged. */
 
-/* One layer's cache. blocks[0] blocks in the arena of entries e >= 0, blocks[1] in that of entries e < 0
+/* One layer's cache (of a slice_t's arenas: in layout 0, where a layer's blocks are evenly spaced by id). blocks[0] blocks in the arena of entries e >= 0, blocks[1] in that of entries e < 0
  * (the lent part, or a staging slot; 0 and NULL when there is none). block = K plane
  * [block_tokens][num_kv_heads][head_dim], then the V plane, in the swizzled order of the block format. */
 typedef struct {
@@ -632,7 +634,8 @@ int paged_decode_workspace(const paged_cache_t* cache, uint32_t num_q_rows, uint
  *   q, out   [nseq] rows of [num_heads][head_dim], q_stride / out_stride bytes apart
  *   lse      [nseq][num_heads] f32 (natural-log sum of exponentials), or NULL
  * A sequence of length 0 gets zeros and minus infinity. What block tails hold does not matter; the rows of V that are
- * attended to must be finite. Arithmetic: 16-bit products, f32 accumulation and softmax, result rounded once.
+ * attended to must be finite, and in bf16 their magnitudes added up over the positions below the largest f32 (products are
+ * accumulated before the division by the sum of weights). Arithmetic: 16-bit products, f32 accumulation and softmax, result rounded once.
  * The result does not depend on timing. Status: EINVAL (length below 0 or above max_blocks * block_tokens: zeros, like
  * an empty sequence; an entry outside its arena: reads as zeros, the row is not meaningful; lengths seen to change during the call: no row of it
  * is), ETIMEOUT (a copy or a warp did not come within seconds: rows are missing).

@@ -446,7 +446,9 @@ def slice_schedule_gll(slices) -> int:
 # -- device-driven path: torch tensors in, one launch per call ---------------------------------------
 # On a small batch the host's part of a call takes longer than the kernel: tensors are checked, and the argument structs of
 # the C ABI filled in, by an extension module (csrc/torch_calls.cpp: 0.3 us a call, 3 to 5 us in Python). What does not fit is
-# a ValueError; what the C entry point refuses comes back as its code.
+# a ValueError; what the C entry point refuses comes back as its code. As everywhere in this module `stream` is a torch stream, its
+# address or None, and None is the legacy default stream, NOT torch's current one: inside torch.cuda.stream(s) pass s, or the call
+# has no order with what is enqueued there.
 
 _calls = None
 
@@ -545,11 +547,13 @@ class PagedPool:
 
 def paged_build_tables(pool: PagedPool, lens, new_lens, block_tokens: int, tables, offsets, slots, positions, status=None,
                        stream=None) -> int:
+    """Block tables and slot maps from request lengths (see include/emaslice.h). stream=None: the legacy default stream."""
     return (_calls or _torch_calls()).build(pool._addr, pool._dev, lens, new_lens, block_tokens, tables, offsets, slots, positions, status,
                                             stream)
 
 
 def paged_write_kv(cache: PagedCache, k, v, slots, status=None, stream=None) -> int:
+    """K and V rows into the blocks that their slots name. stream=None: the legacy default stream."""
     return (_calls or _torch_calls()).write(cache._addr, cache._dev, k, v, slots, status, stream)
 
 
@@ -565,10 +569,12 @@ def paged_decode_workspace(cache: PagedCache, num_q_rows: int) -> int:
 
 def paged_decode_tables(cache: PagedCache, tables, lens, q, sm_scale: float, out, workspace, lse=None, window: int = 0, status=None,
                         stream=None) -> int:
+    """Attention of one new token per sequence. stream=None: the legacy default stream."""
     return (_calls or _torch_calls()).decode(cache._addr, cache._dev, tables, lens, q, sm_scale, out, workspace, window, status, stream, lse)
 
 
 def paged_decode_diff(cache: PagedCache, tables, lens, q, lam, sm_scale: float, out, workspace, norm_weight=None, eps: float = 1e-5,
                       out_scale: float = 1.0, window: int = 0, status=None, stream=None) -> int:
+    """Differential attention of one new token per sequence. stream=None: the legacy default stream."""
     return (_calls or _torch_calls()).diff(cache._addr, cache._dev, tables, lens, q, sm_scale, out, workspace, window, status, stream, lam,
                                            norm_weight, eps, out_scale)
