@@ -47,3 +47,26 @@ def test_copy_kernels_leave_room_beside_the_layer_kernel():
     assert len(bulk) == 1
     regs = lambda per_thread, threads: -(-per_thread * 32 // 256) * 256 * (threads // 32)   # allocated per warp, in units of 256
     assert regs(layer, 352) + regs(bulk[0]["registers"], 32) <= 65536
+
+
+def test_device_driven_kernels_fit_their_cta_and_do_not_spill():
+    """One CTA to an SM; no stack and no spills but in the variant of 9 to 16 columns with heads of 256, whose eight consumer warps
+    leave 168 registers to a thread (about 20 of a lane's values are kept in local memory)."""
+    res = build_mod.kernel_resources()
+    decode = {k: v for k, v in res.items() if "paged_decode_kernel" in k}
+    assert len(decode) == 12, sorted(res)                 # heads of 64 / 128 / 256 x one group of columns or two x bf16 / fp16
+    for name, r in decode.items():
+        two = "Lj2E" in name
+        warps = (4 * 2 + 1 + 2) if two else (6 + 1 + 1)   # consumers, scheduler, mergers (one group, heads of 256: five consumers)
+        if two:                                           # a scheduler's quarter of the registers holds three of the eleven warps
+            assert r["registers"] * 32 * -(-warps // 4) <= 16384, (name, r)
+        assert r["registers"] <= 255 and r["registers"] * 32 * warps <= 65536, (name, r)
+        if two and "Lj256E" in name:
+            assert r["stack"] <= 64 and r["spill_stores"] <= 128 and r["spill_loads"] <= 192, (name, r)
+        else:
+            assert r["stack"] == r["spill_stores"] == r["spill_loads"] == 0, (name, r)
+    others = {k: v for k, v in res.items() if "write_kv_kernel" in k or "build_tables_kernel" in k}
+    assert len(others) == 3
+    for name, r in others.items():
+        assert r["stack"] == r["spill_stores"] == r["spill_loads"] == 0, (name, r)
+        assert r["registers"] <= (64 if "write_kv" in name else 128), (name, r)   # four CTAs of 256 threads; one of 512
