@@ -6,10 +6,10 @@
 //
 // Every K and V byte is needed once and used for a handful of query rows: the kernel is bound by HBM,
 // and what it does is keep enough copies in flight on every SM while the arithmetic stays hidden. Measured
-// (B200, 6.45 TB/s copy rate): 64 sequences of 512 to 4095 tokens, 32/8 heads of 128: 101 us, 6.0 TB/s; 5 of 60000
-// to 100001, 64/8 heads: 252 us, 6.5 TB/s; 200 with a window of 1000, 12 heads of 64: 95 us, 5.8 TB/s; differential,
-// 8 of 9000 to 40000, 16/4 heads of 256: 134 us, 6.0 TB/s; one of 20000, 32/8 heads: 26 us; one of 500: 10.8 us (launch,
-// one read of the lengths, of a table cell, of the cache, one merge, each a trip to L2 or HBM).
+// (B200, 6.45 TB/s copy rate, in a captured graph): 64 sequences of 512 to 4095 tokens, 32/8 heads of 128: 100 us, 6.0 TB/s; 5 of
+// 60000 to 100001, 64/8 heads: 253 us, 6.5 TB/s; 200 with a window of 1000, 12 heads of 64: 96 us, 5.8 TB/s (102 us as called from
+// Python); differential, 8 of 9000 to 40000, 16/4 heads of 256: 133 us, 6.0 TB/s; one of 8000, 32/8 heads: 19 us; one of 500: 10.9 us
+// (launch, one read of the lengths, of a table cell, of the cache, one merge, each a trip to L2 or HBM).
 //   * Work is cut into pieces, runs of chunks of one (sequence, KV head), an item; a chunk is 16 KB of it (64 /
 //     32 / 16 tokens of K and V for head_dim 64 / 128 / 256). How items are cut (cut_of, share_of) depends on the
 //     lengths alone; who computes a piece is settled by a ticket counter, because the SMs do not get equal shares of
@@ -53,8 +53,11 @@ constexpr uint32_t kNotes = 16;                     // most pieces known to the 
 // a piece's rows and the weights took their present forms).
 constexpr uint32_t kAhead = 6;
 // Items of at most two chunks are taken by one warp, which also writes them out (a merge takes longer than a chunk). Where
-// pieces are many and this small on average, items of so many chunks are, too: 1000 sequences of 10 to 260 tokens
-// 119 us, with 4 (which leaves most of them to all warps) 183.
+// pieces are many (four to every consumer warp of the grid) and this small on average, items of so many chunks are, too: 1000 sequences
+// of 10 to 260 tokens 119 us, with 4 (which leaves most of them to all warps) 183. Without and with it, sequences of 10 to 240
+// tokens, 8 KV heads of 128, by their number: 40: 16 / 18 us, 80: 24 / 22, 160: 41 / 32, 300: 67 / 47, 440 (the last without it): 93 / 62,
+// 460 (the first with it): 95 / 64, 900: 172 / 105; 155 of up to 104, 15 KV heads, differential, heads of 64: 27 / 28, of 128: 45 / 32. So the
+// rule is cautious: one warp an item pays from about half an item to a warp of the grid on.
 constexpr uint32_t kSolo = 8;
 constexpr uint32_t kFan = kPagedFan;                // most pieces that meet at a time
 static_assert(kFan == 32, "sum_parts takes two times sixteen");
@@ -1315,7 +1318,7 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) paged_decode_kernel
     const uint32_t mean = pieces ? static_cast<uint32_t>(min(total / pieces, 24ull)) : 24;
     most = 24 / max(mean, 1u);
     batch = batch_of(pieces, most);
-    // Items that one warp takes alone: only where every warp gets several of them.
+    // Items that one warp takes alone: only where every warp gets several of them (times on both sides: at kSolo).
     many = pieces >= 4 * S::kWarps * gridDim.x && total <= static_cast<unsigned long long>(pieces) * kSolo;
   }
   __syncthreads();
