@@ -735,3 +735,76 @@ def test_a_thread_whose_first_use_of_the_gpu_is_the_call(diff):
     t.join()
     torch.cuda.synchronize()
     assert codes == [B.OK, B.OK] and torch.equal(c.out[:4], want) and int(c.status) == 0
+
+
+@pytest.mark.parametrize("T,Hkv,G,D,dtype", [(16, 2, 3, 64, BF), (32, 4, 4, 128, HF), (16, 1, 12, 256, BF)])
+def test_a_captured_serving_step_follows_the_requests(T, Hkv, G, D, dtype):
+    """One graph of tables, rows, attention of both forms and the new lengths taking the old ones' place, replayed while requests come,
+    grow by one or by several, fall back and finish, against dense 64-bit caches."""
+    n, width, room = 7, 12, 400
+    rng = np.random.default_rng(T + D)
+    gen = torch.Generator(device="cuda").manual_seed(D)
+    blocks = (20, 40)
+    arenas = [torch.full((b, 2, T, Hkv, D), float("nan"), dtype=dtype, device="cuda") for b in blocks]
+    cache = B.PagedCache(*arenas)
+    free, work, status = gpu(list(blocks)), gpu([0]), gpu([0])
+    pool = B.PagedPool(*(gpu(rng.permutation(b).tolist()) for b in blocks), free, free, work)
+    tables = torch.full((n, width), -1, dtype=torch.int32, device="cuda")
+    twice = 2 if G <= 8 else 0                                   # heads of the differential form: none beyond 8 to a KV head
+    ws = torch.zeros(B.paged_decode_workspace(cache, Hkv * G * (twice or 1)), dtype=torch.uint8, device="cuda")
+    lens_t, new_t, offsets = gpu([0] * n), gpu([0] * n), gpu([0] * (n + 1))
+    slots, positions = torch.zeros(room, dtype=torch.int64, device="cuda"), gpu([0] * room)
+    k, v = torch.zeros((room, Hkv, D), dtype=dtype, device="cuda"), torch.zeros((room, Hkv, D), dtype=dtype, device="cuda")
+    q = torch.zeros((n, Hkv * G, D), dtype=dtype, device="cuda")
+    qd, lam = torch.zeros((n, 2 * Hkv * G, D // 2), dtype=dtype, device="cuda"), torch.full((Hkv * G,), 0.5, device="cuda")
+    out, out2, lse = torch.zeros_like(q), torch.zeros_like(q), torch.zeros((n, Hkv * G), device="cuda")
+    s, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph, stream=s):
+        now = torch.cuda.current_stream()
+        assert B.paged_build_tables(pool, lens_t, new_t, T, tables, offsets, slots, positions, status, now) == B.OK
+        assert B.paged_write_kv(cache, k, v, slots, status, now) == B.OK
+        assert B.paged_decode_tables(cache, tables, new_t, q, 0.125, out, ws, lse=lse, status=status, stream=now) == B.OK
+        if twice:
+            assert B.paged_decode_diff(cache, tables, new_t, qd, lam, 0.2, out2, ws, status=status, stream=now) == B.OK
+        lens_t.copy_(new_t)
+    lens, dense = [0] * n, [[] for _ in range(n)]
+    finished = fell = 0
+    for step in range(30):
+        new = []
+        for x in lens:
+            kind = rng.random()
+            new.append(int(rng.integers(0, 50)) if not x else 0 if kind < 0.08 else max(0, x - int(rng.integers(1, 40))) if kind < 0.16 else
+                       min(x + (1 if kind < 0.8 else int(rng.integers(1, 9))), 100))
+        finished += sum(a > 0 and b == 0 for a, b in zip(lens, new))
+        fell += sum(a > b > 0 for a, b in zip(lens, new))
+        for x in (k, v, q, qd):
+            x.copy_(torch.randn(x.shape, device="cuda", generator=gen))
+        new_t.copy_(gpu(new))
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert int(status) == 0 and lens_t.tolist() == new
+        at = 0
+        for i in range(n):
+            dense[i] = dense[i][:new[i]]
+            for _ in range(max(0, new[i] - lens[i])):
+                dense[i].append((k[at].double(), v[at].double()))
+                at += 1
+            if not new[i]:
+                assert not out[i].any() and not out2[i].any() and (lse[i] == -math.inf).all()
+                continue
+            kk, vv = torch.stack([x[0] for x in dense[i]]), torch.stack([x[1] for x in dense[i]])
+            top = float(vv.abs().max())
+            ref, ref_lse, size = attend(q[i].double(), kk, vv, 0.125)
+            ok, worst = close(out[i], ref, row_error(new[i], D, size, top), torch.finfo(dtype).eps)
+            assert ok and float((lse[i].double() - ref_lse).abs().max()) <= lse_slack(new[i], D, size), (step, i, worst)
+            if twice:
+                o1, _, s1 = attend(qd[i, 0::2].double(), kk[..., :D // 2], vv, 0.2)
+                o2, _, s2 = attend(qd[i, 1::2].double(), kk[..., D // 2:], vv, 0.2)
+                e = row_error(new[i], D, s1, top) + 0.5 * row_error(new[i], D, s2, top) + 2.0 ** -22 * top
+                ok, worst = close(out2[i], o1 - 0.5 * o2, e, torch.finfo(dtype).eps)
+                assert ok, (step, i, worst)
+        assert at == offsets.tolist()[n] and sum(free.tolist()) + sum(ceil_div(x, T) for x in new) == sum(blocks)
+        lens = new
+    assert finished and fell
