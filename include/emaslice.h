@@ -519,8 +519,8 @@ int slice_copy_blocks_series(void* ring_base, uint32_t ring_slots, uint64_t slot
  *     at one array only (out, offsets, the slots of paged_write_kv: EINVAL where it is another device's or plain host memory).
  *   - Strides: bytes for rows of elements, multiples of 16; entries for tables, at least max_blocks. Pointers to
  *     elements (arenas, q, k, v, out, workspace) are 16-byte aligned.
- *   - What a call writes overlaps nothing that it reads (free_out may be free_in; k and v of paged_write_kv lie outside the
- *     arenas), and nobody else writes what a call reads while it runs.
+ *   - An array that a call writes overlaps no other array of it (free_out may be free_in; k and v of paged_write_kv lie outside
+ *     the arenas), and nobody else writes what a call reads while it runs.
  *   - Workspaces must not be in use by two calls at a time (calls on streams without an order between them, or
  *     two captured graphs that may run together, need one each); calls in stream order may share one.
  *   - Ids of a pool that are taken from a slice_t belong to a sequence of that slice which the caller
