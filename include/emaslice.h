@@ -654,6 +654,152 @@ int paged_decode_tables(const paged_decode_t* args, void* stream);
  * finite, too: an infinity in one map's half of a K row makes the other map's score not a number. */
 int paged_decode_diff(const paged_decode_t* args, void* stream);
 
+/* ---- Several new tokens per request, and blocks that requests share --------------------------------
+ * The rest of speculative decoding and of sampling several continuations, device-driven like the calls above (what is said there holds
+ * here: status, strides, streams, workspaces, nothing overlaps). A step that verifies drafted tokens: paged_build_tables grows the requests by
+ * them, paged_write_kv writes their rows, paged_tree_attention attends, paged_keep_rows moves the accepted rows to their places, and
+ * paged_build_tables takes back the rest. */
+
+/* Attention of several new tokens per request. Request i has the tokens offsets[i] .. offsets[i + 1] - 1 of the token arrays, m of
+ * them, which are the last m of its lens[i] positions (their K and V rows are in the cache); c = lens[i] - m positions are its context.
+ * For query head h (KV head h / G, G = num_heads / num_kv_heads in 1..128) and token j of the request
+ *   out = softmax(sm_scale * q K^T) V over the positions that token j sees:
+ *     mask NULL   (a chain, a piece of a prompt) positions up to c + j; with a window the last `window` of them, counted from the token's position
+ *     mask given  (a tree) new token b where bit b of the token's mask is set (its own bit as any other), and the context; with a
+ *                 window the context's positions above the token's position - window
+ *   The token's position is positions[t], taken into c .. lens[i] - 1, or c + j where that is NULL.
+ *   q, out     [ntok] rows of [num_heads][head_dim], q_stride / out_stride bytes apart
+ *   mask       [ntok] rows of mask_words 64-bit words, mask_stride words apart: bit b of a row is bit b % 64 of word b / 64; tokens
+ *              past the row's words are not seen, bits past m mean nothing
+ *   lse        [ntok][num_heads] f32, or NULL
+ * offsets [nseq + 1] rises from a number >= 0 to one <= ntok; rows that it leaves out are not touched. A token that sees nothing gets zeros and
+ * minus infinity. Rows of V that no token of a request sees may hold anything, as may rows of K that a token does not see; the
+ * other rows of V must be finite, as for paged_decode_tables. Arithmetic as there: 16-bit products, f32 accumulation and softmax,
+ * weights as the sum of two 16-bit numbers, result rounded once; it does not depend on timing.
+ * workspace: paged_tree_workspace bytes; it needs no clearing.
+ * Status: EINVAL (a length or an offset out of range, fewer positions than tokens: the request's rows are zeros where its offsets name any;
+ * an entry outside its arena: reads as zeros), ETIMEOUT. Returns EINVAL, ESCRATCH, ECUDA. Two launches. */
+typedef struct {
+  const paged_cache_t* cache;
+  const int32_t* tables;                  /* [nseq] rows of max_blocks cells                      */
+  uint64_t table_stride;
+  const int32_t *lens, *offsets;          /* [nseq], [nseq + 1]                                   */
+  const void* q;
+  uint64_t q_stride;
+  void* out;
+  uint64_t out_stride;
+  float* lse;
+  const uint64_t* mask;
+  uint64_t mask_stride;
+  const int32_t* positions;               /* [ntok], or NULL                                      */
+  void* workspace;
+  uint64_t workspace_bytes;
+  int32_t* status;
+  uint32_t nseq, max_blocks, ntok, num_heads, mask_words, window;
+  float sm_scale;
+} paged_tree_t;
+int paged_tree_workspace(const paged_cache_t* cache, uint32_t num_heads, uint64_t* out_bytes);
+int paged_tree_attention(const paged_tree_t* args, void* stream);
+
+/* The layers of a cache, for calls that move rows in all of them: nlayers (1..128) descriptors that differ in their bases only. */
+
+/* Accepted rows to their places, in all layers: row lens[i] + j of request i takes what row lens[i] + keep[i][j] held before the
+ * call, for j < counts[i] <= max_keep (rows of K and of V, positions of the request). keep[i] rises (the same row twice is refused). Blocks that are written
+ * to have one holder. Status: EINVAL (a count, a length, an index or an entry out of range, a list that does not rise: the request is left as
+ * it is). Returns EINVAL, ECUDA. */
+typedef struct {
+  const paged_cache_t* layers;            /* host, [nlayers]                                      */
+  const int32_t* tables;
+  uint64_t table_stride;
+  const int32_t* lens;                    /* [nseq]                                               */
+  const int32_t* keep;                    /* [nseq] rows of max_keep indices                      */
+  uint64_t keep_stride;
+  const int32_t* counts;                  /* [nseq]                                               */
+  int32_t* status;
+  uint32_t nlayers, nseq, max_blocks, max_keep;
+} paged_keep_rows_t;
+int paged_keep_rows(const paged_keep_rows_t* args, void* stream);
+
+/* Blocks that several requests hold. refs[a][b] is the number of requests that hold block b of arena a besides the first one: 0
+ * for a block with one holder and for a free one, so that arrays of zeros describe a cache without sharing, and paged_build_tables, which
+ * knows nothing of holders, may grow any request, and shrink it by blocks that it holds alone. Only whole blocks are shared: a request's last block, if it is not
+ * full, has one holder. work: paged_shares_workspace bytes, zero before its first use; every call leaves it fit for the next one. */
+typedef struct {
+  int32_t* refs[2];                       /* [blocks[a]]; NULL where blocks[a] is 0               */
+  uint32_t blocks[2];
+  void* work;
+  uint64_t work_bytes;
+} paged_shares_t;
+int paged_shares_workspace(uint32_t blocks0, uint32_t blocks1, uint64_t* out_bytes);
+
+/* Forks: request dst[f], which holds nothing (lens 0), gets what src[f] holds: whole blocks are shared, and for a last block that is
+ * not full one is popped, in the order of the forks, and copies[f] = (entry of the source's block, entry of the new one, rows to be
+ * copied): paged_copy_blocks does that. Other rows of copies are zeros, which copy nothing. new_lens[dst[f]] = lens[src[f]] (new_lens
+ * may be lens); the rest of new_lens is left alone. dst[f] < 0: no fork. nseq is at most 262144.
+ * Status: EINVAL (an index, a length or a top out of range, a dst that holds tokens, is another fork's dst or is a fork's src), ENOSPC: then
+ * nothing has changed but copies, which are zeros. EINVAL also for an entry of a source that is outside its arena: it is copied, nobody holds it.
+ * Returns EINVAL, ECUDA. */
+typedef struct {
+  const paged_pool_t* pool;
+  const paged_shares_t* shares;
+  const int32_t* lens;                    /* [nseq]                                               */
+  int32_t* new_lens;
+  int32_t* tables;
+  uint64_t table_stride;
+  const int32_t *src, *dst;               /* [nfork]                                              */
+  int32_t* copies;                        /* [nfork][3]                                           */
+  int32_t* status;
+  uint32_t nseq, nfork, block_tokens, max_blocks;
+} paged_fork_t;
+int paged_fork(const paged_fork_t* args, void* stream);
+
+/* Requests that end or shrink, where blocks may be shared: request i gives up the blocks past new_lens[i] tokens (those with
+ * new_lens[i] >= lens[i] none). A block's id is pushed when its last holder has given it up: of the blocks freed by a call, the highest id of each arena
+ * first. Tables are not changed. Status: EINVAL (a length or a top out of range: nothing has changed; an entry outside its arena: passed over; a
+ * block given up more often than it is held: pushed once; ids that exceed a stack's capacity: dropped). Returns EINVAL, ECUDA. */
+typedef struct {
+  const paged_pool_t* pool;
+  const paged_shares_t* shares;
+  const int32_t *lens, *new_lens;         /* [nseq]                                               */
+  const int32_t* tables;
+  uint64_t table_stride;
+  int32_t* status;
+  uint32_t nseq, block_tokens, max_blocks;
+} paged_free_t;
+int paged_free(const paged_free_t* args, void* stream);
+
+/* Ids that are taken away (slice_reclaim, from device arrays), or a cache moved to the front of its arenas: afterwards no request holds,
+ * and no stack has, a block of arena a with an id of limits[a] or more (all of them: limits[a] >= blocks[a]; none: 0). The blocks to be
+ * moved, in the order of entries 0, 1, .. of the first arena, then of ids 0, 1, .. of the second, get the free ids below the limits as pops would
+ * give them. Tables and counts of holders follow, and copies[r] = (old entry, new entry, block_tokens) is what paged_copy_blocks has to copy; the other
+ * rows of copies are zeros. Old blocks keep what they hold until somebody writes there.
+ * Status: EINVAL (a length, limit or top out of range, more than max_copies blocks to be moved), ENOSPC (too few free ids below the
+ * limits): then nothing has changed but copies, which are zeros. EINVAL also for an entry outside its arena, which is left as it is, and for
+ * such an id on a stack, which is dropped. Returns EINVAL, ECUDA. Two launches. */
+typedef struct {
+  const paged_pool_t* pool;
+  const paged_shares_t* shares;
+  const int32_t* limits;                  /* [2]                                                  */
+  const int32_t* lens;                    /* [nseq]                                               */
+  int32_t* tables;
+  uint64_t table_stride;
+  int32_t* copies;                        /* [max_copies][3]                                      */
+  int32_t* status;
+  uint32_t nseq, max_copies, block_tokens, max_blocks;
+} paged_compact_t;
+int paged_compact(const paged_compact_t* args, void* stream);
+
+/* The first rows of blocks into other blocks, in all layers: copies[x] = (from entry, to entry, rows); rows 0 copies nothing. No block
+ * is copied to twice, and none that is copied to is copied from. Status: EINVAL (an entry or a number of rows out of range: not copied).
+ * Returns EINVAL, ECUDA. */
+typedef struct {
+  const paged_cache_t* layers;            /* host, [nlayers]                                      */
+  const int32_t* copies;                  /* [ncopies][3]                                         */
+  int32_t* status;
+  uint32_t nlayers, ncopies;
+} paged_copy_blocks_t;
+int paged_copy_blocks(const paged_copy_blocks_t* args, void* stream);
+
 const char* slice_strerror(int code);
 
 #ifdef __cplusplus

@@ -37,6 +37,8 @@ EXPORTS = [
     "slice_step_begin", "slice_step_submit_q", "slice_step_wait_out", "slice_step_flags", "slice_step_relay",
     "slice_copy_blocks_series",
     "paged_build_tables", "paged_write_kv", "paged_decode_workspace", "paged_decode_tables", "paged_decode_diff",
+    "paged_tree_workspace", "paged_tree_attention", "paged_keep_rows", "paged_shares_workspace", "paged_fork", "paged_free", "paged_compact",
+    "paged_copy_blocks",
 ]
 
 
@@ -98,6 +100,10 @@ class PagedPoolDesc(C.Structure):
     ]
 
 
+class PagedSharesDesc(C.Structure):
+    _fields_ = [("refs", C.c_void_p * 2), ("blocks", C.c_uint32 * 2), ("work", C.c_void_p), ("work_bytes", C.c_uint64)]
+
+
 _lib = None
 
 
@@ -143,9 +149,12 @@ def lib() -> C.CDLL:
         L.slice_cta_trace.argtypes = [vp, i32, vp, u64, vp, vp]
         L.slice_copy_blocks.argtypes = [vp, vp, vp, vp, u32, u64, u32, u32, vp]
         L.slice_copy_blocks_series.argtypes = [vp, u32, u64, vp, vp, u64, u32, u64, i32, u32, u32, vp]
-        for name in ("paged_build_tables", "paged_write_kv", "paged_decode_tables", "paged_decode_diff"):
+        for name in ("paged_build_tables", "paged_write_kv", "paged_decode_tables", "paged_decode_diff", "paged_tree_attention", "paged_keep_rows",
+                     "paged_fork", "paged_free", "paged_compact", "paged_copy_blocks"):
             getattr(L, name).argtypes = [C.c_char_p, vp]              # an argument struct's bytes, the stream
         L.paged_decode_workspace.argtypes = [C.POINTER(PagedCacheDesc), u32, C.POINTER(u64)]
+        L.paged_tree_workspace.argtypes = [C.POINTER(PagedCacheDesc), u32, C.POINTER(u64)]
+        L.paged_shares_workspace.argtypes = [u32, u32, C.POINTER(u64)]
         L.slice_strerror.argtypes = [C.c_int]
         L.slice_strerror.restype = C.c_char_p
         _lib = L
@@ -469,6 +478,8 @@ def _torch_calls():
             raise RuntimeError("the _torch_calls extension cannot be loaded: build it with paper_2609_27040_b200/build.py") from e
         x.bind(*(C.cast(getattr(L, name), C.c_void_p).value
                  for name in ("paged_build_tables", "paged_write_kv", "paged_decode_tables", "paged_decode_diff")))
+        x.bind_more(*(C.cast(getattr(L, name), C.c_void_p).value
+                      for name in ("paged_tree_attention", "paged_keep_rows", "paged_copy_blocks", "paged_fork", "paged_free", "paged_compact")))
         _calls = x
     return _calls
 
@@ -578,3 +589,101 @@ def paged_decode_diff(cache: PagedCache, tables, lens, q, lam, sm_scale: float, 
     """Differential attention of one new token per sequence. stream=None: the legacy default stream."""
     return (_calls or _torch_calls()).diff(cache._addr, cache._dev, tables, lens, q, sm_scale, out, workspace, window, status, stream, lam,
                                            norm_weight, eps, out_scale)
+
+
+class PagedLayers:
+    """The layers of a cache (1 to 128 PagedCache objects of one shape, block stride and device), for the calls that move rows in all of them."""
+
+    def __init__(self, caches):
+        caches = list(caches)
+        if not 1 <= len(caches) <= 128:
+            _refuse(f"layers: 1 to 128, got {len(caches)}")
+        ref = caches[0].desc
+        for c in caches[1:]:
+            d = c.desc
+            if (d.dtype, d.num_kv_heads, d.head_dim, d.block_tokens, list(d.blocks), list(d.block_stride)) != \
+                    (ref.dtype, ref.num_kv_heads, ref.head_dim, ref.block_tokens, list(ref.blocks), list(ref.block_stride)) or c._dev != caches[0]._dev:
+                _refuse("layers: caches of one shape, block stride and device")
+        self.descs = (PagedCacheDesc * len(caches))(*[c.desc for c in caches])
+        self._addr, self._dev, self._n, self.caches = C.addressof(self.descs), caches[0]._dev, len(caches), caches
+
+
+def paged_shares_workspace(local_blocks: int, lent_blocks: int) -> int:
+    """Bytes of PagedShares' workspace (zeroed by the caller before its first use)."""
+    out = C.c_uint64(0)
+    rc = lib().paged_shares_workspace(local_blocks, lent_blocks, C.byref(out))
+    if rc != OK:
+        raise SliceError(rc, "paged_shares_workspace")
+    return int(out.value)
+
+
+class PagedShares:
+    """Holders of blocks besides the first one: int32 [blocks] for either arena (`lent_refs` may be None), zeros for a cache without
+    sharing, and paged_shares_workspace bytes of zeroed workspace."""
+
+    def __init__(self, local_refs, lent_refs, work):
+        _torch_types()
+        dev = work.get_device()
+        d = PagedSharesDesc()
+        for j, t in enumerate((local_refs, lent_refs)):
+            if t is not None and t.numel():
+                d.refs[j], d.blocks[j] = _words(t, "refs", dev, _I32), t.numel()
+        if not work.is_contiguous():
+            _refuse("work: a contiguous tensor")
+        d.work, d.work_bytes = work.data_ptr(), work.numel() * work.element_size()
+        self.desc, self._addr, self.device, self._dev = d, C.addressof(d), work.device, dev
+        self._keep = (local_refs, lent_refs, work)
+
+
+def _same_device(pool: PagedPool, shares: PagedShares):
+    if pool._dev != shares._dev:
+        _refuse("pool and shares: on one device")
+
+
+def paged_tree_workspace(cache: PagedCache, num_heads: int) -> int:
+    """Bytes of workspace of paged_tree_attention."""
+    out = C.c_uint64(0)
+    rc = lib().paged_tree_workspace(cache._ref, num_heads, C.byref(out))
+    if rc != OK:
+        raise SliceError(rc, "paged_tree_workspace")
+    return int(out.value)
+
+
+def paged_tree_attention(cache: PagedCache, tables, lens, offsets, q, sm_scale: float, out, workspace, mask=None, lse=None, window: int = 0,
+                         positions=None, status=None, stream=None) -> int:
+    """Attention of several new tokens per request: a tree of drafted tokens (`mask`, int64 [tokens, words], bit b of a row: the token sees new
+    token b of its request) or a chain. stream=None: the legacy default stream."""
+    return (_calls or _torch_calls()).tree(cache._addr, cache._dev, tables, lens, offsets, q, sm_scale, out, workspace, mask, lse, window,
+                                           positions, status, stream)
+
+
+def paged_keep_rows(layers: PagedLayers, tables, lens, keep, counts, status=None, stream=None) -> int:
+    """Accepted rows to their places, in all layers. stream=None: the legacy default stream."""
+    return (_calls or _torch_calls()).keep(layers._addr, layers._n, layers._dev, tables, lens, keep, counts, status, stream)
+
+
+def paged_copy_blocks(layers: PagedLayers, copies, status=None, stream=None) -> int:
+    """The first rows of blocks into other blocks, in all layers: copies int32 [n, 3], as paged_fork and paged_compact leave them.
+    stream=None: the legacy default stream."""
+    return (_calls or _torch_calls()).copy(layers._addr, layers._n, layers._dev, copies, status, stream)
+
+
+def paged_fork(pool: PagedPool, shares: PagedShares, lens, new_lens, src, dst, block_tokens: int, tables, copies, status=None,
+               stream=None) -> int:
+    """Requests `dst` become forks of `src`: whole blocks shared, copies of last blocks asked for. stream=None: the legacy default stream."""
+    _same_device(pool, shares)
+    return (_calls or _torch_calls()).fork(pool._addr, shares._addr, pool._dev, lens, block_tokens, tables, new_lens, src, dst, copies, status,
+                                           stream)
+
+
+def paged_free(pool: PagedPool, shares: PagedShares, lens, new_lens, block_tokens: int, tables, status=None, stream=None) -> int:
+    """Requests end or shrink; a block is freed by its last holder. stream=None: the legacy default stream."""
+    _same_device(pool, shares)
+    return (_calls or _torch_calls()).free(pool._addr, shares._addr, pool._dev, lens, block_tokens, tables, new_lens, status, stream)
+
+
+def paged_compact(pool: PagedPool, shares: PagedShares, limits, lens, block_tokens: int, tables, copies, status=None, stream=None) -> int:
+    """Blocks out of the ids from `limits` (int32 [2], device) on: tables and counts rewritten, copies asked for. stream=None: the
+    legacy default stream."""
+    _same_device(pool, shares)
+    return (_calls or _torch_calls()).compact(pool._addr, shares._addr, pool._dev, lens, block_tokens, tables, limits, copies, status, stream)

@@ -12,8 +12,8 @@ import sysconfig
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libemaslice.so")
-SOURCES = ["slice.cpp", "copy_kernels.cu", "layer_kernel.cu", "noalloc.cu", "paged_api.cpp", "paged_tables.cu", "paged_decode.cu"]
-HEADERS = ["kernels.h", "ptx.cuh", "attention_tiles.cuh", os.path.join("..", "..", "include", "emaslice.h")]
+SOURCES = ["slice.cpp", "copy_kernels.cu", "layer_kernel.cu", "noalloc.cu", "paged_api.cpp", "paged_tables.cu", "paged_decode.cu", "paged_tree.cu", "paged_pages.cu"]
+HEADERS = ["kernels.h", "ptx.cuh", "tcgen05.cuh", "attention_tiles.cuh", os.path.join("..", "..", "include", "emaslice.h")]
 
 
 def _nvcc() -> str:

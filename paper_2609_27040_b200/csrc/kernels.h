@@ -222,9 +222,9 @@ cudaError_t launch_append(const AppendParams& p, cudaStream_t stream);
 // threads wait for that one's end (ptx::grid_dependency_wait) before they touch global memory, and let the next one start
 // as soon as all CTAs have (ptx::launch_dependents), so that of a step's launches only the first one's latency shows.
 template <typename... Params, typename... Args>
-cudaError_t launch_early(void (*kernel)(Params...), unsigned grid, unsigned threads, size_t shared, cudaStream_t stream, const Args&... args) {
+cudaError_t launch_ahead(void (*kernel)(Params...), dim3 grid, unsigned threads, size_t shared, cudaStream_t stream, const Args&... args) {
   cudaLaunchConfig_t cfg{};
-  cfg.gridDim = dim3(grid);
+  cfg.gridDim = grid;
   cfg.blockDim = dim3(threads);
   cfg.dynamicSmemBytes = shared;
   cfg.stream = stream;
@@ -234,6 +234,11 @@ cudaError_t launch_early(void (*kernel)(Params...), unsigned grid, unsigned thre
   cfg.attrs = &attr;
   cfg.numAttrs = 1;
   return cudaLaunchKernelEx(&cfg, kernel, args...);
+}
+
+template <typename... Params, typename... Args>
+cudaError_t launch_early(void (*kernel)(Params...), unsigned grid, unsigned threads, size_t shared, cudaStream_t stream, const Args&... args) {
+  return launch_ahead(kernel, dim3(grid), threads, shared, stream, args...);
 }
 
 // paged_tables.cu: block tables and slot maps from request lengths (see paged_build_tables).
@@ -323,5 +328,88 @@ struct PagedDecodeParams {
 size_t paged_workspace_bytes(uint32_t rows, uint32_t head_dim);
 // dev < 64: the current device.
 cudaError_t launch_paged_decode(const PagedDecodeParams& p, int dev, int num_sms, cudaStream_t stream);
+
+// paged_pages.cu: shared blocks, see paged_fork, paged_free and paged_compact.
+struct PagesParams {
+  int32_t* ids[2];             // free stacks, top at the end
+  uint32_t capacity[2];
+  const int32_t* free_in;      // [2]; free_out may be the same array
+  int32_t* free_out;
+  uint32_t* work;              // ticket word, zero before and after
+  int32_t* refs[2];            // [blocks[a]] holders besides the first one
+  uint32_t blocks[2];
+  uint32_t* bits[2];           // a bit per block, zero before and after
+  int32_t* map[2];             // [blocks[a]] entries that blocks have moved to
+  uint32_t* moved;             // how many have
+  const int32_t* lens;         // [nseq]
+  const int32_t* new_lens;
+  int32_t* new_lens_out;       // fork: may be lens
+  const int32_t* src;          // [nfork]
+  const int32_t* dst;
+  const int32_t* limits;       // [2]
+  int32_t* tables;
+  uint64_t table_stride;
+  uint32_t nseq, nfork, max_blocks, block_shift;
+  int32_t* copies;             // [ncopies][3]: from, to, rows
+  uint32_t ncopies;
+  int* status;
+};
+cudaError_t launch_free(const PagesParams& p, int num_sms, cudaStream_t stream);
+cudaError_t launch_fork(const PagesParams& p, int num_sms, cudaStream_t stream);
+cudaError_t launch_compact(const PagesParams& p, int num_sms, cudaStream_t stream);
+
+// paged_pages.cu: rows that move, in all layers (see paged_copy_blocks and paged_keep_rows).
+constexpr uint32_t kMoveLayers = 128;
+struct MoveParams {
+  uint8_t* base[2][kMoveLayers];
+  uint64_t block_stride[2];
+  uint32_t blocks[2];
+  uint32_t nlayers, row_bytes, block_shift;
+  const int32_t* copies;       // [ncopies][3]
+  uint32_t ncopies;
+  const int32_t* tables;       // the rest: paged_keep_rows
+  uint64_t table_stride, keep_stride;
+  uint32_t max_blocks, max_keep, nseq;
+  const int32_t* lens;
+  const int32_t* keep;
+  const int32_t* counts;
+  int* status;
+};
+cudaError_t launch_copy_rows(const MoveParams& p, int num_sms, cudaStream_t stream);
+cudaError_t launch_keep_rows(const MoveParams& p, cudaStream_t stream);
+
+// paged_tree.cu: attention of several new tokens per request (see paged_tree_attention).
+constexpr uint32_t kTreeMaxCtas = 160;
+constexpr uint32_t kTreeNotesBytes = 16384;     // at the start of the workspace: what is left to be joined
+struct TreeParams {
+  uint8_t* base[2];
+  uint64_t block_stride[2];
+  uint32_t blocks[2];
+  uint32_t dtype, num_kv_heads, head_dim, block_tokens, block_shift;
+  const int32_t* tables;
+  uint64_t table_stride;
+  uint32_t max_blocks;
+  const int32_t* lens;         // [nseq]
+  const int32_t* offsets;      // [nseq + 1]
+  uint32_t nseq, ntok;
+  const uint8_t* q;            // [ntok] rows, strides in bytes
+  uint64_t q_stride;
+  uint8_t* out;
+  uint64_t out_stride;
+  float* lse;                  // [ntok][heads] or NULL
+  const uint32_t* mask;        // [ntok] rows of mask_words 32-bit words, mask_stride words apart; NULL: a chain
+  uint64_t mask_stride;
+  uint32_t mask_words;
+  const int32_t* positions;    // [ntok] or NULL
+  uint32_t group;              // query heads per KV head
+  uint32_t window;
+  float scale_log2;            // above 0
+  uint32_t q_keep, q_flip;
+  uint8_t* notes;              // kTreeNotesBytes
+  float* parts;
+  int* status;
+};
+size_t tree_workspace_bytes(uint32_t head_dim);
+cudaError_t launch_tree(const TreeParams& p, int dev, int num_sms, cudaStream_t stream);
 
 }  // namespace ema

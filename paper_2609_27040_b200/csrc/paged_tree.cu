@@ -1,0 +1,947 @@
+// paged_tree.cu — attention of several new tokens per request over a paged KV cache: the drafted tokens of speculative decoding (a
+// tree, given as a bit mask, or a chain) and pieces of prompts; tables, lengths and offsets read from device memory.
+//
+//   o = softmax(s q K^T) V over the context and those of the request's new tokens that the row sees, per query head.
+//
+// The query rows of one KV head (tokens x heads of the group) are tiles of 128, the M side of tcgen05 products; with one tile
+// the 64 KB of K and V of 128 positions (head_dim 128) take the tensor cores 1536 cycles and an SM's share of HBM about 2800,
+// with two tiles 3072: few drafted tokens are bound by HBM, two tiles by both about alike, prompts by the products.
+//   * An item is up to two tiles of one (request, KV head). The line of all items' positions, in steps of kTok, is cut into equal
+//     ranges, one to a CTA: an item may be cut, and its parts are joined by a second launch.
+//   * Warp 8 copies K and V (tiled bulk copies; the block format's order of 16-byte units within 128 bytes is the one that the
+//     tensor cores want, so a tile is used as it lies in the block), warp 9 issues the products, and two groups of four warps do the
+//     softmax, a row to a thread. Each group has a stream of its own: scores, weights and sums O in tensor memory. With two
+//     tiles a stream is a tile; with one, the streams take every other step and are added at the end. While one group works on
+//     its scores the tensor cores work for the other one. (head_dim 256: O takes half of the tensor memory, so there is one stream
+//     with two buffers for scores.)
+//   * Weights take the place of their scores in tensor memory, as the sum of two 16-bit numbers (error 2^-16 for bf16): one
+//     rounded weight would add an error as large as the output's own rounding. Sums and statistics are f32.
+//   * O is rescaled only when a row's maximum has grown by more than 2^kSlack; until then weights are larger than 1.
+#include <cuda.h>
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+
+#include <atomic>
+
+#include "kernels.h"
+#include "ptx.cuh"
+#include "tcgen05.cuh"
+
+namespace ema {
+
+namespace {
+
+constexpr float kMinusInf = -INFINITY;
+constexpr uint32_t kThreads = 320;                  // two groups of four warps, the copying warp, the issuing warp
+constexpr uint32_t kNotes = 4;
+
+template <uint32_t D>
+struct Shape {
+  static constexpr uint32_t kTok = D == 256 ? 64 : 128;      // positions of a step
+  static constexpr uint32_t kStreams = D == 256 ? 1 : 2;     // which is also the most tiles of an item
+  static constexpr uint32_t kRows = kStreams * 128;
+  static constexpr uint32_t kChunks = D / 64;                // pieces of 128 bytes of a head
+  static constexpr uint32_t kTileBytes = 128 * D * 2;        // of queries
+  static constexpr uint32_t kSlotBytes = kTok * D * 2;       // of K or of V
+  static constexpr uint32_t kSlots = D == 64 ? 12 : 5;
+  static constexpr uint32_t kO = 2 * kTok;                   // columns of tensor memory: two buffers of scores, then O
+  static constexpr uint32_t kPart = kRows * (D + 2);         // floats of a part: [D / 4][rows] float4, maxima, sums
+  static_assert(kO + kStreams * D <= 512, "tensor memory");
+};
+
+struct Maps {
+  CUtensorMap m[2];
+};
+
+// An item, or the part of it that a CTA does. tiles == 0: there are no more.
+struct Note {
+  uint32_t seq, head;
+  uint32_t off, m, c;           // the request's first token, how many, and the context before them
+  uint32_t tok0, ntok;          // those of the item
+  uint32_t hi, lo, lo_all;      // positions [lo, hi) are seen by some row; from lo_all on by all of them,
+  uint32_t full;                // up to here (less than that where a mask has the say)
+  uint32_t first, tiles;        // steps of kTok positions
+  uint32_t before;              // steps of this CTA before them
+  uint32_t slot;                // part, or ~0: the whole item
+};
+
+template <uint32_t D>
+struct Control {
+  using S = Shape<D>;
+  uint64_t full[S::kSlots], empty[S::kSlots];
+  uint64_t note_full[kNotes], note_empty[kNotes];
+  uint64_t q_full, o_empty, item, joint, drain;
+  uint64_t s_full[2], p_full[2], o_full[2], group[2];
+  Note note[kNotes];
+  uint32_t seen[2][2][4];       // positions of a step that some row sees: the groups' own, two steps' in turn
+  uint32_t tmem, dead;
+  unsigned long long warp_total[kThreads / 32];
+};
+
+template <uint32_t D>
+constexpr uint32_t tiles_bytes() {
+  return Shape<D>::kStreams * Shape<D>::kTileBytes + Shape<D>::kSlots * Shape<D>::kSlotBytes;
+}
+
+__device__ __forceinline__ void tma_box(uint32_t dst, const CUtensorMap* map, uint32_t y, uint32_t chunk, uint32_t block, uint32_t bar,
+                                        uint64_t policy) {
+  asm volatile(
+      "cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.L2::cache_hint [%0], [%1, {%2, %3, %4, %5}], "
+      "[%6], %7;" ::"r"(dst),
+      "l"(map), "r"(0), "r"(y), "r"(chunk), "r"(block), "r"(bar), "l"(policy)
+      : "memory");
+}
+
+template <bool kBf16>
+__device__ __forceinline__ uint32_t pack(float lo, float hi) {
+  if constexpr (kBf16) return ptx::pack_bf16x2(lo, hi);
+  uint32_t r;
+  asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+  return r;
+}
+
+template <bool kBf16>
+__device__ __forceinline__ float2 unpack(uint32_t v) {
+  if constexpr (kBf16) return make_float2(__uint_as_float(v << 16), __uint_as_float(v & 0xffff0000u));
+  return __half22float2(*reinterpret_cast<const __half2*>(&v));
+}
+
+// Weights are 2^kTop at a row's reference, and 2^(kTop + kSlack) at most: an fp16 number ends at 65504 and has no bits below 2^-24.
+template <bool kBf16>
+__device__ constexpr float kTop = kBf16 ? 0.f : 11.f;
+template <bool kBf16>
+__device__ constexpr float kSlack = kBf16 ? 8.f : 4.f;
+
+// Bounded wait; when it runs out nobody waits any more.
+template <typename Ctl>
+__device__ __forceinline__ bool wait(uint64_t& bar, uint32_t parity, Ctl& ctl, int* status) {
+  const uint32_t b = ptx::smem_u32(&bar);
+  if (ptx::mbar_try_wait(b, parity)) return true;
+  const uint64_t t0 = ptx::global_timer_ns();
+  for (uint32_t polls = 1;; ++polls) {
+    if (ptx::mbar_try_wait(b, parity)) return true;
+    if ((polls & 63u) == 0) {
+      if (*reinterpret_cast<volatile uint32_t*>(&ctl.dead)) return false;
+      if (ptx::global_timer_ns() - t0 > 2000000000ull) break;
+    }
+  }
+  *reinterpret_cast<volatile uint32_t*>(&ctl.dead) = 1;
+  ptx::report_status(status, kDevTimeout);
+  return false;
+}
+
+template <typename Ctl>
+__device__ __forceinline__ bool warp_wait(uint64_t& bar, uint32_t parity, Ctl& ctl, int* status) {
+  return __all_sync(0xffffffffu, wait(bar, parity, ctl, status));
+}
+
+__device__ __forceinline__ void arrive(uint64_t& bar) { ptx::mbar_arrive(ptx::smem_u32(&bar)); }
+
+struct Request {
+  uint32_t off, m, c;
+  bool ok;                      // lengths and offsets are in range
+};
+
+__device__ __forceinline__ Request request(const TreeParams& p, uint32_t i) {
+  const int32_t a = p.offsets[i], b = p.offsets[i + 1], n = p.lens[i];
+  Request r{};
+  r.ok = a >= 0 && b >= a && static_cast<uint32_t>(b) <= p.ntok && n >= 0 && static_cast<uint64_t>(n) <= static_cast<uint64_t>(p.max_blocks) * p.block_tokens &&
+         b - a <= n;
+  if (!r.ok) return r;
+  r.off = static_cast<uint32_t>(a);
+  r.m = static_cast<uint32_t>(b - a);
+  r.c = static_cast<uint32_t>(n) - r.m;
+  return r;
+}
+
+// Tokens of a tile and of an item.
+__device__ __forceinline__ uint32_t tile_tokens(const TreeParams& p) { return 128 / p.group; }
+
+struct Range {
+  uint32_t lo, hi, first, tiles;
+};
+
+// Item k of a request: what its rows see.
+template <uint32_t D>
+__device__ __forceinline__ Range range_of(const TreeParams& p, const Request& r, uint32_t k, uint32_t each) {
+  constexpr uint32_t kTok = Shape<D>::kTok;
+  const uint32_t t0 = k * each, t1 = min(r.m, t0 + each);
+  Range g;
+  g.hi = r.c + (p.mask ? r.m : t1);
+  const uint32_t pos = r.c + (p.positions ? 0 : t0);  // the least of the rows' positions, or below
+  g.lo = p.window && pos + 1 > p.window ? pos + 1 - p.window : 0;
+  if (p.mask) g.lo = min(g.lo, r.c);  // the mask says which new tokens are seen, however far back
+  g.first = g.lo / kTok;
+  g.tiles = (g.hi + kTok - 1) / kTok - g.first;
+  return g;
+}
+
+// Bits of the positions t .. t + 31 that the row of token j sees.
+struct Row {
+  const uint32_t* mask;
+  uint32_t lo, end;             // from here on; a chain: before here. A mask: context before c, new tokens by their bits
+  bool on;
+};
+
+__device__ __forceinline__ Row row_of(const TreeParams& p, const Note& n, uint32_t j, bool on) {
+  Row r{};
+  r.on = on;
+  if (!on) return r;
+  uint32_t pos = n.c + j;
+  if (p.positions) pos = static_cast<uint32_t>(max(static_cast<int64_t>(n.c), min(static_cast<int64_t>(p.positions[n.off + j]), static_cast<int64_t>(n.c) + n.m - 1)));
+  r.lo = p.window && pos + 1 > p.window ? pos + 1 - p.window : 0;
+  r.end = n.c + j + 1;
+  if (p.mask) {
+    r.mask = p.mask + static_cast<uint64_t>(n.off + j) * p.mask_stride;
+    r.lo = min(r.lo, n.c);
+    r.end = n.c + n.m;
+  }
+  return r;
+}
+
+__device__ __forceinline__ uint32_t below(int64_t n) { return n <= 0 ? 0u : n >= 32 ? ~0u : (1u << n) - 1; }
+
+__device__ __forceinline__ uint32_t visible(const TreeParams& p, const Row& r, uint32_t c, uint32_t t) {
+  if (!r.on) return 0;
+  uint32_t w = below(static_cast<int64_t>(r.end) - t) & ~below(static_cast<int64_t>(r.lo) - t);
+  if (r.mask) {
+    const uint32_t context = below(static_cast<int64_t>(c) - t);
+    uint32_t bits = 0;
+    if (context != ~0u && w) {
+      const int64_t b = static_cast<int64_t>(t) - c;  // the first of these new tokens, if it is one
+      const uint32_t i = b > 0 ? static_cast<uint32_t>(b >> 5) : 0;
+      const uint32_t w0 = i < p.mask_words ? r.mask[i] : 0;
+      if (b > 0)
+        bits = __funnelshift_r(w0, i + 1 < p.mask_words ? r.mask[i + 1] : 0, static_cast<uint32_t>(b) & 31u);
+      else
+        bits = w0 << static_cast<uint32_t>(-b);
+    }
+    w &= context | bits;
+  }
+  return w;
+}
+
+// The copying warp finds the CTA's items, tells the others, and copies K and V.
+template <uint32_t D>
+__device__ void feed(const TreeParams& p, const Maps& maps, Control<D>& ctl, uint8_t* slots, const unsigned long long* before, uint32_t size) {
+  using S = Shape<D>;
+  constexpr uint32_t kTok = S::kTok;
+  const uint32_t lane = threadIdx.x & 31u;
+  const uint64_t policy = ptx::policy_evict_first();
+  const uint32_t run = (p.nseq + kThreads - 1) / kThreads, each = S::kStreams * tile_tokens(p);
+  const uint64_t from = static_cast<uint64_t>(blockIdx.x) * size, to = from + size;
+  // The item in which the range begins.
+  uint32_t x = 0, n = kThreads;
+  while (n > 1) {
+    const uint32_t half = n >> 1;
+    if (before[x + half] <= from) x += half;
+    n -= half;
+  }
+  uint64_t at = before[x];
+  uint32_t seq = x * run, head = 0, k = 0, items = 0;
+  Request r{};
+  Range g{};
+  auto per_head = [&] {
+    uint64_t sum = 0;
+    for (uint32_t i = 0; i < items; ++i) sum += range_of<D>(p, r, i, each).tiles;
+    return sum;
+  };
+  for (; seq < p.nseq; ++seq) {
+    r = request(p, seq);
+    items = (r.m + each - 1) / each;
+    const uint64_t one = per_head(), all = one * p.num_kv_heads;
+    if (from < at + all) {
+      head = static_cast<uint32_t>((from - at) / one);
+      at += head * one;
+      for (;; ++k) {
+        g = range_of<D>(p, r, k, each);
+        if (from < at + g.tiles) break;
+        at += g.tiles;
+      }
+      break;
+    }
+    at += all;
+  }
+  int32_t* joins = reinterpret_cast<int32_t*>(p.notes) + blockIdx.x * 8;
+  uint32_t steps = 0, slot = 0, phase = 1;  // ring: next slot, parity of its being empty
+  bool goes_on = false, alive = true;
+  const uint32_t nb_shift = (kTok == 128 ? 7 : 6) - p.block_shift, blk = lane & ((1u << nb_shift) - 1), chunk = lane >> nb_shift;
+  for (uint32_t j = 0; alive; ++j) {
+    if (j >= kNotes) alive = warp_wait(ctl.note_empty[j % kNotes], (j / kNotes - 1) & 1u, ctl, p.status);
+    if (!alive) break;
+    Note& note = ctl.note[j % kNotes];
+    const bool have = seq < p.nseq && at < to;
+    if (!have) {
+      if (lane == 0) {
+        note.tiles = 0;
+        arrive(ctl.note_full[j % kNotes]);
+      }
+      break;
+    }
+    const uint32_t a = from > at ? static_cast<uint32_t>(from - at) : 0;
+    const uint32_t b = to < at + g.tiles ? static_cast<uint32_t>(to - at) : g.tiles;
+    const uint32_t tok0 = k * each, ntok = min(each, r.m - tok0);
+    if (lane == 0) {
+      note.seq = seq;
+      note.head = head;
+      note.off = r.off;
+      note.m = r.m;
+      note.c = r.c;
+      note.tok0 = tok0;
+      note.ntok = ntok;
+      note.hi = g.hi;
+      note.lo = g.lo;
+      const uint32_t last = r.c + (p.positions ? r.m : tok0 + ntok);  // behind the last of the rows' positions
+      note.lo_all = p.window && last > p.window ? last - p.window : 0;
+      note.full = r.c + (p.mask ? 0 : tok0 + 1);
+      note.first = g.first + a;
+      note.tiles = b - a;
+      note.before = steps;
+      note.slot = a ? 2 * blockIdx.x : b < g.tiles ? 2 * blockIdx.x + 1 : ~0u;
+      arrive(ctl.note_full[j % kNotes]);
+      if (a == 0 && b < g.tiles) {
+        goes_on = true;
+        joins[1] = static_cast<int32_t>(r.off + tok0);
+        joins[2] = static_cast<int32_t>(ntok);
+        joins[3] = static_cast<int32_t>(head);
+        joins[0] = static_cast<int32_t>((at + g.tiles - 1) / size - blockIdx.x + 1);
+      }
+    }
+    __syncwarp();
+    for (uint32_t t = a; t < b && alive; ++t, ++steps) {
+      const uint32_t pos = (g.first + t) * kTok + (blk << p.block_shift);
+      const bool on = chunk < S::kChunks && pos < g.hi && pos + p.block_tokens > g.lo;
+      int32_t entry = on ? p.tables[seq * p.table_stride + (pos >> p.block_shift)] : 0;
+      const uint32_t boxes = __ballot_sync(0xffffffffu, on);
+      const bool second = entry < 0;
+      const uint32_t blocks = second ? p.blocks[1] : p.blocks[0];
+      uint32_t id = static_cast<uint32_t>(second ? ~entry : entry);
+      if (on && id >= blocks) {  // a bad page: reads as zeros (a box outside the tensor), and is reported
+        ptx::report_status(p.status, kStatusInvalid);
+        id = blocks ? blocks : second ? p.blocks[0] : p.blocks[1];  // of an arena without blocks the map is the other one's
+      }
+      const CUtensorMap* map = second ? &maps.m[1] : &maps.m[0];
+#pragma unroll
+      for (uint32_t half = 0; half < 2; ++half) {
+        alive = alive && warp_wait(ctl.empty[slot], phase, ctl, p.status);
+        if (!alive) break;
+        const uint32_t bar = ptx::smem_u32(&ctl.full[slot]);
+        if (lane == 0) ptx::mbar_arrive_expect_tx(bar, __popc(boxes) << (p.block_shift + 7));
+        __syncwarp();
+        if (on)
+          tma_box(ptx::smem_u32(slots) + slot * S::kSlotBytes + chunk * (kTok * 128) + ((blk << p.block_shift) << 7), map,
+                  half ? p.block_tokens : 0, head * S::kChunks + chunk, id, bar, policy);
+        __syncwarp();
+        if (++slot == S::kSlots) {
+          slot = 0;
+          phase ^= 1;
+        }
+      }
+    }
+    // The next item.
+    at += g.tiles;
+    if (++k == items) {
+      k = 0;
+      if (++head == p.num_kv_heads) {
+        head = 0;
+        do {
+          ++seq;
+          r = seq < p.nseq ? request(p, seq) : Request{};
+        } while (seq < p.nseq && r.m == 0);
+        items = (r.m + each - 1) / each;
+      }
+    }
+    if (seq < p.nseq) g = range_of<D>(p, r, k, each);
+  }
+  if (lane == 0 && !goes_on) joins[0] = 0;
+  if (!alive)  // copies still in flight get a bounded time to land before the CTA's shared memory is given back
+    for (uint32_t s = 0; s < S::kSlots; ++s) ptx::mbar_wait(ptx::smem_u32(&ctl.full[s]), (s < slot ? phase ^ 1u : phase) & 1u, nullptr, 0);
+}
+
+// The issuing warp.
+template <uint32_t D, bool kBf16>
+__device__ void issue(const TreeParams& p, Control<D>& ctl, uint8_t* queries, uint8_t* slots) {
+  using S = Shape<D>;
+  constexpr uint32_t kTok = S::kTok;
+  constexpr uint32_t kScores = tc::product(kBf16, kTok, false), kSums = tc::product(kBf16, D, true);
+  const uint32_t lane = threadIdx.x & 31u, tmem = ctl.tmem;
+  const uint64_t q0 = tc::operand(ptx::smem_u32(queries), 16, 1024);
+  uint32_t p_parity = 0, slot = 0, phase = 0;  // K of step t lies in slot, V in the next one
+  bool alive = true;
+  for (uint32_t j = 0; alive; ++j) {
+    alive = warp_wait(ctl.note_full[j % kNotes], j / kNotes & 1u, ctl, p.status);
+    if (!alive) break;
+    const uint32_t tiles = ctl.note[j % kNotes].tiles;
+    const bool pair = S::kStreams == 2 && ctl.note[j % kNotes].ntok > tile_tokens(p);
+    if (tiles == 0) break;
+    __syncwarp();
+    if (lane == 0) arrive(ctl.note_empty[j % kNotes]);
+    alive = warp_wait(ctl.q_full, j & 1u, ctl, p.status);
+    if (alive && j) alive = warp_wait(ctl.o_empty, (j - 1) & 1u, ctl, p.status);
+    tc::fence_after();
+    const uint32_t units = pair ? 2 * tiles : tiles;
+    uint32_t k_slot = slot, k_phase = phase, v_slot = slot, v_phase = phase;
+    auto next = [](uint32_t& s, uint32_t& ph) {
+      if (++s == S::kSlots) {
+        s = 0;
+        ph ^= 1;
+      }
+    };
+    next(v_slot, v_phase);
+    for (uint32_t u = 0; u <= units && alive; ++u) {
+      if (u < units) {
+        if (!pair || !(u & 1u)) alive = warp_wait(ctl.full[k_slot], k_phase, ctl, p.status);
+        if (!alive) break;
+        tc::fence_after();
+        if (lane == 0) {
+          const uint64_t a = q0 + (pair && (u & 1u) ? S::kTileBytes >> 4 : 0);
+          const uint64_t b = tc::operand(ptx::smem_u32(slots) + k_slot * S::kSlotBytes, 16, 1024);
+#pragma unroll
+          for (uint32_t ks = 0; ks < D / 16; ++ks)
+            tc::mma_ss(tmem + (u & 1u) * kTok, a + (ks / 4) * (128 * 128 >> 4) + (ks % 4) * 2, b + (ks / 4) * (kTok * 128 >> 4) + (ks % 4) * 2, kScores,
+                       ks != 0);
+          tc::commit(ptx::smem_u32(&ctl.s_full[u & 1u]));
+          if (!pair || (u & 1u)) tc::commit(ptx::smem_u32(&ctl.empty[k_slot]));
+        }
+        __syncwarp();
+        if (!pair || (u & 1u)) {
+          next(k_slot, k_phase);
+          next(k_slot, k_phase);
+        }
+      }
+      if (u > 0) {
+        const uint32_t w = u - 1, buf = w & 1u, stream = S::kStreams == 2 ? buf : 0;
+        if (!pair || !(w & 1u)) alive = warp_wait(ctl.full[v_slot], v_phase, ctl, p.status);
+        alive = alive && warp_wait(ctl.p_full[buf], p_parity >> buf & 1u, ctl, p.status);
+        if (!alive) break;
+        p_parity ^= 1u << buf;
+        tc::fence_after();
+        if (lane == 0) {
+          const uint32_t o = tmem + S::kO + stream * D, weights = tmem + buf * kTok;
+          const uint64_t b = tc::operand(ptx::smem_u32(slots) + v_slot * S::kSlotBytes, kTok * 128, 1024);
+#pragma unroll
+          for (uint32_t part = 0; part < 2; ++part)
+#pragma unroll
+            for (uint32_t ks = 0; ks < kTok / 16; ++ks)
+              tc::mma_ts(o, weights + part * (kTok / 2) + ks * 8, b + ks * (16 * 128 >> 4), kSums, part || ks || w >= S::kStreams);
+          if (!pair || (w & 1u)) tc::commit(ptx::smem_u32(&ctl.empty[v_slot]));
+          if (S::kStreams == 1 || w + S::kStreams >= units) tc::commit(ptx::smem_u32(&ctl.o_full[stream]));
+        }
+        __syncwarp();
+        if (!pair || (w & 1u)) {
+          next(v_slot, v_phase);
+          next(v_slot, v_phase);
+        }
+      }
+    }
+    slot = k_slot;
+    phase = k_phase;
+  }
+  // Everything issued has been done before tensor and shared memory are given back.
+  if (lane == 0) {
+    tc::commit(ptx::smem_u32(&ctl.drain));
+    ptx::mbar_wait(ptx::smem_u32(&ctl.drain), 0, p.status, kDevTimeout);
+  }
+  __syncwarp();
+}
+
+__device__ __forceinline__ void touch(uint32_t* r) {
+#pragma unroll
+  for (uint32_t i = 0; i < 32; ++i) asm volatile("" : "+r"(r[i]));
+}
+
+// A group of four warps: queries in, softmax of its stream, rows out.
+template <uint32_t D, bool kBf16>
+__device__ void soften(const TreeParams& p, Control<D>& ctl, uint8_t* queries, uint8_t* slots) {
+  using S = Shape<D>;
+  constexpr uint32_t kTok = S::kTok, kWords = kTok / 32;
+  const uint32_t lane = threadIdx.x & 31u, x = threadIdx.x >> 7, r = threadIdx.x & 127u;
+  const uint32_t lanes = (r & ~31u) << 16;       // this warp's part of tensor memory
+  const uint32_t tmem = ctl.tmem + lanes;
+  const uint32_t G = p.group, tt = tile_tokens(p), in_tile = r / G, my_head = r - in_tile * G;
+  const bool packed = r < tt * G;                // rows behind the tile's last token are padding
+  const uint32_t heads = p.num_kv_heads * G;
+  float2* ml = reinterpret_cast<float2*>(queries + (S::kStreams - 1) * S::kTileBytes);  // [2][128]: the second tile's place, or nobody's by then
+  uint32_t s_parity = 0, o_count = 0, joint = 0, group = 0;
+  bool alive = true;
+  for (uint32_t j = 0; alive; ++j) {
+    alive = warp_wait(ctl.note_full[j % kNotes], j / kNotes & 1u, ctl, p.status);
+    if (!alive) break;
+    const Note n = ctl.note[j % kNotes];
+    if (n.tiles == 0) break;
+    const bool pair = S::kStreams == 2 && n.ntok > tt;
+    // Everybody is done with the item before.
+    __syncwarp();
+    if (lane == 0) arrive(ctl.item);
+    alive = warp_wait(ctl.item, j & 1u, ctl, p.status);
+    if (!alive) break;
+    {
+      constexpr uint32_t kUnits = D / 8;
+      const uint32_t tile = pair ? x : 0, row0 = pair ? 0 : x * 64, rows = pair ? 128 : 64;
+      uint8_t* dst = queries + tile * S::kTileBytes;
+      for (uint32_t i = r; i < rows * kUnits; i += 128) {
+        const uint32_t row = row0 + i / kUnits, u = i % kUnits, t = row / G, h = row - t * G, tok = tile * tt + t;
+        uint4 v = make_uint4(0, 0, 0, 0);
+        if (t < tt && tok < n.ntok) {
+          v = ptx::ld_once_v4(p.q + static_cast<uint64_t>(n.off + n.tok0 + tok) * p.q_stride + (static_cast<uint64_t>(n.head * G + h) * D + u * 8) * 2);
+          v.x = (v.x & p.q_keep) ^ p.q_flip;
+          v.y = (v.y & p.q_keep) ^ p.q_flip;
+          v.z = (v.z & p.q_keep) ^ p.q_flip;
+          v.w = (v.w & p.q_keep) ^ p.q_flip;
+        }
+        *reinterpret_cast<uint4*>(dst + (u / 8) * 16384 + row * 128 + ((u & 7u) ^ (row & 7u)) * 16) = v;
+      }
+      ptx::fence_proxy_async();
+      __syncwarp();
+      if (lane == 0) arrive(ctl.q_full);
+    }
+    const uint32_t my_tok = (pair ? x * tt : 0) + in_tile;
+    const bool mine = packed && my_tok < n.ntok;
+    const Row row = row_of(p, n, n.tok0 + my_tok, mine);
+    Row other{};                                 // of the second tile, whose V is the same
+    if (pair && x == 0) other = row_of(p, n, n.tok0 + tt + in_tile, packed && tt + in_tile < n.ntok);
+    float top = kMinusInf, sum = 0.f;            // reference of the row's weights, and their sum
+    const uint32_t units = pair ? 2 * n.tiles : n.tiles, stride = S::kStreams;
+    const uint32_t o_base = o_count;
+    const uint32_t taddr_o = tmem + S::kO + (S::kStreams == 2 ? x * D : 0);
+    const bool works = S::kStreams == 2 || x == 0;
+    uint32_t done = 0;                           // units of this stream
+    for (uint32_t u = x; works && u < units; u += stride, ++done) {
+      const uint32_t buf = u & 1u, kt = pair ? u >> 1 : u, t0 = (n.first + kt) * kTok;
+      alive = warp_wait(ctl.s_full[buf], s_parity >> buf & 1u, ctl, p.status);
+      if (!alive) break;
+      s_parity ^= 1u << buf;
+      tc::fence_after();
+      uint32_t s[kTok];
+#pragma unroll
+      for (uint32_t w = 0; w < kWords; ++w) tc::ld32(s + w * 32, tmem + buf * kTok + w * 32);
+      tc::wait_ld();
+#pragma unroll
+      for (uint32_t w = 0; w < kWords; ++w) touch(s + w * 32);
+      if (t0 < n.lo_all || t0 + kTok > n.full) {
+        uint32_t any[kWords];
+#pragma unroll
+        for (uint32_t w = 0; w < kWords; ++w) {
+          const uint32_t see = visible(p, row, n.c, t0 + w * 32);
+#pragma unroll
+          for (uint32_t i = 0; i < 32; ++i) s[w * 32 + i] = see >> i & 1u ? s[w * 32 + i] : __float_as_uint(kMinusInf);
+          any[w] = see;
+          if (pair && x == 0) any[w] |= visible(p, other, n.c, t0 + w * 32);
+        }
+        // Rows of V that no row of the item sees are made zeros, whatever they hold (a weight of 0 would not do). Of two tiles
+        // the first one's product comes first.
+        if (!pair || x == 0) {
+          uint32_t* seen = ctl.seen[x][group >> 1 & 1u];
+          if (r < kWords) seen[r] = 0;
+          __syncwarp();
+          if (lane == 0) arrive(ctl.group[x]);
+          alive = warp_wait(ctl.group[x], group++ & 1u, ctl, p.status);
+          if (!alive) break;
+#pragma unroll
+          for (uint32_t w = 0; w < kWords; ++w) {
+            const uint32_t all = __reduce_or_sync(0xffffffffu, any[w]);
+            if (lane == 0 && all) atomicOr(&seen[w], all);
+          }
+          __syncwarp();
+          if (lane == 0) arrive(ctl.group[x]);
+          alive = warp_wait(ctl.group[x], group++ & 1u, ctl, p.status);
+          if (!alive) break;
+          const uint32_t ring = 2 * (n.before + kt) + 1, slot = ring % S::kSlots;
+          alive = warp_wait(ctl.full[slot], ring / S::kSlots & 1u, ctl, p.status);
+          if (!alive) break;
+          if (r < kTok && !(seen[r / 32] >> (r & 31u) & 1u)) {
+#pragma unroll
+            for (uint32_t c = 0; c < S::kChunks; ++c)
+#pragma unroll
+              for (uint32_t i = 0; i < 8; ++i)
+                *reinterpret_cast<uint4*>(slots + slot * S::kSlotBytes + c * (kTok * 128) + r * 128 + i * 16) = make_uint4(0, 0, 0, 0);
+          }
+          ptx::fence_proxy_async();
+        }
+      }
+      float mx[4] = {kMinusInf, kMinusInf, kMinusInf, kMinusInf};
+#pragma unroll
+      for (uint32_t i = 0; i < kTok; ++i) mx[i & 3u] = fmaxf(mx[i & 3u], __uint_as_float(s[i]));
+      const float most = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
+      if (__any_sync(0xffffffffu, (most - top) * p.scale_log2 > kSlack<kBf16>)) {
+        const float now = fmaxf(top, most), al = now == kMinusInf ? 1.f : ptx::exp2_approx((top - now) * p.scale_log2);
+        top = now;
+        sum *= al;
+        if (done) {
+          // The stream's products so far have been done: of two streams, as the scores come after them; of one, the last may still run.
+          if (S::kStreams == 1) {
+            alive = warp_wait(ctl.o_full[0], (o_base + u - 1) & 1u, ctl, p.status);
+            if (!alive) break;
+            tc::fence_after();
+          }
+#pragma unroll 1
+          for (uint32_t c = 0; c < D; c += 32) {
+            uint32_t o[32];
+            tc::ld32(o, taddr_o + c);
+            tc::wait_ld();
+            touch(o);
+#pragma unroll
+            for (uint32_t i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * al);
+            tc::st32(taddr_o + c, o);
+          }
+          tc::wait_st();
+        }
+      }
+      const float ref = top == kMinusInf ? 0.f : top;
+      float sums[2] = {0.f, 0.f};
+#pragma unroll
+      for (uint32_t w = 0; w < kWords; ++w) {
+        uint32_t hi[16], lo[16];
+#pragma unroll
+        for (uint32_t i = 0; i < 16; ++i) {
+          const float a = ptx::exp2_approx(fmaf(__uint_as_float(s[w * 32 + 2 * i]) - ref, p.scale_log2, kTop<kBf16>));
+          const float b = ptx::exp2_approx(fmaf(__uint_as_float(s[w * 32 + 2 * i + 1]) - ref, p.scale_log2, kTop<kBf16>));
+          sums[0] += a;
+          sums[1] += b;
+          hi[i] = pack<kBf16>(a, b);
+          const float2 h = unpack<kBf16>(hi[i]);
+          lo[i] = pack<kBf16>(a - h.x, b - h.y);
+        }
+        tc::st16(tmem + buf * kTok + w * 16, hi);
+        tc::st16(tmem + buf * kTok + kTok / 2 + w * 16, lo);
+      }
+      sum += sums[0] + sums[1];
+      tc::wait_st();
+      tc::fence_before();
+      __syncwarp();
+      if (lane == 0) arrive(ctl.p_full[buf]);
+    }
+    if (!alive) break;
+    o_count += S::kStreams == 1 ? units : (done ? 1u : 0u);
+    if (works && done) {
+      // (Of one stream, the last product but one may still run as well, and a barrier tells only neighbouring phases apart.)
+      if (S::kStreams == 1 && done > 1) alive = warp_wait(ctl.o_full[0], (o_count - 2) & 1u, ctl, p.status);
+      alive = alive && warp_wait(ctl.o_full[S::kStreams == 2 ? x : 0], (o_count - 1) & 1u, ctl, p.status);
+      if (!alive) break;
+    }
+    float w0 = 1.f, w1 = 0.f;                    // of the streams' sums
+    uint32_t c0 = 0, c1 = D;                     // this group's columns
+    uint32_t o0 = S::kStreams == 2 ? x * D : 0;
+    if (!pair) {
+      if (works) ml[x * 128 + r] = make_float2(top, sum);
+      tc::fence_before();
+      __syncwarp();
+      if (lane == 0) arrive(ctl.joint);
+      alive = warp_wait(ctl.joint, joint++ & 1u, ctl, p.status);
+      if (!alive) break;
+      const float2 a = ml[r], b = S::kStreams == 2 ? ml[128 + r] : make_float2(kMinusInf, 0.f);
+      top = fmaxf(a.x, b.x);
+      const float ref = top == kMinusInf ? 0.f : top;
+      w0 = ptx::exp2_approx((a.x - ref) * p.scale_log2);
+      w1 = ptx::exp2_approx((b.x - ref) * p.scale_log2);
+      sum = a.y * w0 + b.y * w1;
+      o0 = 0;
+      c0 = x * (D / 2);
+      c1 = c0 + D / 2;
+    }
+    tc::fence_after();
+    const bool two = !pair && S::kStreams == 2 && units > 1;
+    const uint64_t tok = n.off + n.tok0 + my_tok;
+    const float inv = sum > 0.f ? 1.f / sum : sum;  // no weight at all: a row of zeros; not a number stays one
+    uint8_t* out = p.out + tok * p.out_stride + static_cast<uint64_t>(n.head * G + my_head) * D * 2;
+    const uint32_t part_row = pair ? x * 128 + r : r;
+    float4* part = reinterpret_cast<float4*>(p.parts + static_cast<uint64_t>(n.slot) * S::kPart);
+#pragma unroll 1
+    for (uint32_t c = c0; c < c1; c += 32) {
+      uint32_t o[32];
+      __syncwarp();
+      tc::ld32(o, tmem + S::kO + o0 + c);
+      if (two) {
+        uint32_t more[32];
+        tc::ld32(more, tmem + S::kO + D + c);
+        tc::wait_ld();
+        touch(o);
+        touch(more);
+#pragma unroll
+        for (uint32_t i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * w0 + __uint_as_float(more[i]) * w1);
+      } else {
+        tc::wait_ld();
+        touch(o);
+      }
+      if (!mine) continue;
+      if (n.slot == ~0u) {
+#pragma unroll
+        for (uint32_t i = 0; i < 4; ++i) {
+          uint32_t v[4];
+#pragma unroll
+          for (uint32_t e = 0; e < 4; ++e)
+            v[e] = pack<kBf16>(__uint_as_float(o[i * 8 + e * 2]) * inv, __uint_as_float(o[i * 8 + e * 2 + 1]) * inv);
+          *reinterpret_cast<uint4*>(out + (c + i * 8) * 2) = make_uint4(v[0], v[1], v[2], v[3]);
+        }
+      } else {
+#pragma unroll
+        for (uint32_t i = 0; i < 8; ++i)
+          part[(c / 4 + i) * S::kRows + part_row] = make_float4(__uint_as_float(o[i * 4]), __uint_as_float(o[i * 4 + 1]), __uint_as_float(o[i * 4 + 2]),
+                                                               __uint_as_float(o[i * 4 + 3]));
+      }
+    }
+    tc::fence_before();
+    __syncwarp();
+    if (lane == 0) {
+      arrive(ctl.o_empty);
+      arrive(ctl.note_empty[j % kNotes]);
+    }
+    if (mine && (pair || x == 0)) {
+      if (n.slot == ~0u) {
+        if (p.lse) p.lse[tok * heads + n.head * G + my_head] = fmaf(top, p.scale_log2, log2f(sum) - kTop<kBf16>) * 0.6931471805599453f;
+      } else {
+        float* stats = reinterpret_cast<float*>(part) + S::kRows * D;
+        stats[part_row] = top;
+        stats[S::kRows + part_row] = sum;
+      }
+    }
+  }
+}
+
+template <uint32_t D, bool kBf16>
+__global__ void __launch_bounds__(kThreads, 1) paged_tree_kernel(const TreeParams p, const __grid_constant__ Maps maps) {
+  using S = Shape<D>;
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* queries = smem_raw + ((1024u - (ptx::smem_u32(smem_raw) & 1023u)) & 1023u);
+  uint8_t* slots = queries + S::kStreams * S::kTileBytes;
+  Control<D>& ctl = *reinterpret_cast<Control<D>*>(slots + S::kSlots * S::kSlotBytes);
+  const uint32_t tid = threadIdx.x, warp = tid >> 5, lane = tid & 31u;
+  if (tid == 0) {
+    for (uint32_t s = 0; s < S::kSlots; ++s) {
+      ptx::mbar_init(ptx::smem_u32(&ctl.full[s]), 1);
+      ptx::mbar_init(ptx::smem_u32(&ctl.empty[s]), 1);
+    }
+    for (uint32_t s = 0; s < kNotes; ++s) {
+      ptx::mbar_init(ptx::smem_u32(&ctl.note_full[s]), 1);
+      ptx::mbar_init(ptx::smem_u32(&ctl.note_empty[s]), 9);
+    }
+    ptx::mbar_init(ptx::smem_u32(&ctl.q_full), 8);
+    ptx::mbar_init(ptx::smem_u32(&ctl.o_empty), 8);
+    ptx::mbar_init(ptx::smem_u32(&ctl.item), 8);
+    ptx::mbar_init(ptx::smem_u32(&ctl.joint), 8);
+    ptx::mbar_init(ptx::smem_u32(&ctl.drain), 1);
+    for (uint32_t s = 0; s < 2; ++s) {
+      ptx::mbar_init(ptx::smem_u32(&ctl.s_full[s]), 1);
+      ptx::mbar_init(ptx::smem_u32(&ctl.p_full[s]), 4);
+      ptx::mbar_init(ptx::smem_u32(&ctl.o_full[s]), 1);
+      ptx::mbar_init(ptx::smem_u32(&ctl.group[s]), 4);
+    }
+    ptx::fence_barrier_init();
+    asm volatile("prefetch.tensormap [%0];" ::"l"(&maps.m[0]));
+    asm volatile("prefetch.tensormap [%0];" ::"l"(&maps.m[1]));
+    ctl.dead = 0;
+  }
+  if (warp == 9) tc::alloc(ptx::smem_u32(&ctl.tmem), 512);
+  ptx::launch_dependents();
+  ptx::grid_dependency_wait();
+
+  // How the work is cut: steps before each thread's run of requests. The sums lie where the queries come later.
+  unsigned long long* before = reinterpret_cast<unsigned long long*>(queries);
+  const uint32_t run = (p.nseq + kThreads - 1) / kThreads, each = S::kStreams * tile_tokens(p);
+  const uint32_t i0 = min(tid * run, p.nseq), i1 = min(i0 + run, p.nseq);
+  unsigned long long mine = 0;
+  for (uint32_t i = i0; i < i1; ++i) {
+    const Request r = request(p, i);
+    unsigned long long one = 0;
+    for (uint32_t k = 0; k * each < r.m; ++k) one += range_of<D>(p, r, k, each).tiles;
+    mine += one * p.num_kv_heads;
+  }
+  unsigned long long inc = mine;
+#pragma unroll
+  for (int d = 1; d < 32; d <<= 1) {
+    const unsigned long long o = __shfl_up_sync(0xffffffffu, inc, d);
+    if (lane >= static_cast<uint32_t>(d)) inc += o;
+  }
+  if (lane == 31) ctl.warp_total[warp] = inc;
+  tc::fence_before();
+  __syncthreads();
+  tc::fence_after();
+  unsigned long long total = 0, sum = inc - mine;
+  for (uint32_t x = 0; x < kThreads / 32; ++x) {
+    if (x < warp) sum += ctl.warp_total[x];
+    total += ctl.warp_total[x];
+  }
+  before[tid] = sum;
+  // A part of less than two steps would leave a stream without work.
+  const unsigned long long share = (total + gridDim.x - 1) / gridDim.x;
+  const uint32_t size = static_cast<uint32_t>(min(max(share, 2ull), 0xffffffffull));
+  __syncthreads();
+
+  if (warp < 8)
+    soften<D, kBf16>(p, ctl, queries, slots);
+  else if (warp == 8)
+    feed<D>(p, maps, ctl, slots, before, size);
+  else
+    issue<D, kBf16>(p, ctl, queries, slots);
+
+  // Requests whose length or offsets are out of range: zeros, where the offsets name rows.
+  const uint32_t heads = p.num_kv_heads * p.group;
+  for (uint32_t i = blockIdx.x; i < p.nseq; i += gridDim.x) {
+    if (request(p, i).ok) continue;
+    if (tid == 0) ptx::report_status(p.status, kStatusInvalid);
+    const int32_t a = p.offsets[i], b = p.offsets[i + 1];
+    if (a < 0 || b < a || static_cast<uint32_t>(b) > p.ntok) continue;
+    for (uint32_t t = static_cast<uint32_t>(a); t < static_cast<uint32_t>(b); ++t) {
+      uint4* dst = reinterpret_cast<uint4*>(p.out + t * p.out_stride);
+      for (uint32_t x = tid; x < heads * D / 8; x += kThreads) dst[x] = make_uint4(0, 0, 0, 0);
+      if (p.lse)
+        for (uint32_t x = tid; x < heads; x += kThreads) p.lse[static_cast<uint64_t>(t) * heads + x] = kMinusInf;
+    }
+  }
+  tc::fence_before();
+  __syncthreads();
+  if (warp == 9) tc::dealloc(ctl.tmem, 512);
+}
+
+// Items that were cut: the sum of their parts, weighted by their references, and the division. A CTA takes 32 rows of an item's
+// part of the columns at a time.
+constexpr uint32_t kJoinThreads = 256;
+static_assert(kTreeMaxCtas <= kJoinThreads, "a thread for every CTA's item");
+
+template <uint32_t D, bool kBf16>
+__global__ void __launch_bounds__(kJoinThreads) tree_join_kernel(const TreeParams p, const uint32_t ctas) {
+  using S = Shape<D>;
+  __shared__ uint32_t list[kTreeMaxCtas], warp_count[kJoinThreads / 32];
+  __shared__ float weight[kTreeMaxCtas][32], total[32];
+  ptx::launch_dependents();
+  ptx::grid_dependency_wait();
+  const uint32_t tid = threadIdx.x, lane = tid & 31u, warp = tid >> 5;
+  const int32_t* notes = reinterpret_cast<const int32_t*>(p.notes);
+  const bool cut = tid < ctas && notes[tid * 8] > 0;  // in order: every CTA takes the same piece of the same item
+  const uint32_t ballot = __ballot_sync(0xffffffffu, cut);
+  if (lane == 0) warp_count[warp] = __popc(ballot);
+  __syncthreads();
+  uint32_t at = __popc(ballot & ((1u << lane) - 1)), count = 0;
+#pragma unroll
+  for (uint32_t w = 0; w < kJoinThreads / 32; ++w) {
+    if (w < warp) at += warp_count[w];
+    count += warp_count[w];
+  }
+  if (cut) list[at] = tid;
+  __syncthreads();
+  const uint32_t G = p.group, tt = tile_tokens(p), heads = p.num_kv_heads * G;
+  constexpr uint32_t kSlabs = S::kRows / 32;
+  const uint32_t tasks = count * kSlabs;
+  for (uint32_t x = blockIdx.x; x < tasks; x += gridDim.x) {
+    const uint32_t k = list[x / kSlabs], row = x % kSlabs * 32 + lane;
+    const uint32_t parts = static_cast<uint32_t>(notes[k * 8]), tok0 = static_cast<uint32_t>(notes[k * 8 + 1]), ntok = static_cast<uint32_t>(notes[k * 8 + 2]),
+                   head = static_cast<uint32_t>(notes[k * 8 + 3]);
+    const uint32_t tile = row >> 7, in_tile = (row & 127u) / G, h = (row & 127u) - in_tile * G, tok = tile * tt + in_tile;
+    const bool on = in_tile < tt && tok < ntok;
+    if (!__any_sync(0xffffffffu, on)) continue;  // the same for all warps
+    auto part = [&](uint32_t i) { return p.parts + static_cast<uint64_t>(i ? 2 * (k + i) : 2 * k + 1) * S::kPart; };
+    __syncthreads();
+    if (warp == 0) {
+      float most = kMinusInf, sum = 0.f;
+      if (on) {
+        for (uint32_t i = 0; i < parts; ++i) most = fmaxf(most, part(i)[S::kRows * D + row]);
+        const float ref = most == kMinusInf ? 0.f : most;
+        for (uint32_t i = 0; i < parts; ++i) {
+          const float w = ptx::exp2_approx((part(i)[S::kRows * D + row] - ref) * p.scale_log2);
+          weight[i][lane] = w;
+          sum += part(i)[S::kRows * (D + 1) + row] * w;
+        }
+        if (p.lse) p.lse[static_cast<uint64_t>(tok0 + tok) * heads + head * G + h] = fmaf(most, p.scale_log2, log2f(sum) - kTop<kBf16>) * 0.6931471805599453f;
+      }
+      total[lane] = sum > 0.f ? 1.f / sum : sum;
+    }
+    __syncthreads();
+    if (!on) continue;
+    uint8_t* out = p.out + static_cast<uint64_t>(tok0 + tok) * p.out_stride + static_cast<uint64_t>(head * G + h) * D * 2;
+    for (uint32_t c = warp; c < D / 4; c += kJoinThreads / 32) {
+      float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+      for (uint32_t i = 0; i < parts; ++i) {
+        const float4 v = reinterpret_cast<const float4*>(part(i))[c * S::kRows + row];
+        const float w = weight[i][lane];
+        acc.x = fmaf(v.x, w, acc.x);
+        acc.y = fmaf(v.y, w, acc.y);
+        acc.z = fmaf(v.z, w, acc.z);
+        acc.w = fmaf(v.w, w, acc.w);
+      }
+      const float inv = total[lane];
+      *reinterpret_cast<uint2*>(out + c * 8) = make_uint2(pack<kBf16>(acc.x * inv, acc.y * inv), pack<kBf16>(acc.z * inv, acc.w * inv));
+    }
+  }
+}
+
+using EncodeFn = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
+                              const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion,
+                              CUtensorMapFloatOOBfill);
+
+EncodeFn encode_fn() {
+  static const EncodeFn fn = []() -> EncodeFn {
+    void* f = nullptr;
+    cudaDriverEntryPointQueryResult r;
+    if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &f, 12000, cudaEnableDefault, &r) != cudaSuccess ||
+        r != cudaDriverEntryPointSuccess)
+      return nullptr;
+    return reinterpret_cast<EncodeFn>(f);
+  }();
+  return fn;
+}
+
+template <uint32_t D, bool kBf16>
+cudaError_t launch(const TreeParams& p, const Maps& maps, uint32_t grid, int dev, cudaStream_t stream) {
+  constexpr size_t kSharedBytes = tiles_bytes<D>() + 1024 + sizeof(Control<D>);
+  static_assert(kSharedBytes <= 232448, "one CTA per SM");
+  static std::atomic<bool> ready[64] = {};  // the attribute is a property of the function on one device; several threads may launch
+  if (!ready[dev].load(std::memory_order_acquire)) {
+    const cudaError_t e = cudaFuncSetAttribute(paged_tree_kernel<D, kBf16>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(kSharedBytes));
+    if (e != cudaSuccess) return e;
+    ready[dev].store(true, std::memory_order_release);
+  }
+  const cudaError_t e = launch_ahead(paged_tree_kernel<D, kBf16>, grid, kThreads, kSharedBytes, stream, p, maps);
+  if (e != cudaSuccess) return e;
+  return launch_ahead(tree_join_kernel<D, kBf16>, grid * 2, kJoinThreads, 0, stream, p, grid);
+}
+
+template <uint32_t D>
+cudaError_t launch_d(const TreeParams& p, const Maps& maps, uint32_t grid, int dev, cudaStream_t stream) {
+  return p.dtype == 0 ? launch<D, true>(p, maps, grid, dev, stream) : launch<D, false>(p, maps, grid, dev, stream);
+}
+
+}  // namespace
+
+size_t tree_workspace_bytes(uint32_t head_dim) {
+  const size_t part = head_dim == 64 ? Shape<64>::kPart : head_dim == 128 ? Shape<128>::kPart : Shape<256>::kPart;
+  static_assert(kTreeMaxCtas * 8 * 4 <= kTreeNotesBytes, "notes");
+  return kTreeNotesBytes + 2 * kTreeMaxCtas * part * sizeof(float);
+}
+
+cudaError_t launch_tree(const TreeParams& p, int dev, int num_sms, cudaStream_t stream) {
+  const EncodeFn encode = encode_fn();
+  if (!encode) return cudaErrorNotSupported;
+  Maps maps;
+  for (int j = 0; j < 2; ++j) {
+    if (j == 1 && (!p.blocks[0] || !p.blocks[1])) {  // one arena: one map serves both
+      maps.m[1] = maps.m[0];
+      break;
+    }
+    const int a = p.blocks[j] ? j : 1 - j;
+    const cuuint64_t chunks = static_cast<cuuint64_t>(p.num_kv_heads) * p.head_dim / 64;
+    const cuuint64_t dims[4] = {64, 2ull * p.block_tokens, chunks, p.blocks[a]};
+    const cuuint64_t strides[3] = {chunks * 128, 128, p.block_stride[a]};
+    const cuuint32_t box[4] = {64, p.block_tokens, 1, 1};
+    const cuuint32_t elem[4] = {1, 1, 1, 1};
+    auto make = [&] {
+      return encode(&maps.m[j], CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, p.base[a], dims, strides, box, elem, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                    CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    };
+    CUresult r = make();
+    // A thread that has not used the GPU yet: the runtime would make its device's context current at the launch, the driver's call needs it now.
+    if (r == CUDA_ERROR_INVALID_CONTEXT || r == CUDA_ERROR_NOT_INITIALIZED) {
+      const cudaError_t e = cudaSetDevice(dev);
+      if (e != cudaSuccess) return e;
+      r = make();
+    }
+    if (r != CUDA_SUCCESS) return cudaErrorInvalidValue;
+  }
+  const uint32_t sms = static_cast<uint32_t>(num_sms);
+  const uint32_t grid = sms < kTreeMaxCtas ? sms : kTreeMaxCtas;
+  if (p.head_dim == 64) return launch_d<64>(p, maps, grid, dev, stream);
+  if (p.head_dim == 128) return launch_d<128>(p, maps, grid, dev, stream);
+  return launch_d<256>(p, maps, grid, dev, stream);
+}
+
+}  // namespace ema
