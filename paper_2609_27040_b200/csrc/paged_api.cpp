@@ -311,7 +311,7 @@ int paged_tree_attention(const paged_tree_t* a, void* stream) {
   if (!a->tables || !a->lens || !a->offsets || !a->q || !a->out || !a->workspace || a->ntok > kMost || a->nseq > kMost - 1) return SLICE_EINVAL;
   if (a->max_blocks == 0 || a->table_stride < a->max_blocks || static_cast<uint64_t>(a->max_blocks) * c->block_tokens > kMost) return SLICE_EINVAL;
   const uint64_t row = static_cast<uint64_t>(a->num_heads) * c->head_dim * 2;
-  if ((a->ntok > 1 && (a->q_stride < row || a->out_stride < row)) || ((a->q_stride | a->out_stride) & 15u)) return SLICE_EINVAL;
+  if ((a->ntok > 1 && (a->q_stride < row || a->out_stride < row || a->q_stride >= (1ull << 40))) || ((a->q_stride | a->out_stride) & 15u)) return SLICE_EINVAL;
   if (!aligned(a->q, 16) || !aligned(a->out, 16) || !aligned(a->workspace, 16) || !aligned(a->tables, 4) || !aligned(a->lens, 4) ||
       !aligned(a->offsets, 4) || !aligned(a->lse, 4) || !aligned(a->mask, 8) || !aligned(a->positions, 4) || !aligned(a->status, 4))
     return SLICE_EINVAL;

@@ -32,8 +32,11 @@ namespace ema {
 namespace {
 
 constexpr float kMinusInf = -INFINITY;
-constexpr uint32_t kThreads = 320;                  // two groups of four warps, the copying warp, the issuing warp
+constexpr uint32_t kThreads = 384;                  // two groups of four warps; the copying warp, the issuing warp and two idle ones
 constexpr uint32_t kNotes = 4;
+// Registers of a thread: a row of scores takes 128. The launch has 168 for everybody; the third group of warps gives up what the others get.
+constexpr uint32_t kSoftRegs = 216, kOtherRegs = 72;
+static_assert(2 * kSoftRegs + kOtherRegs <= 3 * 168, "no more than the block was launched with");
 
 template <uint32_t D>
 struct Shape {
@@ -46,11 +49,13 @@ struct Shape {
   static constexpr uint32_t kSlots = D == 64 ? 12 : 5;
   static constexpr uint32_t kO = 2 * kTok;                   // columns of tensor memory: two buffers of scores, then O
   static constexpr uint32_t kPart = kRows * (D + 2);         // floats of a part: [D / 4][rows] float4, maxima, sums
+  static constexpr uint32_t kItem = 1;                       // steps that an item costs besides its own
   static_assert(kO + kStreams * D <= 512, "tensor memory");
 };
 
 struct Maps {
-  CUtensorMap m[2];
+  CUtensorMap m[2];             // K and V of either arena
+  CUtensorMap q;
 };
 
 // An item, or the part of it that a CTA does. tiles == 0: there are no more.
@@ -62,6 +67,7 @@ struct Note {
   uint32_t full;                // up to here (less than that where a mask has the say)
   uint32_t first, tiles;        // steps of kTok positions
   uint32_t before;              // steps of this CTA before them
+  uint32_t q;                   // where the queries of a single tile lie
   uint32_t slot;                // part, or ~0: the whole item
 };
 
@@ -70,10 +76,11 @@ struct Control {
   using S = Shape<D>;
   uint64_t full[S::kSlots], empty[S::kSlots];
   uint64_t note_full[kNotes], note_empty[kNotes];
-  uint64_t q_full, o_empty, item, joint, drain;
+  uint64_t q_full[2], q_empty[2], o_empty, joint, drain;
   uint64_t s_full[2], p_full[2], o_full[2], group[2];
   Note note[kNotes];
-  uint32_t seen[2][2][4];       // positions of a step that some row sees: the groups' own, two steps' in turn
+  uint32_t seen[2][2][4][4];    // positions of a step that some row sees: the groups' own, two steps' in turn, by warps
+  float2 stats[S::kStreams][128];  // references and sums of one tile's streams
   uint32_t tmem, dead;
   unsigned long long warp_total[kThreads / 32];
 };
@@ -90,6 +97,35 @@ __device__ __forceinline__ void tma_box(uint32_t dst, const CUtensorMap* map, ui
       "[%6], %7;" ::"r"(dst),
       "l"(map), "r"(0), "r"(y), "r"(chunk), "r"(block), "r"(bar), "l"(policy)
       : "memory");
+}
+
+__device__ __forceinline__ void tma_queries(uint32_t dst, const CUtensorMap* map, uint32_t x, uint32_t head, uint32_t token, uint32_t bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(dst),
+      "l"(map), "r"(x), "r"(head), "r"(token), "r"(bar)
+      : "memory");
+}
+
+// Two f32 numbers in one register pair: the pipes take both at a time.
+__device__ __forceinline__ uint64_t two(float a, float b) {
+  uint64_t r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+  return r;
+}
+__device__ __forceinline__ float2 each(uint64_t v) {
+  float2 r;
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(v));
+  return r;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+  uint64_t r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
 }
 
 template <bool kBf16>
@@ -199,31 +235,29 @@ __device__ __forceinline__ Row row_of(const TreeParams& p, const Note& n, uint32
   return r;
 }
 
-__device__ __forceinline__ uint32_t below(int64_t n) { return n <= 0 ? 0u : n >= 32 ? ~0u : (1u << n) - 1; }
+__device__ __forceinline__ uint32_t below(int32_t n) { return n <= 0 ? 0u : n >= 32 ? ~0u : (1u << n) - 1; }
 
-__device__ __forceinline__ uint32_t visible(const TreeParams& p, const Row& r, uint32_t c, uint32_t t) {
-  if (!r.on) return 0;
-  uint32_t w = below(static_cast<int64_t>(r.end) - t) & ~below(static_cast<int64_t>(r.lo) - t);
-  if (r.mask) {
-    const uint32_t context = below(static_cast<int64_t>(c) - t);
-    uint32_t bits = 0;
-    if (context != ~0u && w) {
-      const int64_t b = static_cast<int64_t>(t) - c;  // the first of these new tokens, if it is one
-      const uint32_t i = b > 0 ? static_cast<uint32_t>(b >> 5) : 0;
-      const uint32_t w0 = i < p.mask_words ? r.mask[i] : 0;
-      if (b > 0)
-        bits = __funnelshift_r(w0, i + 1 < p.mask_words ? r.mask[i + 1] : 0, static_cast<uint32_t>(b) & 31u);
-      else
-        bits = w0 << static_cast<uint32_t>(-b);
-    }
-    w &= context | bits;
+// Bit i of see[w]: the row sees position t0 + 32 w + i.
+template <uint32_t kWords>
+__device__ __forceinline__ void visible(const TreeParams& p, const Row& r, uint32_t c, uint32_t t0, uint32_t (&see)[kWords]) {
+  uint32_t bits[kWords + 1];
+  const int32_t b = static_cast<int32_t>(t0 - c);  // the first position as a new token, if it is one
+#pragma unroll
+  for (uint32_t w = 0; w <= kWords; ++w) {
+    const int32_t i = (b >> 5) + static_cast<int32_t>(w);
+    bits[w] = r.on && r.mask && i >= 0 && i < static_cast<int32_t>(p.mask_words) ? r.mask[i] : 0u;
   }
-  return w;
+#pragma unroll
+  for (uint32_t w = 0; w < kWords; ++w) {
+    const uint32_t t = t0 + 32 * w;
+    see[w] = r.on ? below(static_cast<int32_t>(r.end - t)) & ~below(static_cast<int32_t>(r.lo - t)) : 0u;
+    if (r.mask) see[w] &= below(static_cast<int32_t>(c - t)) | __funnelshift_r(bits[w], bits[w + 1], static_cast<uint32_t>(b) & 31u);
+  }
 }
 
 // The copying warp finds the CTA's items, tells the others, and copies K and V.
 template <uint32_t D>
-__device__ void feed(const TreeParams& p, const Maps& maps, Control<D>& ctl, uint8_t* slots, const unsigned long long* before, uint32_t size) {
+__device__ void feed(const TreeParams& p, const Maps& maps, Control<D>& ctl, uint8_t* queries, uint8_t* slots, const unsigned long long* before, uint32_t size) {
   using S = Shape<D>;
   constexpr uint32_t kTok = S::kTok;
   const uint32_t lane = threadIdx.x & 31u;
@@ -241,22 +275,19 @@ __device__ void feed(const TreeParams& p, const Maps& maps, Control<D>& ctl, uin
   uint32_t seq = x * run, head = 0, k = 0, items = 0;
   Request r{};
   Range g{};
-  auto per_head = [&] {
-    uint64_t sum = 0;
-    for (uint32_t i = 0; i < items; ++i) sum += range_of<D>(p, r, i, each).tiles;
-    return sum;
-  };
   for (; seq < p.nseq; ++seq) {
     r = request(p, seq);
     items = (r.m + each - 1) / each;
-    const uint64_t one = per_head(), all = one * p.num_kv_heads;
+    uint64_t one = 0;
+    for (uint32_t i = 0; i < items; ++i) one += range_of<D>(p, r, i, each).tiles + S::kItem;
+    const uint64_t all = one * p.num_kv_heads;
     if (from < at + all) {
       head = static_cast<uint32_t>((from - at) / one);
       at += head * one;
       for (;; ++k) {
         g = range_of<D>(p, r, k, each);
-        if (from < at + g.tiles) break;
-        at += g.tiles;
+        if (from < at + g.tiles + S::kItem) break;
+        at += g.tiles + S::kItem;
       }
       break;
     }
@@ -264,82 +295,113 @@ __device__ void feed(const TreeParams& p, const Maps& maps, Control<D>& ctl, uin
   }
   int32_t* joins = reinterpret_cast<int32_t*>(p.notes) + blockIdx.x * 8;
   uint32_t steps = 0, slot = 0, phase = 1;  // ring: next slot, parity of its being empty
+  uint32_t q_next = 0, q_parity = 3;        // where the next single tile's queries go; parities of either place being empty
   bool goes_on = false, alive = true;
   const uint32_t nb_shift = (kTok == 128 ? 7 : 6) - p.block_shift, blk = lane & ((1u << nb_shift) - 1), chunk = lane >> nb_shift;
-  for (uint32_t j = 0; alive; ++j) {
-    if (j >= kNotes) alive = warp_wait(ctl.note_empty[j % kNotes], (j / kNotes - 1) & 1u, ctl, p.status);
-    if (!alive) break;
-    Note& note = ctl.note[j % kNotes];
+  for (uint32_t j = 0; alive;) {
+    const uint32_t cost = g.tiles + S::kItem;
     const bool have = seq < p.nseq && at < to;
-    if (!have) {
+    // A cut inside the item's own cost lies at its beginning.
+    auto step_of = [&](uint64_t pos) { return pos <= S::kItem ? 0u : static_cast<uint32_t>(pos) - S::kItem; };
+    const uint32_t a = have && from > at ? step_of(from - at) : 0, b = have && to < at + cost ? step_of(to - at) : g.tiles;
+    if (!have || a < b) {
+      if (j >= kNotes) alive = warp_wait(ctl.note_empty[j % kNotes], (j / kNotes - 1) & 1u, ctl, p.status);
+      if (!alive) break;
+      Note& note = ctl.note[j % kNotes];
+      if (!have) {
+        if (lane == 0) {
+          note.tiles = 0;
+          arrive(ctl.note_full[j % kNotes]);
+        }
+        break;
+      }
+      const uint32_t tok0 = k * each, ntok = min(each, r.m - tok0);
+      const bool pair = S::kStreams == 2 && ntok > tile_tokens(p);
       if (lane == 0) {
-        note.tiles = 0;
+        note.seq = seq;
+        note.head = head;
+        note.off = r.off;
+        note.m = r.m;
+        note.c = r.c;
+        note.tok0 = tok0;
+        note.ntok = ntok;
+        note.hi = g.hi;
+        note.lo = g.lo;
+        const uint32_t last = r.c + (p.positions ? r.m : tok0 + ntok);  // behind the last of the rows' positions
+        note.lo_all = p.window && last > p.window ? last - p.window : 0;
+        note.full = r.c + (p.mask ? 0 : tok0 + 1);
+        note.first = g.first + a;
+        note.tiles = b - a;
+        note.before = steps;
+        note.q = q_next;
+        note.slot = a ? 2 * blockIdx.x : b < g.tiles ? 2 * blockIdx.x + 1 : ~0u;
         arrive(ctl.note_full[j % kNotes]);
-      }
-      break;
-    }
-    const uint32_t a = from > at ? static_cast<uint32_t>(from - at) : 0;
-    const uint32_t b = to < at + g.tiles ? static_cast<uint32_t>(to - at) : g.tiles;
-    const uint32_t tok0 = k * each, ntok = min(each, r.m - tok0);
-    if (lane == 0) {
-      note.seq = seq;
-      note.head = head;
-      note.off = r.off;
-      note.m = r.m;
-      note.c = r.c;
-      note.tok0 = tok0;
-      note.ntok = ntok;
-      note.hi = g.hi;
-      note.lo = g.lo;
-      const uint32_t last = r.c + (p.positions ? r.m : tok0 + ntok);  // behind the last of the rows' positions
-      note.lo_all = p.window && last > p.window ? last - p.window : 0;
-      note.full = r.c + (p.mask ? 0 : tok0 + 1);
-      note.first = g.first + a;
-      note.tiles = b - a;
-      note.before = steps;
-      note.slot = a ? 2 * blockIdx.x : b < g.tiles ? 2 * blockIdx.x + 1 : ~0u;
-      arrive(ctl.note_full[j % kNotes]);
-      if (a == 0 && b < g.tiles) {
-        goes_on = true;
-        joins[1] = static_cast<int32_t>(r.off + tok0);
-        joins[2] = static_cast<int32_t>(ntok);
-        joins[3] = static_cast<int32_t>(head);
-        joins[0] = static_cast<int32_t>((at + g.tiles - 1) / size - blockIdx.x + 1);
-      }
-    }
-    __syncwarp();
-    for (uint32_t t = a; t < b && alive; ++t, ++steps) {
-      const uint32_t pos = (g.first + t) * kTok + (blk << p.block_shift);
-      const bool on = chunk < S::kChunks && pos < g.hi && pos + p.block_tokens > g.lo;
-      int32_t entry = on ? p.tables[seq * p.table_stride + (pos >> p.block_shift)] : 0;
-      const uint32_t boxes = __ballot_sync(0xffffffffu, on);
-      const bool second = entry < 0;
-      const uint32_t blocks = second ? p.blocks[1] : p.blocks[0];
-      uint32_t id = static_cast<uint32_t>(second ? ~entry : entry);
-      if (on && id >= blocks) {  // a bad page: reads as zeros (a box outside the tensor), and is reported
-        ptx::report_status(p.status, kStatusInvalid);
-        id = blocks ? blocks : second ? p.blocks[0] : p.blocks[1];  // of an arena without blocks the map is the other one's
-      }
-      const CUtensorMap* map = second ? &maps.m[1] : &maps.m[0];
-#pragma unroll
-      for (uint32_t half = 0; half < 2; ++half) {
-        alive = alive && warp_wait(ctl.empty[slot], phase, ctl, p.status);
-        if (!alive) break;
-        const uint32_t bar = ptx::smem_u32(&ctl.full[slot]);
-        if (lane == 0) ptx::mbar_arrive_expect_tx(bar, __popc(boxes) << (p.block_shift + 7));
-        __syncwarp();
-        if (on)
-          tma_box(ptx::smem_u32(slots) + slot * S::kSlotBytes + chunk * (kTok * 128) + ((blk << p.block_shift) << 7), map,
-                  half ? p.block_tokens : 0, head * S::kChunks + chunk, id, bar, policy);
-        __syncwarp();
-        if (++slot == S::kSlots) {
-          slot = 0;
-          phase ^= 1;
+        if (a == 0 && b < g.tiles) {
+          goes_on = true;
+          joins[1] = static_cast<int32_t>(r.off + tok0);
+          joins[2] = static_cast<int32_t>(ntok);
+          joins[3] = static_cast<int32_t>(head);
+          joins[0] = static_cast<int32_t>((at + cost - 1) / size - blockIdx.x + 1);
         }
       }
+      __syncwarp();
+      // Queries: of a single tile, to the place that the item before the last one had; of two tiles (and of head_dim 256), when the last item's
+      // scores have been done, behind the first step's copies. A tile's rows are tokens x heads of the group; rows of tokens
+      // behind the item's last one are somebody's, and nobody's results.
+      auto ask = [&] {
+#pragma unroll
+        for (uint32_t i = 0; i < S::kStreams; ++i) {
+          const uint32_t place = pair ? i : q_next;
+          if (i && !pair) break;
+          alive = alive && warp_wait(ctl.q_empty[place], q_parity >> place & 1u, ctl, p.status);
+          if (!alive) return;
+          q_parity ^= 1u << place;
+          if (lane == 0) ptx::mbar_arrive_expect_tx(ptx::smem_u32(&ctl.q_full[place]), S::kChunks * tile_tokens(p) * p.group * 128);
+          __syncwarp();
+          if (lane < S::kChunks)
+            tma_queries(ptx::smem_u32(queries) + place * S::kTileBytes + lane * 16384, &maps.q, lane * 64, head * p.group,
+                        r.off + tok0 + i * tile_tokens(p), ptx::smem_u32(&ctl.q_full[place]));
+          __syncwarp();
+        }
+      };
+      const bool late = pair || S::kStreams == 1;
+      if (!late) ask();
+      for (uint32_t t = a; t < b && alive; ++t, ++steps) {
+        const uint32_t pos = (g.first + t) * kTok + (blk << p.block_shift);
+        const bool on = chunk < S::kChunks && pos < g.hi && pos + p.block_tokens > g.lo;
+        int32_t entry = on ? p.tables[seq * p.table_stride + (pos >> p.block_shift)] : 0;
+        const uint32_t boxes = __ballot_sync(0xffffffffu, on);
+        const bool second = entry < 0;
+        const uint32_t blocks = second ? p.blocks[1] : p.blocks[0];
+        uint32_t id = static_cast<uint32_t>(second ? ~entry : entry);
+        if (on && id >= blocks) {  // a bad page: reads as zeros (a box outside the tensor), and is reported
+          ptx::report_status(p.status, kStatusInvalid);
+          id = blocks ? blocks : second ? p.blocks[0] : p.blocks[1];  // of an arena without blocks the map is the other one's
+        }
+        const CUtensorMap* map = second ? &maps.m[1] : &maps.m[0];
+#pragma unroll
+        for (uint32_t half = 0; half < 2; ++half) {
+          alive = alive && warp_wait(ctl.empty[slot], phase, ctl, p.status);
+          if (!alive) break;
+          const uint32_t bar = ptx::smem_u32(&ctl.full[slot]);
+          if (lane == 0) ptx::mbar_arrive_expect_tx(bar, __popc(boxes) << (p.block_shift + 7));
+          __syncwarp();
+          if (on)
+            tma_box(ptx::smem_u32(slots) + slot * S::kSlotBytes + chunk * (kTok * 128) + ((blk << p.block_shift) << 7), map,
+                    half ? p.block_tokens : 0, head * S::kChunks + chunk, id, bar, policy);
+          __syncwarp();
+          if (++slot == S::kSlots) {
+            slot = 0;
+            phase ^= 1;
+          }
+        }
+        if (late && t == a && alive) ask();
+      }
+      if (S::kStreams == 2 && !pair) q_next ^= 1;
+      ++j;
     }
     // The next item.
-    at += g.tiles;
+    at += cost;
     if (++k == items) {
       k = 0;
       if (++head == p.num_kv_heads) {
@@ -354,95 +416,94 @@ __device__ void feed(const TreeParams& p, const Maps& maps, Control<D>& ctl, uin
     if (seq < p.nseq) g = range_of<D>(p, r, k, each);
   }
   if (lane == 0 && !goes_on) joins[0] = 0;
-  if (!alive)  // copies still in flight get a bounded time to land before the CTA's shared memory is given back
+  if (!alive) {  // copies still in flight get a bounded time to land before the CTA's shared memory is given back
     for (uint32_t s = 0; s < S::kSlots; ++s) ptx::mbar_wait(ptx::smem_u32(&ctl.full[s]), (s < slot ? phase ^ 1u : phase) & 1u, nullptr, 0);
+    for (uint32_t i = 0; i < 2; ++i) ptx::mbar_wait(ptx::smem_u32(&ctl.q_full[i]), q_parity >> i & 1u, nullptr, 0);
+  }
 }
 
-// The issuing warp.
+// The issuing thread. Scores of unit u, then the sums of unit u - 1: while a group works on its scores the tensor cores do the
+// other's. Products are done in the order in which they are issued, so that scores take the place of weights that were issued before.
 template <uint32_t D, bool kBf16>
 __device__ void issue(const TreeParams& p, Control<D>& ctl, uint8_t* queries, uint8_t* slots) {
   using S = Shape<D>;
   constexpr uint32_t kTok = S::kTok;
   constexpr uint32_t kScores = tc::product(kBf16, kTok, false), kSums = tc::product(kBf16, D, true);
-  const uint32_t lane = threadIdx.x & 31u, tmem = ctl.tmem;
+  const uint32_t tmem = ctl.tmem;
+  const uint32_t scores = kScores | (p.q_flip ? 1u << 13 : 0u);  // a scale below 0: queries with the other sign
   const uint64_t q0 = tc::operand(ptx::smem_u32(queries), 16, 1024);
-  uint32_t p_parity = 0, slot = 0, phase = 0;  // K of step t lies in slot, V in the next one
+  uint32_t p_parity = 0, q_parity = 0, slot = 0, phase = 0;  // K of step t lies in slot, V in the next one
   bool alive = true;
+  auto next = [](uint32_t& s, uint32_t& ph) {
+    if (++s == S::kSlots) {
+      s = 0;
+      ph ^= 1;
+    }
+  };
   for (uint32_t j = 0; alive; ++j) {
-    alive = warp_wait(ctl.note_full[j % kNotes], j / kNotes & 1u, ctl, p.status);
+    alive = wait(ctl.note_full[j % kNotes], j / kNotes & 1u, ctl, p.status);
     if (!alive) break;
-    const uint32_t tiles = ctl.note[j % kNotes].tiles;
+    const uint32_t tiles = ctl.note[j % kNotes].tiles, place = ctl.note[j % kNotes].q;
     const bool pair = S::kStreams == 2 && ctl.note[j % kNotes].ntok > tile_tokens(p);
     if (tiles == 0) break;
-    __syncwarp();
-    if (lane == 0) arrive(ctl.note_empty[j % kNotes]);
-    alive = warp_wait(ctl.q_full, j & 1u, ctl, p.status);
-    if (alive && j) alive = warp_wait(ctl.o_empty, (j - 1) & 1u, ctl, p.status);
-    tc::fence_after();
+    arrive(ctl.note_empty[j % kNotes]);
     const uint32_t units = pair ? 2 * tiles : tiles;
     uint32_t k_slot = slot, k_phase = phase, v_slot = slot, v_phase = phase;
-    auto next = [](uint32_t& s, uint32_t& ph) {
-      if (++s == S::kSlots) {
-        s = 0;
-        ph ^= 1;
-      }
-    };
     next(v_slot, v_phase);
-    for (uint32_t u = 0; u <= units && alive; ++u) {
+    for (uint32_t u = 0; u <= units; ++u) {
       if (u < units) {
-        if (!pair || !(u & 1u)) alive = warp_wait(ctl.full[k_slot], k_phase, ctl, p.status);
+        const bool last = !pair || (u & 1u);       // of the step's products with this tile of K
+        const uint32_t q = pair ? u & 1u : place;
+        if (u < (pair ? 2 : 1)) {
+          alive = wait(ctl.q_full[q], q_parity >> q & 1u, ctl, p.status);
+          q_parity ^= 1u << q;
+        }
+        if (alive && (!pair || !(u & 1u))) alive = wait(ctl.full[k_slot], k_phase, ctl, p.status);
         if (!alive) break;
         tc::fence_after();
-        if (lane == 0) {
-          const uint64_t a = q0 + (pair && (u & 1u) ? S::kTileBytes >> 4 : 0);
-          const uint64_t b = tc::operand(ptx::smem_u32(slots) + k_slot * S::kSlotBytes, 16, 1024);
+        const uint64_t a = q0 + q * (S::kTileBytes >> 4);
+        const uint64_t b = tc::operand(ptx::smem_u32(slots) + k_slot * S::kSlotBytes, 16, 1024);
 #pragma unroll
-          for (uint32_t ks = 0; ks < D / 16; ++ks)
-            tc::mma_ss(tmem + (u & 1u) * kTok, a + (ks / 4) * (128 * 128 >> 4) + (ks % 4) * 2, b + (ks / 4) * (kTok * 128 >> 4) + (ks % 4) * 2, kScores,
-                       ks != 0);
-          tc::commit(ptx::smem_u32(&ctl.s_full[u & 1u]));
-          if (!pair || (u & 1u)) tc::commit(ptx::smem_u32(&ctl.empty[k_slot]));
-        }
-        __syncwarp();
-        if (!pair || (u & 1u)) {
+        for (uint32_t ks = 0; ks < D / 16; ++ks)
+          tc::mma_ss(tmem + (u & 1u) * kTok, a + (ks / 4) * (128 * 128 >> 4) + (ks % 4) * 2, b + (ks / 4) * (kTok * 128 >> 4) + (ks % 4) * 2, scores,
+                     ks != 0);
+        tc::commit(ptx::smem_u32(&ctl.s_full[u & 1u]));
+        if (last) {
+          tc::commit(ptx::smem_u32(&ctl.empty[k_slot]));
           next(k_slot, k_phase);
           next(k_slot, k_phase);
         }
+        if (u + (pair ? 2 : 1) >= units) tc::commit(ptx::smem_u32(&ctl.q_empty[q]));
       }
       if (u > 0) {
         const uint32_t w = u - 1, buf = w & 1u, stream = S::kStreams == 2 ? buf : 0;
-        if (!pair || !(w & 1u)) alive = warp_wait(ctl.full[v_slot], v_phase, ctl, p.status);
-        alive = alive && warp_wait(ctl.p_full[buf], p_parity >> buf & 1u, ctl, p.status);
+        if (w == 0 && j) alive = wait(ctl.o_empty, (j - 1) & 1u, ctl, p.status);
+        if (alive && (!pair || !(w & 1u))) alive = wait(ctl.full[v_slot], v_phase, ctl, p.status);
+        alive = alive && wait(ctl.p_full[buf], p_parity >> buf & 1u, ctl, p.status);
         if (!alive) break;
         p_parity ^= 1u << buf;
         tc::fence_after();
-        if (lane == 0) {
-          const uint32_t o = tmem + S::kO + stream * D, weights = tmem + buf * kTok;
-          const uint64_t b = tc::operand(ptx::smem_u32(slots) + v_slot * S::kSlotBytes, kTok * 128, 1024);
+        const uint32_t o = tmem + S::kO + stream * D, weights = tmem + buf * kTok;
+        const uint64_t b = tc::operand(ptx::smem_u32(slots) + v_slot * S::kSlotBytes, kTok * 128, 1024);
 #pragma unroll
-          for (uint32_t part = 0; part < 2; ++part)
+        for (uint32_t part = 0; part < 2; ++part)
 #pragma unroll
-            for (uint32_t ks = 0; ks < kTok / 16; ++ks)
-              tc::mma_ts(o, weights + part * (kTok / 2) + ks * 8, b + ks * (16 * 128 >> 4), kSums, part || ks || w >= S::kStreams);
-          if (!pair || (w & 1u)) tc::commit(ptx::smem_u32(&ctl.empty[v_slot]));
-          if (S::kStreams == 1 || w + S::kStreams >= units) tc::commit(ptx::smem_u32(&ctl.o_full[stream]));
-        }
-        __syncwarp();
+          for (uint32_t ks = 0; ks < kTok / 16; ++ks)
+            tc::mma_ts(o, weights + part * (kTok / 2) + ks * 8, b + ks * (16 * 128 >> 4), kSums, part || ks || w >= S::kStreams);
         if (!pair || (w & 1u)) {
+          tc::commit(ptx::smem_u32(&ctl.empty[v_slot]));
           next(v_slot, v_phase);
           next(v_slot, v_phase);
         }
+        if (S::kStreams == 1 || w + S::kStreams >= units) tc::commit(ptx::smem_u32(&ctl.o_full[stream]));
       }
     }
     slot = k_slot;
     phase = k_phase;
   }
   // Everything issued has been done before tensor and shared memory are given back.
-  if (lane == 0) {
-    tc::commit(ptx::smem_u32(&ctl.drain));
-    ptx::mbar_wait(ptx::smem_u32(&ctl.drain), 0, p.status, kDevTimeout);
-  }
-  __syncwarp();
+  tc::commit(ptx::smem_u32(&ctl.drain));
+  ptx::mbar_wait(ptx::smem_u32(&ctl.drain), 0, p.status, kDevTimeout);
 }
 
 __device__ __forceinline__ void touch(uint32_t* r) {
@@ -452,7 +513,7 @@ __device__ __forceinline__ void touch(uint32_t* r) {
 
 // A group of four warps: queries in, softmax of its stream, rows out.
 template <uint32_t D, bool kBf16>
-__device__ void soften(const TreeParams& p, Control<D>& ctl, uint8_t* queries, uint8_t* slots) {
+__device__ void soften(const TreeParams& p, Control<D>& ctl, uint8_t* slots) {
   using S = Shape<D>;
   constexpr uint32_t kTok = S::kTok, kWords = kTok / 32;
   const uint32_t lane = threadIdx.x & 31u, x = threadIdx.x >> 7, r = threadIdx.x & 127u;
@@ -461,7 +522,6 @@ __device__ void soften(const TreeParams& p, Control<D>& ctl, uint8_t* queries, u
   const uint32_t G = p.group, tt = tile_tokens(p), in_tile = r / G, my_head = r - in_tile * G;
   const bool packed = r < tt * G;                // rows behind the tile's last token are padding
   const uint32_t heads = p.num_kv_heads * G;
-  float2* ml = reinterpret_cast<float2*>(queries + (S::kStreams - 1) * S::kTileBytes);  // [2][128]: the second tile's place, or nobody's by then
   uint32_t s_parity = 0, o_count = 0, joint = 0, group = 0;
   bool alive = true;
   for (uint32_t j = 0; alive; ++j) {
@@ -470,31 +530,6 @@ __device__ void soften(const TreeParams& p, Control<D>& ctl, uint8_t* queries, u
     const Note n = ctl.note[j % kNotes];
     if (n.tiles == 0) break;
     const bool pair = S::kStreams == 2 && n.ntok > tt;
-    // Everybody is done with the item before.
-    __syncwarp();
-    if (lane == 0) arrive(ctl.item);
-    alive = warp_wait(ctl.item, j & 1u, ctl, p.status);
-    if (!alive) break;
-    {
-      constexpr uint32_t kUnits = D / 8;
-      const uint32_t tile = pair ? x : 0, row0 = pair ? 0 : x * 64, rows = pair ? 128 : 64;
-      uint8_t* dst = queries + tile * S::kTileBytes;
-      for (uint32_t i = r; i < rows * kUnits; i += 128) {
-        const uint32_t row = row0 + i / kUnits, u = i % kUnits, t = row / G, h = row - t * G, tok = tile * tt + t;
-        uint4 v = make_uint4(0, 0, 0, 0);
-        if (t < tt && tok < n.ntok) {
-          v = ptx::ld_once_v4(p.q + static_cast<uint64_t>(n.off + n.tok0 + tok) * p.q_stride + (static_cast<uint64_t>(n.head * G + h) * D + u * 8) * 2);
-          v.x = (v.x & p.q_keep) ^ p.q_flip;
-          v.y = (v.y & p.q_keep) ^ p.q_flip;
-          v.z = (v.z & p.q_keep) ^ p.q_flip;
-          v.w = (v.w & p.q_keep) ^ p.q_flip;
-        }
-        *reinterpret_cast<uint4*>(dst + (u / 8) * 16384 + row * 128 + ((u & 7u) ^ (row & 7u)) * 16) = v;
-      }
-      ptx::fence_proxy_async();
-      __syncwarp();
-      if (lane == 0) arrive(ctl.q_full);
-    }
     const uint32_t my_tok = (pair ? x * tt : 0) + in_tile;
     const bool mine = packed && my_tok < n.ntok;
     const Row row = row_of(p, n, n.tok0 + my_tok, mine);
@@ -505,6 +540,7 @@ __device__ void soften(const TreeParams& p, Control<D>& ctl, uint8_t* queries, u
     const uint32_t o_base = o_count;
     const uint32_t taddr_o = tmem + S::kO + (S::kStreams == 2 ? x * D : 0);
     const bool works = S::kStreams == 2 || x == 0;
+    const bool simple = !p.mask && !p.positions;  // some row sees every position in [lo, hi)
     uint32_t done = 0;                           // units of this stream
     for (uint32_t u = x; works && u < units; u += stride, ++done) {
       const uint32_t buf = u & 1u, kt = pair ? u >> 1 : u, t0 = (n.first + kt) * kTok;
@@ -518,46 +554,45 @@ __device__ void soften(const TreeParams& p, Control<D>& ctl, uint8_t* queries, u
       tc::wait_ld();
 #pragma unroll
       for (uint32_t w = 0; w < kWords; ++w) touch(s + w * 32);
+      if (p.q_keep == 0) {                       // a scale of 0: queries of zeros
+#pragma unroll
+        for (uint32_t i = 0; i < kTok; ++i) s[i] = __float_as_uint(__uint_as_float(s[i]) * 0.f);
+      }
+      // Rows of V that no row of the item sees are made zeros, whatever they hold (a weight of 0 would not do). Of two tiles
+      // the first one's product comes first.
+      bool wipe = false, seen = false;
       if (t0 < n.lo_all || t0 + kTok > n.full) {
-        uint32_t any[kWords];
+        uint32_t see[kWords];
+        visible(p, row, n.c, t0, see);
 #pragma unroll
-        for (uint32_t w = 0; w < kWords; ++w) {
-          const uint32_t see = visible(p, row, n.c, t0 + w * 32);
+        for (uint32_t w = 0; w < kWords; ++w)
 #pragma unroll
-          for (uint32_t i = 0; i < 32; ++i) s[w * 32 + i] = see >> i & 1u ? s[w * 32 + i] : __float_as_uint(kMinusInf);
-          any[w] = see;
-          if (pair && x == 0) any[w] |= visible(p, other, n.c, t0 + w * 32);
-        }
-        // Rows of V that no row of the item sees are made zeros, whatever they hold (a weight of 0 would not do). Of two tiles
-        // the first one's product comes first.
-        if (!pair || x == 0) {
-          uint32_t* seen = ctl.seen[x][group >> 1 & 1u];
-          if (r < kWords) seen[r] = 0;
-          __syncwarp();
-          if (lane == 0) arrive(ctl.group[x]);
-          alive = warp_wait(ctl.group[x], group++ & 1u, ctl, p.status);
-          if (!alive) break;
+          for (uint32_t i = 0; i < 32; ++i) s[w * 32 + i] = see[w] >> i & 1u ? s[w * 32 + i] : __float_as_uint(kMinusInf);
+        if (simple) {
+          wipe = t0 < n.lo || t0 + kTok > n.hi;
+          seen = t0 + r >= n.lo && t0 + r < n.hi;
+        } else if (!pair || x == 0) {
+          wipe = true;
+          if (pair) {
+            uint32_t more[kWords];
+            visible(p, other, n.c, t0, more);
+#pragma unroll
+            for (uint32_t w = 0; w < kWords; ++w) see[w] |= more[w];
+          }
+          uint32_t(*by_warps)[4] = ctl.seen[x][group & 1u];
 #pragma unroll
           for (uint32_t w = 0; w < kWords; ++w) {
-            const uint32_t all = __reduce_or_sync(0xffffffffu, any[w]);
-            if (lane == 0 && all) atomicOr(&seen[w], all);
+            const uint32_t all = __reduce_or_sync(0xffffffffu, see[w]);
+            if (lane == 0) by_warps[r >> 5][w] = all;
           }
           __syncwarp();
           if (lane == 0) arrive(ctl.group[x]);
           alive = warp_wait(ctl.group[x], group++ & 1u, ctl, p.status);
           if (!alive) break;
-          const uint32_t ring = 2 * (n.before + kt) + 1, slot = ring % S::kSlots;
-          alive = warp_wait(ctl.full[slot], ring / S::kSlots & 1u, ctl, p.status);
-          if (!alive) break;
-          if (r < kTok && !(seen[r / 32] >> (r & 31u) & 1u)) {
-#pragma unroll
-            for (uint32_t c = 0; c < S::kChunks; ++c)
-#pragma unroll
-              for (uint32_t i = 0; i < 8; ++i)
-                *reinterpret_cast<uint4*>(slots + slot * S::kSlotBytes + c * (kTok * 128) + r * 128 + i * 16) = make_uint4(0, 0, 0, 0);
-          }
-          ptx::fence_proxy_async();
+          const uint32_t w = r / 32 % kWords;
+          seen = (by_warps[0][w] | by_warps[1][w] | by_warps[2][w] | by_warps[3][w]) >> lane & 1u;
         }
+        wipe = wipe && (!pair || x == 0);
       }
       float mx[4] = {kMinusInf, kMinusInf, kMinusInf, kMinusInf};
 #pragma unroll
@@ -588,24 +623,41 @@ __device__ void soften(const TreeParams& p, Control<D>& ctl, uint8_t* queries, u
         }
       }
       const float ref = top == kMinusInf ? 0.f : top;
-      float sums[2] = {0.f, 0.f};
+      const uint64_t ref2 = two(-ref, -ref), scale2 = two(p.scale_log2, p.scale_log2), top2 = two(kTop<kBf16>, kTop<kBf16>), minus2 = two(-1.f, -1.f);
+      uint64_t sums[2] = {0, 0};
 #pragma unroll
       for (uint32_t w = 0; w < kWords; ++w) {
         uint32_t hi[16], lo[16];
 #pragma unroll
         for (uint32_t i = 0; i < 16; ++i) {
-          const float a = ptx::exp2_approx(fmaf(__uint_as_float(s[w * 32 + 2 * i]) - ref, p.scale_log2, kTop<kBf16>));
-          const float b = ptx::exp2_approx(fmaf(__uint_as_float(s[w * 32 + 2 * i + 1]) - ref, p.scale_log2, kTop<kBf16>));
-          sums[0] += a;
-          sums[1] += b;
+          // (The difference is taken first: of scores beyond 2^24 the rounding of a score times the scale would be more than an exponent's worth.)
+          const float2 e = each(fma2(add2(two(__uint_as_float(s[w * 32 + 2 * i]), __uint_as_float(s[w * 32 + 2 * i + 1])), ref2), scale2, top2));
+          const float a = ptx::exp2_approx(e.x), b = ptx::exp2_approx(e.y);
+          const uint64_t ab = two(a, b);
+          sums[i & 1u] = add2(sums[i & 1u], ab);
           hi[i] = pack<kBf16>(a, b);
           const float2 h = unpack<kBf16>(hi[i]);
-          lo[i] = pack<kBf16>(a - h.x, b - h.y);
+          const float2 left = each(fma2(two(h.x, h.y), minus2, ab));
+          lo[i] = pack<kBf16>(left.x, left.y);
         }
         tc::st16(tmem + buf * kTok + w * 16, hi);
         tc::st16(tmem + buf * kTok + kTok / 2 + w * 16, lo);
       }
-      sum += sums[0] + sums[1];
+      const float2 both = each(add2(sums[0], sums[1]));
+      sum += both.x + both.y;
+      if (wipe) {
+        const uint32_t ring = 2 * (n.before + kt) + 1, slot = ring % S::kSlots;
+        alive = warp_wait(ctl.full[slot], ring / S::kSlots & 1u, ctl, p.status);
+        if (!alive) break;
+        if (r < kTok && !seen) {
+#pragma unroll
+          for (uint32_t c = 0; c < S::kChunks; ++c)
+#pragma unroll
+            for (uint32_t i = 0; i < 8; ++i)
+              *reinterpret_cast<uint4*>(slots + slot * S::kSlotBytes + c * (kTok * 128) + r * 128 + i * 16) = make_uint4(0, 0, 0, 0);
+        }
+        ptx::fence_proxy_async();
+      }
       tc::wait_st();
       tc::fence_before();
       __syncwarp();
@@ -623,13 +675,13 @@ __device__ void soften(const TreeParams& p, Control<D>& ctl, uint8_t* queries, u
     uint32_t c0 = 0, c1 = D;                     // this group's columns
     uint32_t o0 = S::kStreams == 2 ? x * D : 0;
     if (!pair) {
-      if (works) ml[x * 128 + r] = make_float2(top, sum);
+      if (done) ctl.stats[S::kStreams == 2 ? x : 0][r] = make_float2(top, sum);
       tc::fence_before();
       __syncwarp();
       if (lane == 0) arrive(ctl.joint);
       alive = warp_wait(ctl.joint, joint++ & 1u, ctl, p.status);
       if (!alive) break;
-      const float2 a = ml[r], b = S::kStreams == 2 ? ml[128 + r] : make_float2(kMinusInf, 0.f);
+      const float2 a = ctl.stats[0][r], b = S::kStreams == 2 && units > 1 ? ctl.stats[S::kStreams - 1][r] : make_float2(kMinusInf, 0.f);
       top = fmaxf(a.x, b.x);
       const float ref = top == kMinusInf ? 0.f : top;
       w0 = ptx::exp2_approx((a.x - ref) * p.scale_log2);
@@ -701,8 +753,8 @@ __device__ void soften(const TreeParams& p, Control<D>& ctl, uint8_t* queries, u
 template <uint32_t D, bool kBf16>
 __global__ void __launch_bounds__(kThreads, 1) paged_tree_kernel(const TreeParams p, const __grid_constant__ Maps maps) {
   using S = Shape<D>;
-  extern __shared__ uint8_t smem_raw[];
-  uint8_t* queries = smem_raw + ((1024u - (ptx::smem_u32(smem_raw) & 1023u)) & 1023u);
+  extern __shared__ __align__(1024) uint8_t smem_raw[];
+  uint8_t* queries = smem_raw;
   uint8_t* slots = queries + S::kStreams * S::kTileBytes;
   Control<D>& ctl = *reinterpret_cast<Control<D>*>(slots + S::kSlots * S::kSlotBytes);
   const uint32_t tid = threadIdx.x, warp = tid >> 5, lane = tid & 31u;
@@ -715,12 +767,12 @@ __global__ void __launch_bounds__(kThreads, 1) paged_tree_kernel(const TreeParam
       ptx::mbar_init(ptx::smem_u32(&ctl.note_full[s]), 1);
       ptx::mbar_init(ptx::smem_u32(&ctl.note_empty[s]), 9);
     }
-    ptx::mbar_init(ptx::smem_u32(&ctl.q_full), 8);
     ptx::mbar_init(ptx::smem_u32(&ctl.o_empty), 8);
-    ptx::mbar_init(ptx::smem_u32(&ctl.item), 8);
     ptx::mbar_init(ptx::smem_u32(&ctl.joint), 8);
     ptx::mbar_init(ptx::smem_u32(&ctl.drain), 1);
     for (uint32_t s = 0; s < 2; ++s) {
+      ptx::mbar_init(ptx::smem_u32(&ctl.q_full[s]), 1);
+      ptx::mbar_init(ptx::smem_u32(&ctl.q_empty[s]), 1);
       ptx::mbar_init(ptx::smem_u32(&ctl.s_full[s]), 1);
       ptx::mbar_init(ptx::smem_u32(&ctl.p_full[s]), 4);
       ptx::mbar_init(ptx::smem_u32(&ctl.o_full[s]), 1);
@@ -729,6 +781,7 @@ __global__ void __launch_bounds__(kThreads, 1) paged_tree_kernel(const TreeParam
     ptx::fence_barrier_init();
     asm volatile("prefetch.tensormap [%0];" ::"l"(&maps.m[0]));
     asm volatile("prefetch.tensormap [%0];" ::"l"(&maps.m[1]));
+    asm volatile("prefetch.tensormap [%0];" ::"l"(&maps.q));
     ctl.dead = 0;
   }
   if (warp == 9) tc::alloc(ptx::smem_u32(&ctl.tmem), 512);
@@ -743,7 +796,7 @@ __global__ void __launch_bounds__(kThreads, 1) paged_tree_kernel(const TreeParam
   for (uint32_t i = i0; i < i1; ++i) {
     const Request r = request(p, i);
     unsigned long long one = 0;
-    for (uint32_t k = 0; k * each < r.m; ++k) one += range_of<D>(p, r, k, each).tiles;
+    for (uint32_t k = 0; k * each < r.m; ++k) one += range_of<D>(p, r, k, each).tiles + S::kItem;
     mine += one * p.num_kv_heads;
   }
   unsigned long long inc = mine;
@@ -764,15 +817,20 @@ __global__ void __launch_bounds__(kThreads, 1) paged_tree_kernel(const TreeParam
   before[tid] = sum;
   // A part of less than two steps would leave a stream without work.
   const unsigned long long share = (total + gridDim.x - 1) / gridDim.x;
-  const uint32_t size = static_cast<uint32_t>(min(max(share, 2ull), 0xffffffffull));
+  const uint32_t size = static_cast<uint32_t>(min(max(share, 2ull + S::kItem), 0xffffffffull));
   __syncthreads();
 
-  if (warp < 8)
-    soften<D, kBf16>(p, ctl, queries, slots);
-  else if (warp == 8)
-    feed<D>(p, maps, ctl, slots, before, size);
-  else
-    issue<D, kBf16>(p, ctl, queries, slots);
+  if (warp < 8) {
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoftRegs));
+    soften<D, kBf16>(p, ctl, slots);
+  } else {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
+    if (warp == 8)
+      feed<D>(p, maps, ctl, queries, slots, before, size);
+    else if (warp == 9 && lane == 0)
+      issue<D, kBf16>(p, ctl, queries, slots);
+    __syncwarp();
+  }
 
   // Requests whose length or offsets are out of range: zeros, where the offsets name rows.
   const uint32_t heads = p.num_kv_heads * p.group;
@@ -883,7 +941,7 @@ EncodeFn encode_fn() {
 
 template <uint32_t D, bool kBf16>
 cudaError_t launch(const TreeParams& p, const Maps& maps, uint32_t grid, int dev, cudaStream_t stream) {
-  constexpr size_t kSharedBytes = tiles_bytes<D>() + 1024 + sizeof(Control<D>);
+  constexpr size_t kSharedBytes = tiles_bytes<D>() + sizeof(Control<D>);
   static_assert(kSharedBytes <= 232448, "one CTA per SM");
   static std::atomic<bool> ready[64] = {};  // the attribute is a property of the function on one device; several threads may launch
   if (!ready[dev].load(std::memory_order_acquire)) {
@@ -936,6 +994,17 @@ cudaError_t launch_tree(const TreeParams& p, int dev, int num_sms, cudaStream_t 
       r = make();
     }
     if (r != CUDA_SUCCESS) return cudaErrorInvalidValue;
+  }
+  {
+    const uint32_t heads = p.num_kv_heads * p.group;
+    const cuuint64_t dims[3] = {p.head_dim, heads, p.ntok};
+    // of one token there is no next one
+    const cuuint64_t strides[2] = {p.head_dim * 2ull, p.ntok > 1 ? p.q_stride : static_cast<cuuint64_t>(heads) * p.head_dim * 2};
+    const cuuint32_t box[3] = {64, p.group, 128 / p.group};
+    const cuuint32_t elem[3] = {1, 1, 1};
+    if (encode(&maps.q, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<uint8_t*>(p.q), dims, strides, box, elem, CU_TENSOR_MAP_INTERLEAVE_NONE,
+               CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
+      return cudaErrorInvalidValue;
   }
   const uint32_t sms = static_cast<uint32_t>(num_sms);
   const uint32_t grid = sms < kTreeMaxCtas ? sms : kTreeMaxCtas;
