@@ -32,11 +32,8 @@ namespace ema {
 namespace {
 
 constexpr float kMinusInf = -INFINITY;
-constexpr uint32_t kThreads = 384;                  // two groups of four warps; the copying warp, the issuing warp and two idle ones
+constexpr uint32_t kThreads = 352;                  // two groups of four warps, two copying warps, the issuing warp
 constexpr uint32_t kNotes = 4;
-// Registers of a thread: a row of scores takes 128. The launch has 168 for everybody; the third group of warps gives up what the others get.
-constexpr uint32_t kSoftRegs = 216, kOtherRegs = 72;
-static_assert(2 * kSoftRegs + kOtherRegs <= 3 * 168, "no more than the block was launched with");
 
 template <uint32_t D>
 struct Shape {
@@ -212,10 +209,11 @@ __device__ __forceinline__ Range range_of(const TreeParams& p, const Request& r,
   return g;
 }
 
-// Bits of the positions t .. t + 31 that the row of token j sees.
+// What the row of a token sees: positions [lo, end), of which a mask takes away new tokens.
 struct Row {
-  const uint32_t* mask;
-  uint32_t lo, end;             // from here on; a chain: before here. A mask: context before c, new tokens by their bits
+  const uint32_t* mask;         // NULL: there is none
+  uint32_t bits[2];             // its first two words (all of it for requests of up to 64 new tokens), read before they are wanted
+  uint32_t lo, end;
   bool on;
 };
 
@@ -229,6 +227,9 @@ __device__ __forceinline__ Row row_of(const TreeParams& p, const Note& n, uint32
   r.end = n.c + j + 1;
   if (p.mask) {
     r.mask = p.mask + static_cast<uint64_t>(n.off + j) * p.mask_stride;
+    const uint2 v = *reinterpret_cast<const uint2*>(r.mask);
+    r.bits[0] = v.x;
+    r.bits[1] = v.y;
     r.lo = min(r.lo, n.c);
     r.end = n.c + n.m;
   }
@@ -237,26 +238,34 @@ __device__ __forceinline__ Row row_of(const TreeParams& p, const Note& n, uint32
 
 __device__ __forceinline__ uint32_t below(int32_t n) { return n <= 0 ? 0u : n >= 32 ? ~0u : (1u << n) - 1; }
 
-// Bit i of see[w]: the row sees position t0 + 32 w + i.
-template <uint32_t kWords>
-__device__ __forceinline__ void visible(const TreeParams& p, const Row& r, uint32_t c, uint32_t t0, uint32_t (&see)[kWords]) {
-  uint32_t bits[kWords + 1];
-  const int32_t b = static_cast<int32_t>(t0 - c);  // the first position as a new token, if it is one
-#pragma unroll
-  for (uint32_t w = 0; w <= kWords; ++w) {
-    const int32_t i = (b >> 5) + static_cast<int32_t>(w);
-    bits[w] = r.on && r.mask && i >= 0 && i < static_cast<int32_t>(p.mask_words) ? r.mask[i] : 0u;
+// Bit i: the row sees position t + i.
+__device__ __forceinline__ uint32_t visible(const TreeParams& p, const Row& r, uint32_t c, uint32_t t) {
+  if (!r.on) return 0;
+  uint32_t see = below(static_cast<int32_t>(r.end - t)) & ~below(static_cast<int32_t>(r.lo - t));
+  if (r.mask) {
+    const int32_t b = static_cast<int32_t>(t - c), i = b >> 5;  // the first position as a new token, if it is one, and its word
+    uint32_t w0, w1;
+    if (p.mask_words == 2) {
+      w0 = i == 0 ? r.bits[0] : i == 1 ? r.bits[1] : 0u;
+      w1 = i == -1 ? r.bits[0] : i == 0 ? r.bits[1] : 0u;
+    } else {
+      w0 = i >= 0 && i < static_cast<int32_t>(p.mask_words) ? r.mask[i] : 0u;
+      w1 = i >= -1 && i + 1 < static_cast<int32_t>(p.mask_words) ? r.mask[i + 1] : 0u;
+    }
+    see &= below(static_cast<int32_t>(c - t)) | __funnelshift_r(w0, w1, static_cast<uint32_t>(b) & 31u);
   }
-#pragma unroll
-  for (uint32_t w = 0; w < kWords; ++w) {
-    const uint32_t t = t0 + 32 * w;
-    see[w] = r.on ? below(static_cast<int32_t>(r.end - t)) & ~below(static_cast<int32_t>(r.lo - t)) : 0u;
-    if (r.mask) see[w] &= below(static_cast<int32_t>(c - t)) | __funnelshift_r(bits[w], bits[w + 1], static_cast<uint32_t>(b) & 31u);
-  }
+  return see;
 }
 
-// The copying warp finds the CTA's items, tells the others, and copies K and V.
-template <uint32_t D>
+// Places in the ring of K and V tiles, in the order in which the products take them, which is the order in which they come free: of an
+// item of n steps K0 V0 K1 V1 .. with two tiles of queries; with one, whose scores are a step ahead of its sums, K0 K1 V0 K2 V1 ..
+// (In the order K0 V0 K1 .. a tile of V would lie there for the time of a softmax before it is used.)
+__device__ __forceinline__ uint32_t k_place(uint32_t t, bool pair) { return pair ? 2 * t : t ? 2 * t - 1 : 0; }
+__device__ __forceinline__ uint32_t v_place(uint32_t t, uint32_t n, bool pair) { return pair || t + 1 == n ? 2 * t + 1 : 2 * t + 2; }
+
+// The copying warps find the CTA's items. One tells the others about them and copies queries and K, the other one copies V (one warp for both took longer
+// over a step's copies than HBM: its code comes from far between the softmax warps').
+template <uint32_t D, bool kV>
 __device__ void feed(const TreeParams& p, const Maps& maps, Control<D>& ctl, uint8_t* queries, uint8_t* slots, const unsigned long long* before, uint32_t size) {
   using S = Shape<D>;
   constexpr uint32_t kTok = S::kTok;
@@ -272,6 +281,7 @@ __device__ void feed(const TreeParams& p, const Maps& maps, Control<D>& ctl, uin
     n -= half;
   }
   uint64_t at = before[x];
+  asm volatile("bar.sync 1, 64;" ::: "memory");  // both have read the sums: copies may take their place
   uint32_t seq = x * run, head = 0, k = 0, items = 0;
   Request r{};
   Range g{};
@@ -294,8 +304,9 @@ __device__ void feed(const TreeParams& p, const Maps& maps, Control<D>& ctl, uin
     at += all;
   }
   int32_t* joins = reinterpret_cast<int32_t*>(p.notes) + blockIdx.x * 8;
-  uint32_t steps = 0, slot = 0, phase = 1;  // ring: next slot, parity of its being empty
+  uint32_t steps = 0;                       // of the items before
   uint32_t q_next = 0, q_parity = 3;        // where the next single tile's queries go; parities of either place being empty
+  uint32_t last = ~0u;                      // the last place that this warp has filled
   bool goes_on = false, alive = true;
   const uint32_t nb_shift = (kTok == 128 ? 7 : 6) - p.block_shift, blk = lane & ((1u << nb_shift) - 1), chunk = lane >> nb_shift;
   for (uint32_t j = 0; alive;) {
@@ -305,11 +316,11 @@ __device__ void feed(const TreeParams& p, const Maps& maps, Control<D>& ctl, uin
     auto step_of = [&](uint64_t pos) { return pos <= S::kItem ? 0u : static_cast<uint32_t>(pos) - S::kItem; };
     const uint32_t a = have && from > at ? step_of(from - at) : 0, b = have && to < at + cost ? step_of(to - at) : g.tiles;
     if (!have || a < b) {
-      if (j >= kNotes) alive = warp_wait(ctl.note_empty[j % kNotes], (j / kNotes - 1) & 1u, ctl, p.status);
+      if (!kV && j >= kNotes) alive = warp_wait(ctl.note_empty[j % kNotes], (j / kNotes - 1) & 1u, ctl, p.status);
       if (!alive) break;
       Note& note = ctl.note[j % kNotes];
       if (!have) {
-        if (lane == 0) {
+        if (!kV && lane == 0) {
           note.tiles = 0;
           arrive(ctl.note_full[j % kNotes]);
         }
@@ -317,7 +328,7 @@ __device__ void feed(const TreeParams& p, const Maps& maps, Control<D>& ctl, uin
       }
       const uint32_t tok0 = k * each, ntok = min(each, r.m - tok0);
       const bool pair = S::kStreams == 2 && ntok > tile_tokens(p);
-      if (lane == 0) {
+      if (!kV && lane == 0) {
         note.seq = seq;
         note.head = head;
         note.off = r.off;
@@ -365,11 +376,17 @@ __device__ void feed(const TreeParams& p, const Maps& maps, Control<D>& ctl, uin
         }
       };
       const bool late = pair || S::kStreams == 1;
-      if (!late) ask();
-      for (uint32_t t = a; t < b && alive; ++t, ++steps) {
+      if (!kV && !late) ask();
+      // A lane's copy of step t, and its block; the next step's entry is read before this one's copies wait.
+      auto wanted = [&](uint32_t t) {
         const uint32_t pos = (g.first + t) * kTok + (blk << p.block_shift);
-        const bool on = chunk < S::kChunks && pos < g.hi && pos + p.block_tokens > g.lo;
-        int32_t entry = on ? p.tables[seq * p.table_stride + (pos >> p.block_shift)] : 0;
+        return t < b && chunk < S::kChunks && pos < g.hi && pos + p.block_tokens > g.lo;
+      };
+      const int32_t* row = p.tables + seq * p.table_stride + blk;
+      auto entry_of = [&](uint32_t t) { return row[((g.first + t) * kTok) >> p.block_shift]; };
+      bool on = wanted(a);
+      int32_t entry = on ? entry_of(a) : 0;
+      for (uint32_t t = a; t < b; ++t) {
         const uint32_t boxes = __ballot_sync(0xffffffffu, on);
         const bool second = entry < 0;
         const uint32_t blocks = second ? p.blocks[1] : p.blocks[0];
@@ -378,25 +395,27 @@ __device__ void feed(const TreeParams& p, const Maps& maps, Control<D>& ctl, uin
           ptx::report_status(p.status, kStatusInvalid);
           id = blocks ? blocks : second ? p.blocks[0] : p.blocks[1];  // of an arena without blocks the map is the other one's
         }
-        const CUtensorMap* map = second ? &maps.m[1] : &maps.m[0];
-#pragma unroll
-        for (uint32_t half = 0; half < 2; ++half) {
-          alive = alive && warp_wait(ctl.empty[slot], phase, ctl, p.status);
+        const bool on_next = wanted(t + 1);
+        const int32_t entry_next = on_next ? entry_of(t + 1) : 0;
+        const uint32_t ring = 2 * steps + (kV ? v_place(t - a, b - a, pair) : k_place(t - a, pair)), slot = ring % S::kSlots;
+        alive = warp_wait(ctl.empty[slot], (ring / S::kSlots & 1u) ^ 1u, ctl, p.status);
+        if (!alive) break;
+        last = ring;
+        const uint32_t bar = ptx::smem_u32(&ctl.full[slot]);
+        if (lane == 0) ptx::mbar_arrive_expect_tx(bar, __popc(boxes) << (p.block_shift + 7));
+        __syncwarp();
+        if (on)
+          tma_box(ptx::smem_u32(slots) + slot * S::kSlotBytes + chunk * (kTok * 128) + ((blk << p.block_shift) << 7), second ? &maps.m[1] : &maps.m[0],
+                  kV ? p.block_tokens : 0, head * S::kChunks + chunk, id, bar, policy);
+        __syncwarp();
+        on = on_next;
+        entry = entry_next;
+        if (!kV && late && t == a) {
+          ask();
           if (!alive) break;
-          const uint32_t bar = ptx::smem_u32(&ctl.full[slot]);
-          if (lane == 0) ptx::mbar_arrive_expect_tx(bar, __popc(boxes) << (p.block_shift + 7));
-          __syncwarp();
-          if (on)
-            tma_box(ptx::smem_u32(slots) + slot * S::kSlotBytes + chunk * (kTok * 128) + ((blk << p.block_shift) << 7), map,
-                    half ? p.block_tokens : 0, head * S::kChunks + chunk, id, bar, policy);
-          __syncwarp();
-          if (++slot == S::kSlots) {
-            slot = 0;
-            phase ^= 1;
-          }
         }
-        if (late && t == a && alive) ask();
       }
+      steps += b - a;
       if (S::kStreams == 2 && !pair) q_next ^= 1;
       ++j;
     }
@@ -415,10 +434,13 @@ __device__ void feed(const TreeParams& p, const Maps& maps, Control<D>& ctl, uin
     }
     if (seq < p.nseq) g = range_of<D>(p, r, k, each);
   }
-  if (lane == 0 && !goes_on) joins[0] = 0;
-  if (!alive) {  // copies still in flight get a bounded time to land before the CTA's shared memory is given back
-    for (uint32_t s = 0; s < S::kSlots; ++s) ptx::mbar_wait(ptx::smem_u32(&ctl.full[s]), (s < slot ? phase ^ 1u : phase) & 1u, nullptr, 0);
-    for (uint32_t i = 0; i < 2; ++i) ptx::mbar_wait(ptx::smem_u32(&ctl.q_full[i]), q_parity >> i & 1u, nullptr, 0);
+  if (!kV && lane == 0 && !goes_on) joins[0] = 0;
+  if (!alive) {
+    // Copies still in flight get a bounded time to land before the CTA's shared memory is given back. (A place that is the other warp's has a phase of
+    // its own: waiting for it does no harm, the wait ends.)
+    for (uint32_t i = 0; i < S::kSlots && last != ~0u; ++i, --last)
+      ptx::mbar_wait(ptx::smem_u32(&ctl.full[last % S::kSlots]), last / S::kSlots & 1u, nullptr, 0);
+    for (uint32_t i = 0; i < 2 && !kV; ++i) ptx::mbar_wait(ptx::smem_u32(&ctl.q_full[i]), q_parity >> i & 1u, nullptr, 0);
   }
 }
 
@@ -432,24 +454,17 @@ __device__ void issue(const TreeParams& p, Control<D>& ctl, uint8_t* queries, ui
   const uint32_t tmem = ctl.tmem;
   const uint32_t scores = kScores | (p.q_flip ? 1u << 13 : 0u);  // a scale below 0: queries with the other sign
   const uint64_t q0 = tc::operand(ptx::smem_u32(queries), 16, 1024);
-  uint32_t p_parity = 0, q_parity = 0, slot = 0, phase = 0;  // K of step t lies in slot, V in the next one
+  uint32_t p_parity = 0, q_parity = 0;
   bool alive = true;
-  auto next = [](uint32_t& s, uint32_t& ph) {
-    if (++s == S::kSlots) {
-      s = 0;
-      ph ^= 1;
-    }
-  };
   for (uint32_t j = 0; alive; ++j) {
     alive = wait(ctl.note_full[j % kNotes], j / kNotes & 1u, ctl, p.status);
     if (!alive) break;
     const uint32_t tiles = ctl.note[j % kNotes].tiles, place = ctl.note[j % kNotes].q;
     const bool pair = S::kStreams == 2 && ctl.note[j % kNotes].ntok > tile_tokens(p);
     if (tiles == 0) break;
+    const uint32_t before = 2 * ctl.note[j % kNotes].before;
     arrive(ctl.note_empty[j % kNotes]);
     const uint32_t units = pair ? 2 * tiles : tiles;
-    uint32_t k_slot = slot, k_phase = phase, v_slot = slot, v_phase = phase;
-    next(v_slot, v_phase);
     for (uint32_t u = 0; u <= units; ++u) {
       if (u < units) {
         const bool last = !pair || (u & 1u);       // of the step's products with this tile of K
@@ -458,48 +473,40 @@ __device__ void issue(const TreeParams& p, Control<D>& ctl, uint8_t* queries, ui
           alive = wait(ctl.q_full[q], q_parity >> q & 1u, ctl, p.status);
           q_parity ^= 1u << q;
         }
-        if (alive && (!pair || !(u & 1u))) alive = wait(ctl.full[k_slot], k_phase, ctl, p.status);
+        const uint32_t ring = before + k_place(pair ? u >> 1 : u, pair), slot = ring % S::kSlots;
+        if (alive && (!pair || !(u & 1u))) alive = wait(ctl.full[slot], ring / S::kSlots & 1u, ctl, p.status);
         if (!alive) break;
         tc::fence_after();
         const uint64_t a = q0 + q * (S::kTileBytes >> 4);
-        const uint64_t b = tc::operand(ptx::smem_u32(slots) + k_slot * S::kSlotBytes, 16, 1024);
+        const uint64_t b = tc::operand(ptx::smem_u32(slots) + slot * S::kSlotBytes, 16, 1024);
 #pragma unroll
         for (uint32_t ks = 0; ks < D / 16; ++ks)
           tc::mma_ss(tmem + (u & 1u) * kTok, a + (ks / 4) * (128 * 128 >> 4) + (ks % 4) * 2, b + (ks / 4) * (kTok * 128 >> 4) + (ks % 4) * 2, scores,
                      ks != 0);
         tc::commit(ptx::smem_u32(&ctl.s_full[u & 1u]));
-        if (last) {
-          tc::commit(ptx::smem_u32(&ctl.empty[k_slot]));
-          next(k_slot, k_phase);
-          next(k_slot, k_phase);
-        }
+        if (last) tc::commit(ptx::smem_u32(&ctl.empty[slot]));
         if (u + (pair ? 2 : 1) >= units) tc::commit(ptx::smem_u32(&ctl.q_empty[q]));
       }
       if (u > 0) {
         const uint32_t w = u - 1, buf = w & 1u, stream = S::kStreams == 2 ? buf : 0;
         if (w == 0 && j) alive = wait(ctl.o_empty, (j - 1) & 1u, ctl, p.status);
-        if (alive && (!pair || !(w & 1u))) alive = wait(ctl.full[v_slot], v_phase, ctl, p.status);
+        const uint32_t ring = before + v_place(pair ? w >> 1 : w, tiles, pair), slot = ring % S::kSlots;
+        if (alive && (!pair || !(w & 1u))) alive = wait(ctl.full[slot], ring / S::kSlots & 1u, ctl, p.status);
         alive = alive && wait(ctl.p_full[buf], p_parity >> buf & 1u, ctl, p.status);
         if (!alive) break;
         p_parity ^= 1u << buf;
         tc::fence_after();
         const uint32_t o = tmem + S::kO + stream * D, weights = tmem + buf * kTok;
-        const uint64_t b = tc::operand(ptx::smem_u32(slots) + v_slot * S::kSlotBytes, kTok * 128, 1024);
+        const uint64_t b = tc::operand(ptx::smem_u32(slots) + slot * S::kSlotBytes, kTok * 128, 1024);
 #pragma unroll
         for (uint32_t part = 0; part < 2; ++part)
 #pragma unroll
           for (uint32_t ks = 0; ks < kTok / 16; ++ks)
-            tc::mma_ts(o, weights + part * (kTok / 2) + ks * 8, b + ks * (16 * 128 >> 4), kSums, part || ks || w >= S::kStreams);
-        if (!pair || (w & 1u)) {
-          tc::commit(ptx::smem_u32(&ctl.empty[v_slot]));
-          next(v_slot, v_phase);
-          next(v_slot, v_phase);
-        }
+            tc::mma_ts(o, weights + ks / 2 * 32 + part * 16 + ks % 2 * 8, b + ks * (16 * 128 >> 4), kSums, part || ks || w >= S::kStreams);
+        if (!pair || (w & 1u)) tc::commit(ptx::smem_u32(&ctl.empty[slot]));
         if (S::kStreams == 1 || w + S::kStreams >= units) tc::commit(ptx::smem_u32(&ctl.o_full[stream]));
       }
     }
-    slot = k_slot;
-    phase = k_phase;
   }
   // Everything issued has been done before tensor and shared memory are given back.
   tc::commit(ptx::smem_u32(&ctl.drain));
@@ -548,55 +555,68 @@ __device__ void soften(const TreeParams& p, Control<D>& ctl, uint8_t* slots) {
       if (!alive) break;
       s_parity ^= 1u << buf;
       tc::fence_after();
-      uint32_t s[kTok];
-#pragma unroll
-      for (uint32_t w = 0; w < kWords; ++w) tc::ld32(s + w * 32, tmem + buf * kTok + w * 32);
-      tc::wait_ld();
-#pragma unroll
-      for (uint32_t w = 0; w < kWords; ++w) touch(s + w * 32);
-      if (p.q_keep == 0) {                       // a scale of 0: queries of zeros
-#pragma unroll
-        for (uint32_t i = 0; i < kTok; ++i) s[i] = __float_as_uint(__uint_as_float(s[i]) * 0.f);
-      }
+      const uint32_t scores = tmem + buf * kTok;
       // Rows of V that no row of the item sees are made zeros, whatever they hold (a weight of 0 would not do). Of two tiles
       // the first one's product comes first.
       bool wipe = false, seen = false;
-      if (t0 < n.lo_all || t0 + kTok > n.full) {
-        uint32_t see[kWords];
-        visible(p, row, n.c, t0, see);
+      if (t0 < n.lo_all || t0 + kTok > n.full || p.q_keep == 0) {
+        uint32_t* by_words = ctl.seen[x][group & 1u][r >> 5];
+        const bool share = !simple && (!pair || x == 0);
+#pragma unroll 1
+        for (uint32_t w = 0; w < kWords; ++w) {
+          uint32_t see = visible(p, row, n.c, t0 + w * 32);
+          if (!__all_sync(0xffffffffu, see == ~0u) || p.q_keep == 0) {
+            uint32_t s[32];
+            tc::ld32(s, scores + w * 32);
+            tc::wait_ld();
+            touch(s);
 #pragma unroll
-        for (uint32_t w = 0; w < kWords; ++w)
-#pragma unroll
-          for (uint32_t i = 0; i < 32; ++i) s[w * 32 + i] = see[w] >> i & 1u ? s[w * 32 + i] : __float_as_uint(kMinusInf);
+            for (uint32_t i = 0; i < 32; ++i) {
+              if (p.q_keep == 0) s[i] = __float_as_uint(__uint_as_float(s[i]) * 0.f);  // a scale of 0: queries of zeros
+              s[i] = see >> i & 1u ? s[i] : __float_as_uint(kMinusInf);
+            }
+            tc::st32(scores + w * 32, s);
+          }
+          if (share) {
+            if (pair) see |= visible(p, other, n.c, t0 + w * 32);
+            see = __reduce_or_sync(0xffffffffu, see);
+            if (lane == 0) by_words[w] = see;
+          }
+        }
+        tc::wait_st();
         if (simple) {
           wipe = t0 < n.lo || t0 + kTok > n.hi;
           seen = t0 + r >= n.lo && t0 + r < n.hi;
-        } else if (!pair || x == 0) {
+        } else if (share) {
           wipe = true;
-          if (pair) {
-            uint32_t more[kWords];
-            visible(p, other, n.c, t0, more);
-#pragma unroll
-            for (uint32_t w = 0; w < kWords; ++w) see[w] |= more[w];
-          }
-          uint32_t(*by_warps)[4] = ctl.seen[x][group & 1u];
-#pragma unroll
-          for (uint32_t w = 0; w < kWords; ++w) {
-            const uint32_t all = __reduce_or_sync(0xffffffffu, see[w]);
-            if (lane == 0) by_warps[r >> 5][w] = all;
-          }
           __syncwarp();
           if (lane == 0) arrive(ctl.group[x]);
-          alive = warp_wait(ctl.group[x], group++ & 1u, ctl, p.status);
+          alive = warp_wait(ctl.group[x], group & 1u, ctl, p.status);
           if (!alive) break;
           const uint32_t w = r / 32 % kWords;
+          const uint32_t(*by_warps)[4] = ctl.seen[x][group++ & 1u];
           seen = (by_warps[0][w] | by_warps[1][w] | by_warps[2][w] | by_warps[3][w]) >> lane & 1u;
         }
         wipe = wipe && (!pair || x == 0);
       }
+      // Twice over the scores, 32 at a time, the next ones on their way: in registers all at once they and their code, straight
+      // through, took longer to fetch than to run.
       float mx[4] = {kMinusInf, kMinusInf, kMinusInf, kMinusInf};
+      {
+        uint32_t s[2][32];
+        tc::ld32(s[0], scores);
+#pragma unroll 1
+        for (uint32_t w = 0; w < kWords; w += 2) {
 #pragma unroll
-      for (uint32_t i = 0; i < kTok; ++i) mx[i & 3u] = fmaxf(mx[i & 3u], __uint_as_float(s[i]));
+          for (uint32_t k = 0; k < 2; ++k) {
+            tc::wait_ld();
+            touch(s[k]);
+            if (k == 0 || w + 2 < kWords) tc::ld32(s[k ^ 1], scores + (w + k + 1) * 32);
+#pragma unroll
+            for (uint32_t i = 0; i < 32; ++i) mx[i & 3u] = fmaxf(mx[i & 3u], __uint_as_float(s[k][i]));
+          }
+        }
+      }
       const float most = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
       if (__any_sync(0xffffffffu, (most - top) * p.scale_log2 > kSlack<kBf16>)) {
         const float now = fmaxf(top, most), al = now == kMinusInf ? 1.f : ptx::exp2_approx((top - now) * p.scale_log2);
@@ -625,28 +645,37 @@ __device__ void soften(const TreeParams& p, Control<D>& ctl, uint8_t* slots) {
       const float ref = top == kMinusInf ? 0.f : top;
       const uint64_t ref2 = two(-ref, -ref), scale2 = two(p.scale_log2, p.scale_log2), top2 = two(kTop<kBf16>, kTop<kBf16>), minus2 = two(-1.f, -1.f);
       uint64_t sums[2] = {0, 0};
+      {
+        uint32_t s[2][32];
+        tc::ld32(s[0], scores);
+#pragma unroll 1
+        for (uint32_t w = 0; w < kWords; w += 2) {
 #pragma unroll
-      for (uint32_t w = 0; w < kWords; ++w) {
-        uint32_t hi[16], lo[16];
+          for (uint32_t k = 0; k < 2; ++k) {
+            tc::wait_ld();
+            touch(s[k]);
+            if (k == 0 || w + 2 < kWords) tc::ld32(s[k ^ 1], scores + (w + k + 1) * 32);
+            uint32_t v[32];                      // in their place: 16 columns of weights, 16 of what their rounding left
 #pragma unroll
-        for (uint32_t i = 0; i < 16; ++i) {
-          // (The difference is taken first: of scores beyond 2^24 the rounding of a score times the scale would be more than an exponent's worth.)
-          const float2 e = each(fma2(add2(two(__uint_as_float(s[w * 32 + 2 * i]), __uint_as_float(s[w * 32 + 2 * i + 1])), ref2), scale2, top2));
-          const float a = ptx::exp2_approx(e.x), b = ptx::exp2_approx(e.y);
-          const uint64_t ab = two(a, b);
-          sums[i & 1u] = add2(sums[i & 1u], ab);
-          hi[i] = pack<kBf16>(a, b);
-          const float2 h = unpack<kBf16>(hi[i]);
-          const float2 left = each(fma2(two(h.x, h.y), minus2, ab));
-          lo[i] = pack<kBf16>(left.x, left.y);
+            for (uint32_t i = 0; i < 16; ++i) {
+              // (The difference is taken first: of scores beyond 2^24 the rounding of a score times the scale would be more than an exponent's worth.)
+              const float2 e = each(fma2(add2(two(__uint_as_float(s[k][2 * i]), __uint_as_float(s[k][2 * i + 1])), ref2), scale2, top2));
+              const float a = ptx::exp2_approx(e.x), b = ptx::exp2_approx(e.y);
+              const uint64_t ab = two(a, b);
+              sums[i & 1u] = add2(sums[i & 1u], ab);
+              v[i] = pack<kBf16>(a, b);
+              const float2 h = unpack<kBf16>(v[i]);
+              const float2 left = each(fma2(two(h.x, h.y), minus2, ab));
+              v[16 + i] = pack<kBf16>(left.x, left.y);
+            }
+            tc::st32(scores + (w + k) * 32, v);
+          }
         }
-        tc::st16(tmem + buf * kTok + w * 16, hi);
-        tc::st16(tmem + buf * kTok + kTok / 2 + w * 16, lo);
       }
       const float2 both = each(add2(sums[0], sums[1]));
       sum += both.x + both.y;
       if (wipe) {
-        const uint32_t ring = 2 * (n.before + kt) + 1, slot = ring % S::kSlots;
+        const uint32_t ring = 2 * n.before + v_place(kt, n.tiles, pair), slot = ring % S::kSlots;
         alive = warp_wait(ctl.full[slot], ring / S::kSlots & 1u, ctl, p.status);
         if (!alive) break;
         if (r < kTok && !seen) {
@@ -820,17 +849,15 @@ __global__ void __launch_bounds__(kThreads, 1) paged_tree_kernel(const TreeParam
   const uint32_t size = static_cast<uint32_t>(min(max(share, 2ull + S::kItem), 0xffffffffull));
   __syncthreads();
 
-  if (warp < 8) {
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoftRegs));
+  if (warp < 8)
     soften<D, kBf16>(p, ctl, slots);
-  } else {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
-    if (warp == 8)
-      feed<D>(p, maps, ctl, queries, slots, before, size);
-    else if (warp == 9 && lane == 0)
-      issue<D, kBf16>(p, ctl, queries, slots);
-    __syncwarp();
-  }
+  else if (warp == 8)
+    feed<D, false>(p, maps, ctl, queries, slots, before, size);
+  else if (warp == 10)
+    feed<D, true>(p, maps, ctl, queries, slots, before, size);
+  else if (lane == 0)
+    issue<D, kBf16>(p, ctl, queries, slots);
+  __syncwarp();
 
   // Requests whose length or offsets are out of range: zeros, where the offsets name rows.
   const uint32_t heads = p.num_kv_heads * p.group;
@@ -851,22 +878,20 @@ __global__ void __launch_bounds__(kThreads, 1) paged_tree_kernel(const TreeParam
   if (warp == 9) tc::dealloc(ctl.tmem, 512);
 }
 
-// Items that were cut: the sum of their parts, weighted by their references, and the division. A CTA takes 32 rows of an item's
-// part of the columns at a time.
+// Items that were cut: the sum of their parts, weighted by their references, and the division. A warp takes 32 rows and 32 columns of an
+// item at a time, a row to a lane. Bound by latency: which items, their references and sums, their rows, each a trip to L2.
 constexpr uint32_t kJoinThreads = 256;
 static_assert(kTreeMaxCtas <= kJoinThreads, "a thread for every CTA's item");
 
 template <uint32_t D, bool kBf16>
 __global__ void __launch_bounds__(kJoinThreads) tree_join_kernel(const TreeParams p, const uint32_t ctas) {
   using S = Shape<D>;
-  __shared__ uint32_t list[kTreeMaxCtas], warp_count[kJoinThreads / 32];
-  __shared__ float weight[kTreeMaxCtas][32], total[32];
+  __shared__ uint32_t list[kTreeMaxCtas][4], warp_count[kJoinThreads / 32];
   ptx::launch_dependents();
   ptx::grid_dependency_wait();
   const uint32_t tid = threadIdx.x, lane = tid & 31u, warp = tid >> 5;
-  const int32_t* notes = reinterpret_cast<const int32_t*>(p.notes);
-  const bool cut = tid < ctas && notes[tid * 8] > 0;  // in order: every CTA takes the same piece of the same item
-  const uint32_t ballot = __ballot_sync(0xffffffffu, cut);
+  const int4 note = tid < ctas ? reinterpret_cast<const int4*>(p.notes)[tid * 2] : make_int4(0, 0, 0, 0);
+  const uint32_t ballot = __ballot_sync(0xffffffffu, note.x > 0);
   if (lane == 0) warp_count[warp] = __popc(ballot);
   __syncthreads();
   uint32_t at = __popc(ballot & ((1u << lane) - 1)), count = 0;
@@ -875,51 +900,55 @@ __global__ void __launch_bounds__(kJoinThreads) tree_join_kernel(const TreeParam
     if (w < warp) at += warp_count[w];
     count += warp_count[w];
   }
-  if (cut) list[at] = tid;
+  if (note.x > 0) {
+    list[at][0] = tid | static_cast<uint32_t>(note.x) << 16;
+    list[at][1] = static_cast<uint32_t>(note.y);
+    list[at][2] = static_cast<uint32_t>(note.z);
+    list[at][3] = static_cast<uint32_t>(note.w);
+  }
   __syncthreads();
   const uint32_t G = p.group, tt = tile_tokens(p), heads = p.num_kv_heads * G;
-  constexpr uint32_t kSlabs = S::kRows / 32;
-  const uint32_t tasks = count * kSlabs;
-  for (uint32_t x = blockIdx.x; x < tasks; x += gridDim.x) {
-    const uint32_t k = list[x / kSlabs], row = x % kSlabs * 32 + lane;
-    const uint32_t parts = static_cast<uint32_t>(notes[k * 8]), tok0 = static_cast<uint32_t>(notes[k * 8 + 1]), ntok = static_cast<uint32_t>(notes[k * 8 + 2]),
-                   head = static_cast<uint32_t>(notes[k * 8 + 3]);
+  constexpr uint32_t kSlabs = S::kRows / 32, kCols = D / 32;
+  const uint32_t tasks = count * kSlabs * kCols;
+  for (uint32_t x = blockIdx.x * (kJoinThreads / 32) + warp; x < tasks; x += gridDim.x * (kJoinThreads / 32)) {
+    const uint32_t* item = list[x / (kSlabs * kCols)];
+    const uint32_t k = item[0] & 0xffffu, parts = item[0] >> 16, tok0 = item[1], ntok = item[2], head = item[3];
+    const uint32_t slab = x / kCols % kSlabs, col = x % kCols, row = slab * 32 + lane;
     const uint32_t tile = row >> 7, in_tile = (row & 127u) / G, h = (row & 127u) - in_tile * G, tok = tile * tt + in_tile;
-    const bool on = in_tile < tt && tok < ntok;
-    if (!__any_sync(0xffffffffu, on)) continue;  // the same for all warps
-    auto part = [&](uint32_t i) { return p.parts + static_cast<uint64_t>(i ? 2 * (k + i) : 2 * k + 1) * S::kPart; };
-    __syncthreads();
-    if (warp == 0) {
-      float most = kMinusInf, sum = 0.f;
-      if (on) {
-        for (uint32_t i = 0; i < parts; ++i) most = fmaxf(most, part(i)[S::kRows * D + row]);
-        const float ref = most == kMinusInf ? 0.f : most;
-        for (uint32_t i = 0; i < parts; ++i) {
-          const float w = ptx::exp2_approx((part(i)[S::kRows * D + row] - ref) * p.scale_log2);
-          weight[i][lane] = w;
-          sum += part(i)[S::kRows * (D + 1) + row] * w;
-        }
-        if (p.lse) p.lse[static_cast<uint64_t>(tok0 + tok) * heads + head * G + h] = fmaf(most, p.scale_log2, log2f(sum) - kTop<kBf16>) * 0.6931471805599453f;
-      }
-      total[lane] = sum > 0.f ? 1.f / sum : sum;
-    }
-    __syncthreads();
-    if (!on) continue;
-    uint8_t* out = p.out + static_cast<uint64_t>(tok0 + tok) * p.out_stride + static_cast<uint64_t>(head * G + h) * D * 2;
-    for (uint32_t c = warp; c < D / 4; c += kJoinThreads / 32) {
-      float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (in_tile >= tt || tok >= ntok) continue;
+    // Part i: the first one in the second place of the CTA where the item begins, the others in the first places of the next ones.
+    const float* first = p.parts + static_cast<uint64_t>(2 * k + 1) * S::kPart;
+    const float* rest = p.parts + static_cast<uint64_t>(2 * k) * S::kPart;
+    auto part = [&](uint32_t i) { return i ? rest + static_cast<uint64_t>(2 * i) * S::kPart : first; };
+    float top = kMinusInf, sum = 0.f;
 #pragma unroll 4
-      for (uint32_t i = 0; i < parts; ++i) {
-        const float4 v = reinterpret_cast<const float4*>(part(i))[c * S::kRows + row];
-        const float w = weight[i][lane];
-        acc.x = fmaf(v.x, w, acc.x);
-        acc.y = fmaf(v.y, w, acc.y);
-        acc.z = fmaf(v.z, w, acc.z);
-        acc.w = fmaf(v.w, w, acc.w);
+    for (uint32_t i = 0; i < parts; ++i) top = fmaxf(top, part(i)[S::kRows * D + row]);
+    const float ref = top == kMinusInf ? 0.f : top;
+    float4 acc[8];
+#pragma unroll
+    for (uint32_t c = 0; c < 8; ++c) acc[c] = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 2
+    for (uint32_t i = 0; i < parts; ++i) {
+      const float* from = part(i);
+      const float w = ptx::exp2_approx((from[S::kRows * D + row] - ref) * p.scale_log2);
+      sum = fmaf(from[S::kRows * (D + 1) + row], w, sum);
+#pragma unroll
+      for (uint32_t c = 0; c < 8; ++c) {
+        const float4 v = reinterpret_cast<const float4*>(from)[(col * 8 + c) * S::kRows + row];
+        acc[c].x = fmaf(v.x, w, acc[c].x);
+        acc[c].y = fmaf(v.y, w, acc[c].y);
+        acc[c].z = fmaf(v.z, w, acc[c].z);
+        acc[c].w = fmaf(v.w, w, acc[c].w);
       }
-      const float inv = total[lane];
-      *reinterpret_cast<uint2*>(out + c * 8) = make_uint2(pack<kBf16>(acc.x * inv, acc.y * inv), pack<kBf16>(acc.z * inv, acc.w * inv));
     }
+    const float inv = sum > 0.f ? 1.f / sum : sum;
+    uint4* out = reinterpret_cast<uint4*>(p.out + static_cast<uint64_t>(tok0 + tok) * p.out_stride + (static_cast<uint64_t>(head * G + h) * D + col * 32) * 2);
+#pragma unroll
+    for (uint32_t c = 0; c < 4; ++c)
+      out[c] = make_uint4(pack<kBf16>(acc[2 * c].x * inv, acc[2 * c].y * inv), pack<kBf16>(acc[2 * c].z * inv, acc[2 * c].w * inv),
+                          pack<kBf16>(acc[2 * c + 1].x * inv, acc[2 * c + 1].y * inv), pack<kBf16>(acc[2 * c + 1].z * inv, acc[2 * c + 1].w * inv));
+    if (p.lse && col == 0)
+      p.lse[static_cast<uint64_t>(tok0 + tok) * heads + head * G + h] = fmaf(top, p.scale_log2, log2f(sum) - kTop<kBf16>) * 0.6931471805599453f;
   }
 }
 
