@@ -32,8 +32,12 @@ namespace ema {
 namespace {
 
 constexpr float kMinusInf = -INFINITY;
-constexpr uint32_t kThreads = 352;                  // two groups of four warps, two copying warps, the issuing warp
+// Warps: two groups of four for the softmax, four that write rows out, two that copy, one that issues the products (and an idle one).
+constexpr uint32_t kThreads = 512, kOutWarp = 8, kFeedWarp = 12, kIssueWarp = 14;
 constexpr uint32_t kNotes = 4;
+// Registers of a thread: the launch has 128 for everybody; the last two groups of warps give up what the first two get.
+constexpr uint32_t kSoftRegs = 168, kOtherRegs = 88;
+static_assert(2 * kSoftRegs + 2 * kOtherRegs <= 4 * 128, "no more than the block was launched with");
 
 template <uint32_t D>
 struct Shape {
@@ -65,6 +69,7 @@ struct Note {
   uint32_t first, tiles;        // steps of kTok positions
   uint32_t before;              // steps of this CTA before them
   uint32_t q;                   // where the queries of a single tile lie
+  uint32_t turn;                // stream (of one: buffer) of the item's first unit
   uint32_t slot;                // part, or ~0: the whole item
 };
 
@@ -73,13 +78,16 @@ struct Control {
   using S = Shape<D>;
   uint64_t full[S::kSlots], empty[S::kSlots];
   uint64_t note_full[kNotes], note_empty[kNotes];
-  uint64_t q_full[2], q_empty[2], o_empty, joint, drain;
-  uint64_t s_full[2], p_full[2], o_full[2], group[2];
+  uint64_t q_full[2], q_empty[2], o_done, o_empty, stats_full, stats_empty, drain;
+  uint64_t s_full[2], p_full[2], group[2];
+  uint64_t summed;              // of one stream: after every product with V
   Note note[kNotes];
   uint32_t seen[2][2][4][4];    // positions of a step that some row sees: the groups' own, two steps' in turn, by warps
-  float2 stats[S::kStreams][128];  // references and sums of one tile's streams
+  union {
+    float2 stats[S::kStreams][128];  // references and sums of the streams' rows
+    unsigned long long warp_total[kThreads / 32];  // before there are any
+  };
   uint32_t tmem, dead;
-  unsigned long long warp_total[kThreads / 32];
 };
 
 template <uint32_t D>
@@ -305,6 +313,7 @@ __device__ void feed(const TreeParams& p, const Maps& maps, Control<D>& ctl, uin
   }
   int32_t* joins = reinterpret_cast<int32_t*>(p.notes) + blockIdx.x * 8;
   uint32_t steps = 0;                       // of the items before
+  uint32_t units = 0;                       // of the items before: a step with every tile of queries is one
   uint32_t q_next = 0, q_parity = 3;        // where the next single tile's queries go; parities of either place being empty
   uint32_t last = ~0u;                      // the last place that this warp has filled
   bool goes_on = false, alive = true;
@@ -345,6 +354,7 @@ __device__ void feed(const TreeParams& p, const Maps& maps, Control<D>& ctl, uin
         note.tiles = b - a;
         note.before = steps;
         note.q = q_next;
+        note.turn = units & 1u;
         note.slot = a ? 2 * blockIdx.x : b < g.tiles ? 2 * blockIdx.x + 1 : ~0u;
         arrive(ctl.note_full[j % kNotes]);
         if (a == 0 && b < g.tiles) {
@@ -416,6 +426,7 @@ __device__ void feed(const TreeParams& p, const Maps& maps, Control<D>& ctl, uin
         }
       }
       steps += b - a;
+      units += pair ? 2 * (b - a) : b - a;
       if (S::kStreams == 2 && !pair) q_next ^= 1;
       ++j;
     }
@@ -444,67 +455,125 @@ __device__ void feed(const TreeParams& p, const Maps& maps, Control<D>& ctl, uin
   }
 }
 
-// The issuing thread. Scores of unit u, then the sums of unit u - 1: while a group works on its scores the tensor cores do the
-// other's. Products are done in the order in which they are issued, so that scores take the place of weights that were issued before.
+// Whether the phase has completed: does not wait.
+__device__ __forceinline__ bool ready(uint64_t& bar, uint32_t parity) {
+  uint32_t done;
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+      "selp.u32 %0, 1, 0, p;\n\t}"
+      : "=r"(done)
+      : "r"(ptx::smem_u32(&bar)), "r"(parity)
+      : "memory");
+  return done != 0;
+}
+
+// The issuing thread. Units (a step with one tile of queries) take the two buffers of scores in turn, across items. Scores of a unit may
+// be issued once the sums of the unit before the last one have been: products are done in the order in which they are issued, so
+// that scores take the place of weights that were used before. Whatever has its operands goes first, scores before sums.
 template <uint32_t D, bool kBf16>
 __device__ void issue(const TreeParams& p, Control<D>& ctl, uint8_t* queries, uint8_t* slots) {
   using S = Shape<D>;
   constexpr uint32_t kTok = S::kTok;
-  constexpr uint32_t kScores = tc::product(kBf16, kTok, false), kSums = tc::product(kBf16, D, true);
-  const uint32_t tmem = ctl.tmem;
-  const uint32_t scores = kScores | (p.q_flip ? 1u << 13 : 0u);  // a scale below 0: queries with the other sign
+  const uint32_t scores = tc::product(kBf16, kTok, false) | (p.q_flip ? 1u << 13 : 0u);  // a scale below 0: queries with the other sign
+  constexpr uint32_t kSums = tc::product(kBf16, D, true);
+  const uint32_t tmem = ctl.tmem, tt = tile_tokens(p);
   const uint64_t q0 = tc::operand(ptx::smem_u32(queries), 16, 1024);
-  uint32_t p_parity = 0, q_parity = 0;
-  bool alive = true;
-  for (uint32_t j = 0; alive; ++j) {
-    alive = wait(ctl.note_full[j % kNotes], j / kNotes & 1u, ctl, p.status);
-    if (!alive) break;
-    const uint32_t tiles = ctl.note[j % kNotes].tiles, place = ctl.note[j % kNotes].q;
-    const bool pair = S::kStreams == 2 && ctl.note[j % kNotes].ntok > tile_tokens(p);
-    if (tiles == 0) break;
-    const uint32_t before = 2 * ctl.note[j % kNotes].before;
-    arrive(ctl.note_empty[j % kNotes]);
-    const uint32_t units = pair ? 2 * tiles : tiles;
-    for (uint32_t u = 0; u <= units; ++u) {
-      if (u < units) {
-        const bool last = !pair || (u & 1u);       // of the step's products with this tile of K
-        const uint32_t q = pair ? u & 1u : place;
-        if (u < (pair ? 2 : 1)) {
-          alive = wait(ctl.q_full[q], q_parity >> q & 1u, ctl, p.status);
-          q_parity ^= 1u << q;
-        }
-        const uint32_t ring = before + k_place(pair ? u >> 1 : u, pair), slot = ring % S::kSlots;
-        if (alive && (!pair || !(u & 1u))) alive = wait(ctl.full[slot], ring / S::kSlots & 1u, ctl, p.status);
-        if (!alive) break;
+  const uint64_t k0 = tc::operand(ptx::smem_u32(slots), 16, 1024), v0 = tc::operand(ptx::smem_u32(slots), kTok * 128, 1024);
+  struct Cursor {
+    uint32_t j, u, units, tiles, before, place, first, hi;
+    bool pair;
+  };
+  Cursor a{}, b{};                // next scores, next sums: item, unit
+  a.j = b.j = ~0u;
+  uint32_t na = 0, nb = 0, q_parity = 0;
+  bool last = false;              // there are no more items
+  // The cursor's next item, if it is known.
+  auto open = [&](Cursor& c) {
+    const uint32_t j = c.j + 1;
+    if (!ready(ctl.note_full[j % kNotes], j / kNotes & 1u)) return false;
+    const Note& n = ctl.note[j % kNotes];
+    c.j = j;
+    c.u = 0;
+    c.tiles = n.tiles;
+    c.pair = S::kStreams == 2 && n.ntok > tt;
+    c.units = c.pair ? 2 * n.tiles : n.tiles;
+    c.before = 2 * n.before;
+    c.place = n.q;
+    c.first = n.first;
+    c.hi = n.hi;
+    return true;
+  };
+  uint64_t t0 = ptx::global_timer_ns();
+  for (uint32_t polls = 1; !last || nb < na; ++polls) {
+    bool moved = false;
+    if (!last && na - nb < 2 && (a.u < a.units || open(a))) {
+      if (a.tiles == 0) {
+        last = true;
+        continue;
+      }
+      const uint32_t kt = a.pair ? a.u >> 1 : a.u, q = a.pair ? a.u & 1u : a.place;
+      const uint32_t ring = a.before + k_place(kt, a.pair), slot = ring % S::kSlots, buf = na & 1u;
+      if (ready(ctl.full[slot], ring / S::kSlots & 1u) && (a.u >= (a.pair ? 2 : 1) || ready(ctl.q_full[q], q_parity >> q & 1u))) {
+        if (a.u < (a.pair ? 2 : 1)) q_parity ^= 1u << q;
         tc::fence_after();
-        const uint64_t a = q0 + q * (S::kTileBytes >> 4);
-        const uint64_t b = tc::operand(ptx::smem_u32(slots) + slot * S::kSlotBytes, 16, 1024);
+        const uint64_t x = q0 + q * (S::kTileBytes >> 4), y = k0 + slot * (S::kSlotBytes >> 4);
 #pragma unroll
         for (uint32_t ks = 0; ks < D / 16; ++ks)
-          tc::mma_ss(tmem + (u & 1u) * kTok, a + (ks / 4) * (128 * 128 >> 4) + (ks % 4) * 2, b + (ks / 4) * (kTok * 128 >> 4) + (ks % 4) * 2, scores,
-                     ks != 0);
-        tc::commit(ptx::smem_u32(&ctl.s_full[u & 1u]));
-        if (last) tc::commit(ptx::smem_u32(&ctl.empty[slot]));
-        if (u + (pair ? 2 : 1) >= units) tc::commit(ptx::smem_u32(&ctl.q_empty[q]));
+          tc::mma_ss(tmem + buf * kTok, x + (ks / 4) * (128 * 128 >> 4) + (ks % 4) * 2, y + (ks / 4) * (kTok * 128 >> 4) + (ks % 4) * 2, scores, ks != 0);
+        tc::commit(ptx::smem_u32(&ctl.s_full[buf]));
+        if (!a.pair || (a.u & 1u)) tc::commit(ptx::smem_u32(&ctl.empty[slot]));
+        if (a.u + (a.pair ? 2 : 1) >= a.units) tc::commit(ptx::smem_u32(&ctl.q_empty[q]));
+        ++a.u;
+        ++na;
+        moved = true;
       }
-      if (u > 0) {
-        const uint32_t w = u - 1, buf = w & 1u, stream = S::kStreams == 2 ? buf : 0;
-        if (w == 0 && j) alive = wait(ctl.o_empty, (j - 1) & 1u, ctl, p.status);
-        const uint32_t ring = before + v_place(pair ? w >> 1 : w, tiles, pair), slot = ring % S::kSlots;
-        if (alive && (!pair || !(w & 1u))) alive = wait(ctl.full[slot], ring / S::kSlots & 1u, ctl, p.status);
-        alive = alive && wait(ctl.p_full[buf], p_parity >> buf & 1u, ctl, p.status);
-        if (!alive) break;
-        p_parity ^= 1u << buf;
+    }
+    if (nb < na && (b.u < b.units || open(b))) {
+      const uint32_t kt = b.pair ? b.u >> 1 : b.u, buf = nb & 1u, stream = S::kStreams == 2 ? buf : 0;
+      const uint32_t ring = b.before + v_place(kt, b.tiles, b.pair), slot = ring % S::kSlots;
+      if (ready(ctl.p_full[buf], nb >> 1 & 1u) && ready(ctl.full[slot], ring / S::kSlots & 1u) &&
+          (b.u || b.j == 0 || ready(ctl.o_empty, (b.j - 1) & 1u))) {
         tc::fence_after();
         const uint32_t o = tmem + S::kO + stream * D, weights = tmem + buf * kTok;
-        const uint64_t b = tc::operand(ptx::smem_u32(slots) + slot * S::kSlotBytes, kTok * 128, 1024);
+        const uint64_t y = v0 + slot * (S::kSlotBytes >> 4);
+        const uint32_t t = (b.first + kt) * kTok;
+        const bool add = b.u >= S::kStreams;
+        if (t + kTok <= b.hi) {
 #pragma unroll
-        for (uint32_t part = 0; part < 2; ++part)
+          for (uint32_t part = 0; part < 2; ++part)
 #pragma unroll
-          for (uint32_t ks = 0; ks < kTok / 16; ++ks)
-            tc::mma_ts(o, weights + ks / 2 * 32 + part * 16 + ks % 2 * 8, b + ks * (16 * 128 >> 4), kSums, part || ks || w >= S::kStreams);
-        if (!pair || (w & 1u)) tc::commit(ptx::smem_u32(&ctl.empty[slot]));
-        if (S::kStreams == 1 || w + S::kStreams >= units) tc::commit(ptx::smem_u32(&ctl.o_full[stream]));
+            for (uint32_t ks = 0; ks < kTok / 16; ++ks)
+              tc::mma_ts(o, weights + ks / 2 * 32 + part * 16 + ks % 2 * 8, y + ks * (16 * 128 >> 4), kSums, part || ks || add);
+        } else {                  // positions that nobody sees are left out
+          const uint32_t n = (b.hi - t + 15) / 16;
+#pragma unroll 1
+          for (uint32_t ks = 0; ks < n; ++ks)
+#pragma unroll
+            for (uint32_t part = 0; part < 2; ++part)
+              tc::mma_ts(o, weights + ks / 2 * 32 + part * 16 + ks % 2 * 8, y + ks * (16 * 128 >> 4), kSums, part || ks || add);
+        }
+        if (!b.pair || (b.u & 1u)) tc::commit(ptx::smem_u32(&ctl.empty[slot]));
+        if (S::kStreams == 1) tc::commit(ptx::smem_u32(&ctl.summed));
+        ++b.u;
+        ++nb;
+        if (b.u == b.units) {
+          tc::commit(ptx::smem_u32(&ctl.o_done));
+          arrive(ctl.note_empty[b.j % kNotes]);
+        }
+        moved = true;
+      }
+    }
+    if (moved) {
+      polls = 0;
+    } else if ((polls & 63u) == 0) {
+      if (*reinterpret_cast<volatile uint32_t*>(&ctl.dead)) break;
+      const uint64_t t = ptx::global_timer_ns();
+      if (polls == 64) t0 = t;
+      if (t - t0 > 2000000000ull) {
+        *reinterpret_cast<volatile uint32_t*>(&ctl.dead) = 1;
+        ptx::report_status(p.status, kDevTimeout);
+        break;
       }
     }
   }
@@ -513,23 +582,25 @@ __device__ void issue(const TreeParams& p, Control<D>& ctl, uint8_t* queries, ui
   ptx::mbar_wait(ptx::smem_u32(&ctl.drain), 0, p.status, kDevTimeout);
 }
 
-__device__ __forceinline__ void touch(uint32_t* r) {
+// Registers that a load has written, from here on.
+template <uint32_t N>
+__device__ __forceinline__ void touch(uint32_t (&r)[N]) {
 #pragma unroll
-  for (uint32_t i = 0; i < 32; ++i) asm volatile("" : "+r"(r[i]));
+  for (uint32_t i = 0; i < N; ++i) asm volatile("" : "+r"(r[i]));
 }
 
-// A group of four warps: queries in, softmax of its stream, rows out.
+// A group of four warps: the softmax of its stream, a row to a thread.
 template <uint32_t D, bool kBf16>
 __device__ void soften(const TreeParams& p, Control<D>& ctl, uint8_t* slots) {
   using S = Shape<D>;
   constexpr uint32_t kTok = S::kTok, kWords = kTok / 32;
   const uint32_t lane = threadIdx.x & 31u, x = threadIdx.x >> 7, r = threadIdx.x & 127u;
-  const uint32_t lanes = (r & ~31u) << 16;       // this warp's part of tensor memory
-  const uint32_t tmem = ctl.tmem + lanes;
-  const uint32_t G = p.group, tt = tile_tokens(p), in_tile = r / G, my_head = r - in_tile * G;
-  const bool packed = r < tt * G;                // rows behind the tile's last token are padding
-  const uint32_t heads = p.num_kv_heads * G;
-  uint32_t s_parity = 0, o_count = 0, joint = 0, group = 0;
+  const uint32_t tmem = ctl.tmem + ((r & ~31u) << 16);  // this warp's part of tensor memory
+  const uint32_t tt = tile_tokens(p), in_tile = r / p.group;
+  const bool packed = r < tt * p.group;          // rows behind the tile's last token are padding
+  const bool works = S::kStreams == 2 || x == 0;
+  const bool simple = !p.mask && !p.positions;   // some row sees every position in [lo, hi)
+  uint32_t s_parity = 0, sums_before = 0, group = 0;
   bool alive = true;
   for (uint32_t j = 0; alive; ++j) {
     alive = warp_wait(ctl.note_full[j % kNotes], j / kNotes & 1u, ctl, p.status);
@@ -537,33 +608,32 @@ __device__ void soften(const TreeParams& p, Control<D>& ctl, uint8_t* slots) {
     const Note n = ctl.note[j % kNotes];
     if (n.tiles == 0) break;
     const bool pair = S::kStreams == 2 && n.ntok > tt;
-    const uint32_t my_tok = (pair ? x * tt : 0) + in_tile;
+    const uint32_t tile = pair ? x ^ n.turn : 0;
+    const uint32_t my_tok = tile * tt + in_tile;
     const bool mine = packed && my_tok < n.ntok;
     const Row row = row_of(p, n, n.tok0 + my_tok, mine);
     Row other{};                                 // of the second tile, whose V is the same
-    if (pair && x == 0) other = row_of(p, n, n.tok0 + tt + in_tile, packed && tt + in_tile < n.ntok);
+    if (pair && tile == 0) other = row_of(p, n, n.tok0 + tt + in_tile, packed && tt + in_tile < n.ntok);
     float top = kMinusInf, sum = 0.f;            // reference of the row's weights, and their sum
-    const uint32_t units = pair ? 2 * n.tiles : n.tiles, stride = S::kStreams;
-    const uint32_t o_base = o_count;
+    const uint32_t units = pair ? 2 * n.tiles : n.tiles;
     const uint32_t taddr_o = tmem + S::kO + (S::kStreams == 2 ? x * D : 0);
-    const bool works = S::kStreams == 2 || x == 0;
-    const bool simple = !p.mask && !p.positions;  // some row sees every position in [lo, hi)
     uint32_t done = 0;                           // units of this stream
-    for (uint32_t u = x; works && u < units; u += stride, ++done) {
-      const uint32_t buf = u & 1u, kt = pair ? u >> 1 : u, t0 = (n.first + kt) * kTok;
+    for (uint32_t u = S::kStreams == 2 ? x ^ n.turn : 0; works && u < units; u += S::kStreams, ++done) {
+      const uint32_t buf = (u + n.turn) & 1u, kt = pair ? u >> 1 : u, t0 = (n.first + kt) * kTok;
       alive = warp_wait(ctl.s_full[buf], s_parity >> buf & 1u, ctl, p.status);
       if (!alive) break;
       s_parity ^= 1u << buf;
       tc::fence_after();
       const uint32_t scores = tmem + buf * kTok;
+      const uint32_t words = t0 + kTok <= n.hi ? kWords : (n.hi - t0 + 31) / 32;  // what is left is not multiplied with V
       // Rows of V that no row of the item sees are made zeros, whatever they hold (a weight of 0 would not do). Of two tiles
       // the first one's product comes first.
       bool wipe = false, seen = false;
       if (t0 < n.lo_all || t0 + kTok > n.full || p.q_keep == 0) {
         uint32_t* by_words = ctl.seen[x][group & 1u][r >> 5];
-        const bool share = !simple && (!pair || x == 0);
+        const bool share = !simple && tile == 0;
 #pragma unroll 1
-        for (uint32_t w = 0; w < kWords; ++w) {
+        for (uint32_t w = 0; w < words; ++w) {
           uint32_t see = visible(p, row, n.c, t0 + w * 32);
           if (!__all_sync(0xffffffffu, see == ~0u) || p.q_keep == 0) {
             uint32_t s[32];
@@ -595,27 +665,21 @@ __device__ void soften(const TreeParams& p, Control<D>& ctl, uint8_t* slots) {
           if (!alive) break;
           const uint32_t w = r / 32 % kWords;
           const uint32_t(*by_warps)[4] = ctl.seen[x][group++ & 1u];
-          seen = (by_warps[0][w] | by_warps[1][w] | by_warps[2][w] | by_warps[3][w]) >> lane & 1u;
+          seen = w < words && ((by_warps[0][w] | by_warps[1][w] | by_warps[2][w] | by_warps[3][w]) >> lane & 1u);
         }
-        wipe = wipe && (!pair || x == 0);
+        wipe = wipe && tile == 0;
       }
       // Twice over the scores, 32 at a time, the next ones on their way: in registers all at once they and their code, straight
       // through, took longer to fetch than to run.
       float mx[4] = {kMinusInf, kMinusInf, kMinusInf, kMinusInf};
-      {
-        uint32_t s[2][32];
-        tc::ld32(s[0], scores);
 #pragma unroll 1
-        for (uint32_t w = 0; w < kWords; w += 2) {
+      for (uint32_t w = 0; w < words; ++w) {
+        uint32_t s[32];
+        tc::ld32(s, scores + w * 32);
+        tc::wait_ld();
+        touch(s);
 #pragma unroll
-          for (uint32_t k = 0; k < 2; ++k) {
-            tc::wait_ld();
-            touch(s[k]);
-            if (k == 0 || w + 2 < kWords) tc::ld32(s[k ^ 1], scores + (w + k + 1) * 32);
-#pragma unroll
-            for (uint32_t i = 0; i < 32; ++i) mx[i & 3u] = fmaxf(mx[i & 3u], __uint_as_float(s[k][i]));
-          }
-        }
+        for (uint32_t i = 0; i < 32; ++i) mx[i & 3u] = fmaxf(mx[i & 3u], __uint_as_float(s[i]));
       }
       const float most = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
       if (__any_sync(0xffffffffu, (most - top) * p.scale_log2 > kSlack<kBf16>)) {
@@ -625,7 +689,7 @@ __device__ void soften(const TreeParams& p, Control<D>& ctl, uint8_t* slots) {
         if (done) {
           // The stream's products so far have been done: of two streams, as the scores come after them; of one, the last may still run.
           if (S::kStreams == 1) {
-            alive = warp_wait(ctl.o_full[0], (o_base + u - 1) & 1u, ctl, p.status);
+            alive = warp_wait(ctl.summed, (sums_before + u - 1) & 1u, ctl, p.status);
             if (!alive) break;
             tc::fence_after();
           }
@@ -645,32 +709,25 @@ __device__ void soften(const TreeParams& p, Control<D>& ctl, uint8_t* slots) {
       const float ref = top == kMinusInf ? 0.f : top;
       const uint64_t ref2 = two(-ref, -ref), scale2 = two(p.scale_log2, p.scale_log2), top2 = two(kTop<kBf16>, kTop<kBf16>), minus2 = two(-1.f, -1.f);
       uint64_t sums[2] = {0, 0};
-      {
-        uint32_t s[2][32];
-        tc::ld32(s[0], scores);
 #pragma unroll 1
-        for (uint32_t w = 0; w < kWords; w += 2) {
+      for (uint32_t w = 0; w < words; ++w) {
+        uint32_t s[32], v[32];                   // in their place: 16 columns of weights, 16 of what their rounding left
+        tc::ld32(s, scores + w * 32);
+        tc::wait_ld();
+        touch(s);
 #pragma unroll
-          for (uint32_t k = 0; k < 2; ++k) {
-            tc::wait_ld();
-            touch(s[k]);
-            if (k == 0 || w + 2 < kWords) tc::ld32(s[k ^ 1], scores + (w + k + 1) * 32);
-            uint32_t v[32];                      // in their place: 16 columns of weights, 16 of what their rounding left
-#pragma unroll
-            for (uint32_t i = 0; i < 16; ++i) {
-              // (The difference is taken first: of scores beyond 2^24 the rounding of a score times the scale would be more than an exponent's worth.)
-              const float2 e = each(fma2(add2(two(__uint_as_float(s[k][2 * i]), __uint_as_float(s[k][2 * i + 1])), ref2), scale2, top2));
-              const float a = ptx::exp2_approx(e.x), b = ptx::exp2_approx(e.y);
-              const uint64_t ab = two(a, b);
-              sums[i & 1u] = add2(sums[i & 1u], ab);
-              v[i] = pack<kBf16>(a, b);
-              const float2 h = unpack<kBf16>(v[i]);
-              const float2 left = each(fma2(two(h.x, h.y), minus2, ab));
-              v[16 + i] = pack<kBf16>(left.x, left.y);
-            }
-            tc::st32(scores + (w + k) * 32, v);
-          }
+        for (uint32_t i = 0; i < 16; ++i) {
+          // (The difference is taken first: of scores beyond 2^24 the rounding of a score times the scale would be more than an exponent's worth.)
+          const float2 e = each(fma2(add2(two(__uint_as_float(s[2 * i]), __uint_as_float(s[2 * i + 1])), ref2), scale2, top2));
+          const float a = ptx::exp2_approx(e.x), b = ptx::exp2_approx(e.y);
+          const uint64_t ab = two(a, b);
+          sums[i & 1u] = add2(sums[i & 1u], ab);
+          v[i] = pack<kBf16>(a, b);
+          const float2 h = unpack<kBf16>(v[i]);
+          const float2 left = each(fma2(two(h.x, h.y), minus2, ab));
+          v[16 + i] = pack<kBf16>(left.x, left.y);
         }
+        tc::st32(scores + w * 32, v);
       }
       const float2 both = each(add2(sums[0], sums[1]));
       sum += both.x + both.y;
@@ -678,7 +735,7 @@ __device__ void soften(const TreeParams& p, Control<D>& ctl, uint8_t* slots) {
         const uint32_t ring = 2 * n.before + v_place(kt, n.tiles, pair), slot = ring % S::kSlots;
         alive = warp_wait(ctl.full[slot], ring / S::kSlots & 1u, ctl, p.status);
         if (!alive) break;
-        if (r < kTok && !seen) {
+        if (r < words * 32 && !seen) {
 #pragma unroll
           for (uint32_t c = 0; c < S::kChunks; ++c)
 #pragma unroll
@@ -693,72 +750,113 @@ __device__ void soften(const TreeParams& p, Control<D>& ctl, uint8_t* slots) {
       if (lane == 0) arrive(ctl.p_full[buf]);
     }
     if (!alive) break;
-    o_count += S::kStreams == 1 ? units : (done ? 1u : 0u);
-    if (works && done) {
-      // (Of one stream, the last product but one may still run as well, and a barrier tells only neighbouring phases apart.)
-      if (S::kStreams == 1 && done > 1) alive = warp_wait(ctl.o_full[0], (o_count - 2) & 1u, ctl, p.status);
-      alive = alive && warp_wait(ctl.o_full[S::kStreams == 2 ? x : 0], (o_count - 1) & 1u, ctl, p.status);
-      if (!alive) break;
+    sums_before += units;
+    // References and sums go to the warps that write rows out.
+    if (j) alive = warp_wait(ctl.stats_empty, (j - 1) & 1u, ctl, p.status);
+    if (done) ctl.stats[S::kStreams == 2 ? x : 0][r] = make_float2(top, sum);
+    __syncwarp();
+    if (lane == 0) {
+      arrive(ctl.stats_full);
+      arrive(ctl.note_empty[j % kNotes]);
     }
-    float w0 = 1.f, w1 = 0.f;                    // of the streams' sums
-    uint32_t c0 = 0, c1 = D;                     // this group's columns
-    uint32_t o0 = S::kStreams == 2 ? x * D : 0;
-    if (!pair) {
-      if (done) ctl.stats[S::kStreams == 2 ? x : 0][r] = make_float2(top, sum);
-      tc::fence_before();
-      __syncwarp();
-      if (lane == 0) arrive(ctl.joint);
-      alive = warp_wait(ctl.joint, joint++ & 1u, ctl, p.status);
-      if (!alive) break;
-      const float2 a = ctl.stats[0][r], b = S::kStreams == 2 && units > 1 ? ctl.stats[S::kStreams - 1][r] : make_float2(kMinusInf, 0.f);
-      top = fmaxf(a.x, b.x);
-      const float ref = top == kMinusInf ? 0.f : top;
+  }
+}
+
+// Four warps write rows out, or into the workspace where the item is cut: of one tile's two streams the sum.
+template <uint32_t D, bool kBf16>
+__device__ void write_rows(const TreeParams& p, Control<D>& ctl) {
+  using S = Shape<D>;
+  const uint32_t lane = threadIdx.x & 31u, r = threadIdx.x & 127u;
+  const uint32_t tmem = ctl.tmem + ((r & ~31u) << 16) + S::kO;
+  const uint32_t G = p.group, tt = tile_tokens(p), in_tile = r / G, my_head = r - in_tile * G;
+  const uint32_t heads = p.num_kv_heads * G;
+  bool alive = true;
+  for (uint32_t j = 0; alive; ++j) {
+    alive = warp_wait(ctl.note_full[j % kNotes], j / kNotes & 1u, ctl, p.status);
+    if (!alive) break;
+    const Note n = ctl.note[j % kNotes];
+    if (n.tiles == 0) break;
+    const bool pair = S::kStreams == 2 && n.ntok > tt;
+    alive = warp_wait(ctl.stats_full, j & 1u, ctl, p.status);
+    if (!alive) break;
+    float top[2], sum[2];                        // of tiles
+    float w0 = 1.f, w1 = 0.f;                    // of one tile's streams
+    const bool both = !pair && S::kStreams == 2 && n.tiles > 1;
+    if (pair) {
+#pragma unroll
+      for (uint32_t i = 0; i < 2; ++i) {
+        const float2 v = ctl.stats[(i ^ n.turn) % S::kStreams][r];
+        top[i] = v.x;
+        sum[i] = v.y;
+      }
+    } else {
+      const float2 a = ctl.stats[n.turn % S::kStreams][r], b = both ? ctl.stats[(n.turn ^ 1u) % S::kStreams][r] : make_float2(kMinusInf, 0.f);
+      top[0] = fmaxf(a.x, b.x);
+      const float ref = top[0] == kMinusInf ? 0.f : top[0];
       w0 = ptx::exp2_approx((a.x - ref) * p.scale_log2);
       w1 = ptx::exp2_approx((b.x - ref) * p.scale_log2);
-      sum = a.y * w0 + b.y * w1;
-      o0 = 0;
-      c0 = x * (D / 2);
-      c1 = c0 + D / 2;
+      sum[0] = a.y * w0 + b.y * w1;
+      top[1] = kMinusInf;
+      sum[1] = 0.f;
     }
+    __syncwarp();
+    if (lane == 0) arrive(ctl.stats_empty);
+    alive = warp_wait(ctl.o_done, j & 1u, ctl, p.status);
+    if (!alive) break;
     tc::fence_after();
-    const bool two = !pair && S::kStreams == 2 && units > 1;
-    const uint64_t tok = n.off + n.tok0 + my_tok;
-    const float inv = sum > 0.f ? 1.f / sum : sum;  // no weight at all: a row of zeros; not a number stays one
-    uint8_t* out = p.out + tok * p.out_stride + static_cast<uint64_t>(n.head * G + my_head) * D * 2;
-    const uint32_t part_row = pair ? x * 128 + r : r;
     float4* part = reinterpret_cast<float4*>(p.parts + static_cast<uint64_t>(n.slot) * S::kPart);
 #pragma unroll 1
-    for (uint32_t c = c0; c < c1; c += 32) {
-      uint32_t o[32];
-      __syncwarp();
-      tc::ld32(o, tmem + S::kO + o0 + c);
-      if (two) {
-        uint32_t more[32];
-        tc::ld32(more, tmem + S::kO + D + c);
-        tc::wait_ld();
-        touch(o);
-        touch(more);
+    for (uint32_t tile = 0; tile < (pair ? 2u : 1u); ++tile) {
+      const uint32_t my_tok = tile * tt + in_tile, part_row = tile * 128 + r;
+      const bool mine = r < tt * G && my_tok < n.ntok;
+      const uint64_t tok = n.off + n.tok0 + my_tok;
+      const float total = tile ? sum[1] : sum[0], inv = total > 0.f ? 1.f / total : total;  // no weight at all: a row of zeros; not a number stays one
+      uint4* out = reinterpret_cast<uint4*>(p.out + tok * p.out_stride + static_cast<uint64_t>(n.head * G + my_head) * D * 2);
+      const uint32_t o0 = S::kStreams == 2 ? ((tile ^ n.turn) & 1u) * D : 0, o1 = S::kStreams == 2 ? ((n.turn ^ 1u) & 1u) * D : 0;
+      if (!__any_sync(0xffffffffu, mine)) continue;
+#pragma unroll 1
+      for (uint32_t c = 0; c < D; c += 16) {
+        uint32_t o[16];
+        __syncwarp();
+        tc::ld16(o, tmem + o0 + c);
+        if (both) {
+          uint32_t more[16];
+          tc::ld16(more, tmem + o1 + c);
+          tc::wait_ld();
+          touch(o);
+          touch(more);
 #pragma unroll
-        for (uint32_t i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * w0 + __uint_as_float(more[i]) * w1);
-      } else {
-        tc::wait_ld();
-        touch(o);
-      }
-      if (!mine) continue;
-      if (n.slot == ~0u) {
-#pragma unroll
-        for (uint32_t i = 0; i < 4; ++i) {
-          uint32_t v[4];
-#pragma unroll
-          for (uint32_t e = 0; e < 4; ++e)
-            v[e] = pack<kBf16>(__uint_as_float(o[i * 8 + e * 2]) * inv, __uint_as_float(o[i * 8 + e * 2 + 1]) * inv);
-          *reinterpret_cast<uint4*>(out + (c + i * 8) * 2) = make_uint4(v[0], v[1], v[2], v[3]);
+          for (uint32_t i = 0; i < 16; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * w0 + __uint_as_float(more[i]) * w1);
+        } else {
+          tc::wait_ld();
+          touch(o);
         }
-      } else {
+        if (!mine) continue;
+        if (n.slot == ~0u) {
 #pragma unroll
-        for (uint32_t i = 0; i < 8; ++i)
-          part[(c / 4 + i) * S::kRows + part_row] = make_float4(__uint_as_float(o[i * 4]), __uint_as_float(o[i * 4 + 1]), __uint_as_float(o[i * 4 + 2]),
-                                                               __uint_as_float(o[i * 4 + 3]));
+          for (uint32_t i = 0; i < 2; ++i) {
+            uint32_t v[4];
+#pragma unroll
+            for (uint32_t e = 0; e < 4; ++e)
+              v[e] = pack<kBf16>(__uint_as_float(o[i * 8 + e * 2]) * inv, __uint_as_float(o[i * 8 + e * 2 + 1]) * inv);
+            out[c / 8 + i] = make_uint4(v[0], v[1], v[2], v[3]);
+          }
+        } else {
+#pragma unroll
+          for (uint32_t i = 0; i < 4; ++i)
+            part[(c / 4 + i) * S::kRows + part_row] = make_float4(__uint_as_float(o[i * 4]), __uint_as_float(o[i * 4 + 1]), __uint_as_float(o[i * 4 + 2]),
+                                                                 __uint_as_float(o[i * 4 + 3]));
+        }
+      }
+      if (mine) {
+        const float ref = tile ? top[1] : top[0];
+        if (n.slot == ~0u) {
+          if (p.lse) p.lse[tok * heads + n.head * G + my_head] = fmaf(ref, p.scale_log2, log2f(total) - kTop<kBf16>) * 0.6931471805599453f;
+        } else {
+          float* stats = reinterpret_cast<float*>(part) + S::kRows * D;
+          stats[part_row] = ref;
+          stats[S::kRows + part_row] = total;
+        }
       }
     }
     tc::fence_before();
@@ -766,15 +864,6 @@ __device__ void soften(const TreeParams& p, Control<D>& ctl, uint8_t* slots) {
     if (lane == 0) {
       arrive(ctl.o_empty);
       arrive(ctl.note_empty[j % kNotes]);
-    }
-    if (mine && (pair || x == 0)) {
-      if (n.slot == ~0u) {
-        if (p.lse) p.lse[tok * heads + n.head * G + my_head] = fmaf(top, p.scale_log2, log2f(sum) - kTop<kBf16>) * 0.6931471805599453f;
-      } else {
-        float* stats = reinterpret_cast<float*>(part) + S::kRows * D;
-        stats[part_row] = top;
-        stats[S::kRows + part_row] = sum;
-      }
     }
   }
 }
@@ -794,17 +883,19 @@ __global__ void __launch_bounds__(kThreads, 1) paged_tree_kernel(const TreeParam
     }
     for (uint32_t s = 0; s < kNotes; ++s) {
       ptx::mbar_init(ptx::smem_u32(&ctl.note_full[s]), 1);
-      ptx::mbar_init(ptx::smem_u32(&ctl.note_empty[s]), 9);
+      ptx::mbar_init(ptx::smem_u32(&ctl.note_empty[s]), 13);
     }
-    ptx::mbar_init(ptx::smem_u32(&ctl.o_empty), 8);
-    ptx::mbar_init(ptx::smem_u32(&ctl.joint), 8);
+    ptx::mbar_init(ptx::smem_u32(&ctl.o_done), 1);
+    ptx::mbar_init(ptx::smem_u32(&ctl.o_empty), 4);
+    ptx::mbar_init(ptx::smem_u32(&ctl.stats_full), 8);
+    ptx::mbar_init(ptx::smem_u32(&ctl.stats_empty), 4);
+    ptx::mbar_init(ptx::smem_u32(&ctl.summed), 1);
     ptx::mbar_init(ptx::smem_u32(&ctl.drain), 1);
     for (uint32_t s = 0; s < 2; ++s) {
       ptx::mbar_init(ptx::smem_u32(&ctl.q_full[s]), 1);
       ptx::mbar_init(ptx::smem_u32(&ctl.q_empty[s]), 1);
       ptx::mbar_init(ptx::smem_u32(&ctl.s_full[s]), 1);
       ptx::mbar_init(ptx::smem_u32(&ctl.p_full[s]), 4);
-      ptx::mbar_init(ptx::smem_u32(&ctl.o_full[s]), 1);
       ptx::mbar_init(ptx::smem_u32(&ctl.group[s]), 4);
     }
     ptx::fence_barrier_init();
@@ -813,7 +904,7 @@ __global__ void __launch_bounds__(kThreads, 1) paged_tree_kernel(const TreeParam
     asm volatile("prefetch.tensormap [%0];" ::"l"(&maps.q));
     ctl.dead = 0;
   }
-  if (warp == 9) tc::alloc(ptx::smem_u32(&ctl.tmem), 512);
+  if (warp == kIssueWarp) tc::alloc(ptx::smem_u32(&ctl.tmem), 512);
   ptx::launch_dependents();
   ptx::grid_dependency_wait();
 
@@ -849,15 +940,21 @@ __global__ void __launch_bounds__(kThreads, 1) paged_tree_kernel(const TreeParam
   const uint32_t size = static_cast<uint32_t>(min(max(share, 2ull + S::kItem), 0xffffffffull));
   __syncthreads();
 
-  if (warp < 8)
+  if (warp < kOutWarp) {
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoftRegs));
     soften<D, kBf16>(p, ctl, slots);
-  else if (warp == 8)
-    feed<D, false>(p, maps, ctl, queries, slots, before, size);
-  else if (warp == 10)
-    feed<D, true>(p, maps, ctl, queries, slots, before, size);
-  else if (lane == 0)
-    issue<D, kBf16>(p, ctl, queries, slots);
-  __syncwarp();
+  } else {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
+    if (warp < kFeedWarp)
+      write_rows<D, kBf16>(p, ctl);
+    else if (warp == kFeedWarp)
+      feed<D, false>(p, maps, ctl, queries, slots, before, size);
+    else if (warp == kFeedWarp + 1)
+      feed<D, true>(p, maps, ctl, queries, slots, before, size);
+    else if (warp == kIssueWarp && lane == 0)
+      issue<D, kBf16>(p, ctl, queries, slots);
+    __syncwarp();
+  }
 
   // Requests whose length or offsets are out of range: zeros, where the offsets name rows.
   const uint32_t heads = p.num_kv_heads * p.group;
@@ -875,7 +972,7 @@ __global__ void __launch_bounds__(kThreads, 1) paged_tree_kernel(const TreeParam
   }
   tc::fence_before();
   __syncthreads();
-  if (warp == 9) tc::dealloc(ctl.tmem, 512);
+  if (warp == kIssueWarp) tc::dealloc(ctl.tmem, 512);
 }
 
 // Items that were cut: the sum of their parts, weighted by their references, and the division. A warp takes 32 rows and 32 columns of an
