@@ -32,8 +32,8 @@ namespace ema {
 namespace {
 
 constexpr float kMinusInf = -INFINITY;
-// Warps: two groups of four for the softmax, four that write rows out, two that copy, one that issues the products (and an idle one).
-constexpr uint32_t kThreads = 512, kOutWarp = 8, kFeedWarp = 12, kIssueWarp = 14;
+// Warps: one that issues the products, two that copy (and an idle one), two groups of four for the softmax, four that write rows out.
+constexpr uint32_t kThreads = 512, kIssueWarp = 0, kFeedWarp = 1, kSoftWarp = 4, kOutWarp = 12;
 constexpr uint32_t kNotes = 4;
 // Registers of a thread: the launch has 128 for everybody; the last two groups of warps give up what the first two get.
 constexpr uint32_t kSoftRegs = 168, kOtherRegs = 88;
@@ -594,7 +594,7 @@ template <uint32_t D, bool kBf16>
 __device__ void soften(const TreeParams& p, Control<D>& ctl, uint8_t* slots) {
   using S = Shape<D>;
   constexpr uint32_t kTok = S::kTok, kWords = kTok / 32;
-  const uint32_t lane = threadIdx.x & 31u, x = threadIdx.x >> 7, r = threadIdx.x & 127u;
+  const uint32_t lane = threadIdx.x & 31u, x = (threadIdx.x >> 7) - kSoftWarp / 4, r = threadIdx.x & 127u;
   const uint32_t tmem = ctl.tmem + ((r & ~31u) << 16);  // this warp's part of tensor memory
   const uint32_t tt = tile_tokens(p), in_tile = r / p.group;
   const bool packed = r < tt * p.group;          // rows behind the tile's last token are padding
@@ -940,12 +940,12 @@ __global__ void __launch_bounds__(kThreads, 1) paged_tree_kernel(const TreeParam
   const uint32_t size = static_cast<uint32_t>(min(max(share, 2ull + S::kItem), 0xffffffffull));
   __syncthreads();
 
-  if (warp < kOutWarp) {
+  if (warp >= kSoftWarp && warp < kOutWarp) {
     asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoftRegs));
     soften<D, kBf16>(p, ctl, slots);
   } else {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
-    if (warp < kFeedWarp)
+    if (warp >= kOutWarp)
       write_rows<D, kBf16>(p, ctl);
     else if (warp == kFeedWarp)
       feed<D, false>(p, maps, ctl, queries, slots, before, size);
