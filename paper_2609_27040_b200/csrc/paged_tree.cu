@@ -494,8 +494,9 @@ __device__ void issue(const TreeParams& p, Control<D>& ctl, uint8_t* queries, ui
     if (!ready(ctl.note_full[j % kNotes], j / kNotes & 1u)) return false;
     const Note& n = ctl.note[j % kNotes];
     c.j = j;
-    c.u = 0;
     c.tiles = n.tiles;
+    if (n.tiles == 0) return true;  // the end: nothing else of the note has been written, the cursor's places stay where they are
+    c.u = 0;
     c.pair = S::kStreams == 2 && n.ntok > tt;
     c.units = c.pair ? 2 * n.tiles : n.tiles;
     c.before = 2 * n.before;
@@ -506,63 +507,61 @@ __device__ void issue(const TreeParams& p, Control<D>& ctl, uint8_t* queries, ui
   };
   uint64_t t0 = ptx::global_timer_ns();
   for (uint32_t polls = 1; !last || nb < na; ++polls) {
+    // What both want, asked for together and before anything is issued: what is issued runs for less time than it takes to ask.
+    if (!last && a.u == a.units && open(a) && a.tiles == 0) last = true;
+    if (nb < na && b.u == b.units) open(b);  // known: its scores have been issued
+    const uint32_t ka = a.pair ? a.u >> 1 : a.u, qa = a.pair ? a.u & 1u : a.place, first_a = a.u < (a.pair ? 2 : 1);
+    const uint32_t ring_a = a.before + k_place(ka, a.pair), slot_a = ring_a % S::kSlots, buf_a = na & 1u;
+    const uint32_t kb = b.pair ? b.u >> 1 : b.u, ring_b = b.before + v_place(kb, b.tiles, b.pair), slot_b = ring_b % S::kSlots, buf_b = nb & 1u;
+    const bool k_there = ready(ctl.full[slot_a], ring_a / S::kSlots & 1u), q_there = ready(ctl.q_full[qa], q_parity >> qa & 1u);
+    const bool p_there = ready(ctl.p_full[buf_b], nb >> 1 & 1u), v_there = ready(ctl.full[slot_b], ring_b / S::kSlots & 1u);
+    const bool o_free = b.u || b.j == 0 || ready(ctl.o_empty, (b.j - 1) & 1u);
+    const bool to_score = !last && a.u < a.units && k_there && (!first_a || q_there);
+    const bool to_sum = nb < na && p_there && v_there && o_free;
     bool moved = false;
-    if (!last && na - nb < 2 && (a.u < a.units || open(a))) {
-      if (a.tiles == 0) {
-        last = true;
-        continue;
-      }
-      const uint32_t kt = a.pair ? a.u >> 1 : a.u, q = a.pair ? a.u & 1u : a.place;
-      const uint32_t ring = a.before + k_place(kt, a.pair), slot = ring % S::kSlots, buf = na & 1u;
-      if (ready(ctl.full[slot], ring / S::kSlots & 1u) && (a.u >= (a.pair ? 2 : 1) || ready(ctl.q_full[q], q_parity >> q & 1u))) {
-        if (a.u < (a.pair ? 2 : 1)) q_parity ^= 1u << q;
-        tc::fence_after();
-        const uint64_t x = q0 + q * (S::kTileBytes >> 4), y = k0 + slot * (S::kSlotBytes >> 4);
+    if (to_sum) {
+      tc::fence_after();
+      const uint32_t stream = S::kStreams == 2 ? buf_b : 0, o = tmem + S::kO + stream * D, weights = tmem + buf_b * kTok;
+      const uint64_t y = v0 + slot_b * (S::kSlotBytes >> 4);
+      const uint32_t t = (b.first + kb) * kTok;
+      const bool add = b.u >= S::kStreams;
+      if (t + kTok <= b.hi) {
 #pragma unroll
-        for (uint32_t ks = 0; ks < D / 16; ++ks)
-          tc::mma_ss(tmem + buf * kTok, x + (ks / 4) * (128 * 128 >> 4) + (ks % 4) * 2, y + (ks / 4) * (kTok * 128 >> 4) + (ks % 4) * 2, scores, ks != 0);
-        tc::commit(ptx::smem_u32(&ctl.s_full[buf]));
-        if (!a.pair || (a.u & 1u)) tc::commit(ptx::smem_u32(&ctl.empty[slot]));
-        if (a.u + (a.pair ? 2 : 1) >= a.units) tc::commit(ptx::smem_u32(&ctl.q_empty[q]));
-        ++a.u;
-        ++na;
-        moved = true;
-      }
-    }
-    if (nb < na && (b.u < b.units || open(b))) {
-      const uint32_t kt = b.pair ? b.u >> 1 : b.u, buf = nb & 1u, stream = S::kStreams == 2 ? buf : 0;
-      const uint32_t ring = b.before + v_place(kt, b.tiles, b.pair), slot = ring % S::kSlots;
-      if (ready(ctl.p_full[buf], nb >> 1 & 1u) && ready(ctl.full[slot], ring / S::kSlots & 1u) &&
-          (b.u || b.j == 0 || ready(ctl.o_empty, (b.j - 1) & 1u))) {
-        tc::fence_after();
-        const uint32_t o = tmem + S::kO + stream * D, weights = tmem + buf * kTok;
-        const uint64_t y = v0 + slot * (S::kSlotBytes >> 4);
-        const uint32_t t = (b.first + kt) * kTok;
-        const bool add = b.u >= S::kStreams;
-        if (t + kTok <= b.hi) {
+        for (uint32_t part = 0; part < 2; ++part)
+#pragma unroll
+          for (uint32_t ks = 0; ks < kTok / 16; ++ks)
+            tc::mma_ts(o, weights + ks / 2 * 32 + part * 16 + ks % 2 * 8, y + ks * (16 * 128 >> 4), kSums, part || ks || add);
+      } else {                    // positions that nobody sees are left out
+        const uint32_t n = (b.hi - t + 15) / 16;
+#pragma unroll 1
+        for (uint32_t ks = 0; ks < n; ++ks)
 #pragma unroll
           for (uint32_t part = 0; part < 2; ++part)
-#pragma unroll
-            for (uint32_t ks = 0; ks < kTok / 16; ++ks)
-              tc::mma_ts(o, weights + ks / 2 * 32 + part * 16 + ks % 2 * 8, y + ks * (16 * 128 >> 4), kSums, part || ks || add);
-        } else {                  // positions that nobody sees are left out
-          const uint32_t n = (b.hi - t + 15) / 16;
-#pragma unroll 1
-          for (uint32_t ks = 0; ks < n; ++ks)
-#pragma unroll
-            for (uint32_t part = 0; part < 2; ++part)
-              tc::mma_ts(o, weights + ks / 2 * 32 + part * 16 + ks % 2 * 8, y + ks * (16 * 128 >> 4), kSums, part || ks || add);
-        }
-        if (!b.pair || (b.u & 1u)) tc::commit(ptx::smem_u32(&ctl.empty[slot]));
-        if (S::kStreams == 1) tc::commit(ptx::smem_u32(&ctl.summed));
-        ++b.u;
-        ++nb;
-        if (b.u == b.units) {
-          tc::commit(ptx::smem_u32(&ctl.o_done));
-          arrive(ctl.note_empty[b.j % kNotes]);
-        }
-        moved = true;
+            tc::mma_ts(o, weights + ks / 2 * 32 + part * 16 + ks % 2 * 8, y + ks * (16 * 128 >> 4), kSums, part || ks || add);
       }
+      if (!b.pair || (b.u & 1u)) tc::commit(ptx::smem_u32(&ctl.empty[slot_b]));
+      if (S::kStreams == 1) tc::commit(ptx::smem_u32(&ctl.summed));
+      ++b.u;
+      ++nb;
+      if (b.u == b.units) {
+        tc::commit(ptx::smem_u32(&ctl.o_done));
+        arrive(ctl.note_empty[b.j % kNotes]);
+      }
+      moved = true;
+    }
+    if (to_score && na - nb < 2) {
+      if (first_a) q_parity ^= 1u << qa;
+      tc::fence_after();
+      const uint64_t x = q0 + qa * (S::kTileBytes >> 4), y = k0 + slot_a * (S::kSlotBytes >> 4);
+#pragma unroll
+      for (uint32_t ks = 0; ks < D / 16; ++ks)
+        tc::mma_ss(tmem + buf_a * kTok, x + (ks / 4) * (128 * 128 >> 4) + (ks % 4) * 2, y + (ks / 4) * (kTok * 128 >> 4) + (ks % 4) * 2, scores, ks != 0);
+      tc::commit(ptx::smem_u32(&ctl.s_full[buf_a]));
+      if (!a.pair || (a.u & 1u)) tc::commit(ptx::smem_u32(&ctl.empty[slot_a]));
+      if (a.u + (a.pair ? 2 : 1) >= a.units) tc::commit(ptx::smem_u32(&ctl.q_empty[qa]));
+      ++a.u;
+      ++na;
+      moved = true;
     }
     if (moved) {
       polls = 0;
