@@ -139,7 +139,11 @@ class Case:
             size = vmax = 0.0
         z = z.masked_fill(~see, -math.inf)
         w = torch.softmax(z, -1).masked_fill(~see.any(1)[:, None], 0.0)
-        out = torch.einsum("hgmn,nhd->mhgd", w, v.masked_fill(~see.any(0)[:, None, None], 0.0)).reshape(m, Hkv * G, D)
+        v = v.masked_fill(~see.any(0)[:, None, None], 0.0)
+        out = torch.einsum("hgmn,nhd->mhgd", w, v).reshape(m, Hkv * G, D)
+        # Of requests with more rows than a tile of 128 has, a weight is one 16-bit number, off by half a step at most, and the sum of
+        # weights is taken before: an output is off by at most half a step times the weighted sum of magnitudes.
+        self.rounded = torch.finfo(self.dtype).eps / 2 * torch.einsum("hgmn,nhd->mhgd", w, v.abs()).reshape(m, Hkv * G, D) if m > 128 // G else 0.0
         return out, torch.logsumexp(z, -1).permute(2, 0, 1).reshape(m, -1), size, vmax
 
     def check(self):
@@ -154,7 +158,7 @@ class Case:
             # A step rescales a row's sum and rows when its largest score has grown by 2^4 or more, at most size log2(e) / 2 times (scores lie between -size
             # and size); the factor is the same for both, what is left are two roundings of 2^-24 each time.
             grown = (size * 1.45 / 2 + 2) * 2.0 ** -23
-            ok, worst = close(self.out[rows], ref, row_error(n, D, size, vmax) + 2 * grown * vmax, eps)
+            ok, worst = close(self.out[rows], ref, row_error(n, D, size, vmax) + 2 * grown * vmax + self.rounded, eps)
             assert ok, (i, n, self.m[i], worst)
             none = lse == -math.inf
             assert (self.lse[rows][none] == -math.inf).all() and not self.out[rows][none].any()
