@@ -953,9 +953,9 @@ __global__ void __launch_bounds__(kThreads, 1) paged_tree_kernel(const TreeParam
     total += ctl.warp_total[x];
   }
   before[tid] = sum;
-  // A part of less than two steps would leave a stream without work.
+  // A part of less than two steps would leave a group without work.
   const unsigned long long share = (total + gridDim.x - 1) / gridDim.x;
-  const uint32_t size = static_cast<uint32_t>(min(max(share, 2ull + S::kItem), 0xffffffffull));
+  const uint32_t size = static_cast<uint32_t>(min(max(share, 2ull), 0xffffffffull));
   __syncthreads();
 
   if (warp >= kSoftWarp && warp < kOutWarp) {
@@ -993,15 +993,18 @@ __global__ void __launch_bounds__(kThreads, 1) paged_tree_kernel(const TreeParam
   if (warp == kIssueWarp) tc::dealloc(ctl.tmem, 512);
 }
 
-// Items that were cut: the sum of their parts, weighted by their references, and the division. A warp takes 32 rows and 32 columns of an
-// item at a time, a row to a lane. Bound by latency: which items, their references and sums, their rows, each a trip to L2.
-constexpr uint32_t kJoinThreads = 256;
+// Items that were cut: the sum of their parts, weighted by their references, and the division. A warp takes 32 rows and 16 columns of an
+// item at a time, a row to a lane, four parts in flight; of an item in many parts the CTA's warps take every eighth part each. Bound by
+// latency: which items, then their parts, each a trip to L2.
+constexpr uint32_t kJoinThreads = 256, kJoinWarps = kJoinThreads / 32, kJoinMany = 8;
 static_assert(kTreeMaxCtas <= kJoinThreads, "a thread for every CTA's item");
 
 template <uint32_t D, bool kBf16>
 __global__ void __launch_bounds__(kJoinThreads) tree_join_kernel(const TreeParams p, const uint32_t ctas) {
   using S = Shape<D>;
-  __shared__ uint32_t list[kTreeMaxCtas][4], warp_count[kJoinThreads / 32];
+  constexpr uint32_t kCols = 16, kAhead = 4;
+  __shared__ uint32_t list[kTreeMaxCtas][4], warp_count[kJoinWarps];
+  __shared__ float rows[kJoinWarps][kCols + 2][32];
   ptx::launch_dependents();
   ptx::grid_dependency_wait();
   const uint32_t tid = threadIdx.x, lane = tid & 31u, warp = tid >> 5;
@@ -1011,7 +1014,7 @@ __global__ void __launch_bounds__(kJoinThreads) tree_join_kernel(const TreeParam
   __syncthreads();
   uint32_t at = __popc(ballot & ((1u << lane) - 1)), count = 0;
 #pragma unroll
-  for (uint32_t w = 0; w < kJoinThreads / 32; ++w) {
+  for (uint32_t w = 0; w < kJoinWarps; ++w) {
     if (w < warp) at += warp_count[w];
     count += warp_count[w];
   }
@@ -1023,47 +1026,115 @@ __global__ void __launch_bounds__(kJoinThreads) tree_join_kernel(const TreeParam
   }
   __syncthreads();
   const uint32_t G = p.group, tt = tile_tokens(p), heads = p.num_kv_heads * G;
-  constexpr uint32_t kSlabs = S::kRows / 32, kCols = D / 32;
-  const uint32_t tasks = count * kSlabs * kCols;
-  for (uint32_t x = blockIdx.x * (kJoinThreads / 32) + warp; x < tasks; x += gridDim.x * (kJoinThreads / 32)) {
-    const uint32_t* item = list[x / (kSlabs * kCols)];
-    const uint32_t k = item[0] & 0xffffu, parts = item[0] >> 16, tok0 = item[1], ntok = item[2], head = item[3];
-    const uint32_t slab = x / kCols % kSlabs, col = x % kCols, row = slab * 32 + lane;
-    const uint32_t tile = row >> 7, in_tile = (row & 127u) / G, h = (row & 127u) - in_tile * G, tok = tile * tt + in_tile;
-    if (in_tile >= tt || tok >= ntok) continue;
-    // Part i: the first one in the second place of the CTA where the item begins, the others in the first places of the next ones.
-    const float* first = p.parts + static_cast<uint64_t>(2 * k + 1) * S::kPart;
-    const float* rest = p.parts + static_cast<uint64_t>(2 * k) * S::kPart;
-    auto part = [&](uint32_t i) { return i ? rest + static_cast<uint64_t>(2 * i) * S::kPart : first; };
-    float top = kMinusInf, sum = 0.f;
-#pragma unroll 4
-    for (uint32_t i = 0; i < parts; ++i) top = fmaxf(top, part(i)[S::kRows * D + row]);
-    const float ref = top == kMinusInf ? 0.f : top;
-    float4 acc[8];
+  constexpr uint32_t kSlabs = S::kRows / 32, kPieces = D / kCols;
+  const uint32_t tasks = count * kSlabs * kPieces;
+
+  struct Task {
+    uint32_t k, parts, row, col, head, h;
+    uint64_t tok;
+    bool on;
+  };
+  auto task_of = [&](uint32_t x) {
+    const uint32_t* item = list[x / (kSlabs * kPieces)];
+    Task t;
+    t.k = item[0] & 0xffffu;
+    t.parts = item[0] >> 16;
+    t.head = item[3];
+    t.col = x % kPieces;
+    t.row = x / kPieces % kSlabs * 32 + lane;
+    const uint32_t in_tile = (t.row & 127u) / G, tok = (t.row >> 7) * tt + in_tile;
+    t.h = (t.row & 127u) - in_tile * G;
+    t.tok = static_cast<uint64_t>(item[1]) + tok;
+    t.on = in_tile < tt && tok < item[2];
+    return t;
+  };
+  // Parts first, first + step, ..: a row's reference, its sum of weights and 16 columns.
+  auto add_parts = [&](const Task& t, uint32_t first, uint32_t step, float& top, float& sum, float (&acc)[kCols]) {
+    top = kMinusInf;
+    sum = 0.f;
 #pragma unroll
-    for (uint32_t c = 0; c < 8; ++c) acc[c] = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 2
-    for (uint32_t i = 0; i < parts; ++i) {
-      const float* from = part(i);
-      const float w = ptx::exp2_approx((from[S::kRows * D + row] - ref) * p.scale_log2);
-      sum = fmaf(from[S::kRows * (D + 1) + row], w, sum);
+    for (uint32_t c = 0; c < kCols; ++c) acc[c] = 0.f;
+#pragma unroll 1
+    for (uint32_t i0 = first; i0 < t.parts; i0 += kAhead * step) {
+      float m[kAhead], l[kAhead];
+      float4 v[kAhead][kCols / 4];
 #pragma unroll
-      for (uint32_t c = 0; c < 8; ++c) {
-        const float4 v = reinterpret_cast<const float4*>(from)[(col * 8 + c) * S::kRows + row];
-        acc[c].x = fmaf(v.x, w, acc[c].x);
-        acc[c].y = fmaf(v.y, w, acc[c].y);
-        acc[c].z = fmaf(v.z, w, acc[c].z);
-        acc[c].w = fmaf(v.w, w, acc[c].w);
+      for (uint32_t k = 0; k < kAhead; ++k) {
+        const uint32_t i = i0 + k * step;
+        const bool there = i < t.parts;
+        // Part 0 lies in the second place of the CTA where the item begins, the others in the first places of the next ones.
+        const float* from = p.parts + static_cast<uint64_t>(there && i ? 2 * (t.k + i) : 2 * t.k + 1) * S::kPart;
+        m[k] = there ? from[S::kRows * D + t.row] : kMinusInf;
+        l[k] = there ? from[S::kRows * (D + 1) + t.row] : 0.f;
+#pragma unroll
+        for (uint32_t c = 0; c < kCols / 4; ++c)
+          v[k][c] = there ? reinterpret_cast<const float4*>(from)[(t.col * (kCols / 4) + c) * S::kRows + t.row] : make_float4(0.f, 0.f, 0.f, 0.f);
+      }
+      const float now = fmaxf(fmaxf(top, m[0]), fmaxf(fmaxf(m[1], m[2]), m[3])), ref = now == kMinusInf ? 0.f : now;
+      const float al = ptx::exp2_approx((top - ref) * p.scale_log2);
+      top = now;
+      sum *= al;
+#pragma unroll
+      for (uint32_t c = 0; c < kCols; ++c) acc[c] *= al;
+#pragma unroll
+      for (uint32_t k = 0; k < kAhead; ++k) {
+        const float w = ptx::exp2_approx((m[k] - ref) * p.scale_log2);
+        sum = fmaf(l[k], w, sum);
+#pragma unroll
+        for (uint32_t c = 0; c < kCols / 4; ++c) {
+          acc[4 * c] = fmaf(v[k][c].x, w, acc[4 * c]);
+          acc[4 * c + 1] = fmaf(v[k][c].y, w, acc[4 * c + 1]);
+          acc[4 * c + 2] = fmaf(v[k][c].z, w, acc[4 * c + 2]);
+          acc[4 * c + 3] = fmaf(v[k][c].w, w, acc[4 * c + 3]);
+        }
       }
     }
+  };
+  auto write = [&](const Task& t, float top, float sum, const float (&acc)[kCols]) {
     const float inv = sum > 0.f ? 1.f / sum : sum;
-    uint4* out = reinterpret_cast<uint4*>(p.out + static_cast<uint64_t>(tok0 + tok) * p.out_stride + (static_cast<uint64_t>(head * G + h) * D + col * 32) * 2);
+    uint4* out = reinterpret_cast<uint4*>(p.out + t.tok * p.out_stride + (static_cast<uint64_t>(t.head * G + t.h) * D + t.col * kCols) * 2);
 #pragma unroll
-    for (uint32_t c = 0; c < 4; ++c)
-      out[c] = make_uint4(pack<kBf16>(acc[2 * c].x * inv, acc[2 * c].y * inv), pack<kBf16>(acc[2 * c].z * inv, acc[2 * c].w * inv),
-                          pack<kBf16>(acc[2 * c + 1].x * inv, acc[2 * c + 1].y * inv), pack<kBf16>(acc[2 * c + 1].z * inv, acc[2 * c + 1].w * inv));
-    if (p.lse && col == 0)
-      p.lse[static_cast<uint64_t>(tok0 + tok) * heads + head * G + h] = fmaf(top, p.scale_log2, log2f(sum) - kTop<kBf16>) * 0.6931471805599453f;
+    for (uint32_t c = 0; c < kCols; c += 8)
+      out[c / 8] = make_uint4(pack<kBf16>(acc[c] * inv, acc[c + 1] * inv), pack<kBf16>(acc[c + 2] * inv, acc[c + 3] * inv),
+                              pack<kBf16>(acc[c + 4] * inv, acc[c + 5] * inv), pack<kBf16>(acc[c + 6] * inv, acc[c + 7] * inv));
+    if (p.lse && t.col == 0) p.lse[t.tok * heads + t.head * G + t.h] = fmaf(top, p.scale_log2, log2f(sum) - kTop<kBf16>) * 0.6931471805599453f;
+  };
+
+  float top, sum, acc[kCols];
+  for (uint32_t x = blockIdx.x * kJoinWarps + warp; x < tasks; x += gridDim.x * kJoinWarps) {
+    const Task t = task_of(x);
+    if (!t.on || t.parts > kJoinMany) continue;
+    add_parts(t, 0, 1, top, sum, acc);
+    write(t, top, sum, acc);
+  }
+  for (uint32_t x = blockIdx.x; x < tasks; x += gridDim.x) {
+    const Task t = task_of(x);
+    if (t.parts <= kJoinMany || !__any_sync(0xffffffffu, t.on)) continue;  // the same for all warps
+    if (t.on) add_parts(t, warp, kJoinWarps, top, sum, acc);
+    __syncthreads();              // the rows may still be read
+    if (t.on) {
+      rows[warp][kCols][lane] = top;
+      rows[warp][kCols + 1][lane] = sum;
+#pragma unroll
+      for (uint32_t c = 0; c < kCols; ++c) rows[warp][c][lane] = acc[c];
+    }
+    __syncthreads();
+    if (warp || !t.on) continue;
+    top = kMinusInf;
+#pragma unroll
+    for (uint32_t w = 0; w < kJoinWarps; ++w) top = fmaxf(top, rows[w][kCols][lane]);
+    const float ref = top == kMinusInf ? 0.f : top;
+    sum = 0.f;
+#pragma unroll
+    for (uint32_t c = 0; c < kCols; ++c) acc[c] = 0.f;
+#pragma unroll 1
+    for (uint32_t w = 0; w < kJoinWarps; ++w) {
+      const float f = ptx::exp2_approx((rows[w][kCols][lane] - ref) * p.scale_log2);
+      sum = fmaf(rows[w][kCols + 1][lane], f, sum);
+#pragma unroll
+      for (uint32_t c = 0; c < kCols; ++c) acc[c] = fmaf(rows[w][c][lane], f, acc[c]);
+    }
+    write(t, top, sum, acc);
   }
 }
 
