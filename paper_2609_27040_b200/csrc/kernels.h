@@ -340,7 +340,7 @@ struct PagesParams {
   uint32_t blocks[2];
   uint32_t* bits[2];           // a bit per block, zero before and after
   int32_t* map[2];             // [blocks[a]] entries that blocks have moved to
-  uint32_t* moved;             // how many have
+  uint32_t* moved;             // how many have, and two counters, zero before and after
   const int32_t* lens;         // [nseq]
   const int32_t* new_lens;
   int32_t* new_lens_out;       // fork: may be lens

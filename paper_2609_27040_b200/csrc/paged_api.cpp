@@ -150,7 +150,7 @@ bool layers_ok(const paged_cache_t* c, uint32_t n, ema::MoveParams& p) {
   return true;
 }
 
-// The start of the workspace of shares: the word that says how many blocks moved, a bit per block, then the entries that blocks move to.
+// The workspace of shares: words of the compaction (how many blocks moved, counters), a bit per block, then the entries that blocks move to.
 constexpr uint64_t kShareWords = 16;
 
 uint64_t bit_words(uint32_t blocks) { return (static_cast<uint64_t>(blocks) + 31) / 32; }

@@ -287,6 +287,17 @@ __global__ void __launch_bounds__(kThreads, 1) compact_plan_kernel(const PagesPa
       }
     }
   }
+  // How many free ids stay: every CTA counts a share of the stacks.
+  for (uint32_t a = 0; !bad && a < 2; ++a) {
+    uint32_t count = 0;
+    for (int32_t k = static_cast<int32_t>(blockIdx.x * kThreads + tid); k < top[a]; k += static_cast<int32_t>(gridDim.x * kThreads)) {
+      const uint32_t id = static_cast<uint32_t>(p.ids[a][k]);
+      count += id < limit[a];
+      if (id >= p.blocks[a]) ptx::report_status(p.status, kStatusInvalid);  // dropped as well
+    }
+    count = __reduce_add_sync(0xffffffffu, count);
+    if (lane == 0 && count) atomicAdd(p.moved + 1 + a, count);
+  }
   if (!last_cta(p.work, &flag)) return;
   constexpr uint32_t kEach = 8;                    // ids of a thread at a time
   uint32_t words[2], marked[2], mine[2], before[2], kept[2];
@@ -296,22 +307,10 @@ __global__ void __launch_bounds__(kThreads, 1) compact_plan_kernel(const PagesPa
     mine[a] = 0;
     for (uint32_t w = min(tid * run, words[a]), end = min(tid * run + run, words[a]); w < end; ++w) mine[a] += __popc(__ldcg(p.bits[a] + w));
     before[a] = block_exclusive(mine[a], warp_sums, marked[a]);
-    uint32_t count = 0;
-    for (int32_t k0 = 0; !bad && k0 < top[a]; k0 += kThreads * kEach) {
-      uint32_t id[kEach];  // read together: one after the other these reads and those below were 30 of 42 us
-#pragma unroll
-      for (uint32_t c = 0; c < kEach; ++c) {
-        const int32_t k = k0 + static_cast<int32_t>(c * kThreads + tid);
-        id[c] = k < top[a] ? static_cast<uint32_t>(p.ids[a][k]) : limit[a];
-      }
-#pragma unroll
-      for (uint32_t c = 0; c < kEach; ++c) {
-        count += id[c] < limit[a];
-        if (id[c] >= p.blocks[a] && k0 + static_cast<int32_t>(c * kThreads + tid) < top[a]) ptx::report_status(p.status, kStatusInvalid);  // dropped as well
-      }
-    }
-    block_exclusive(count, warp_sums, kept[a]);
+    kept[a] = __ldcg(p.moved + 1 + a);
   }
+  __syncthreads();
+  if (tid == 0) p.moved[1] = p.moved[2] = 0;
   const uint32_t need = marked[0] + marked[1];
   const int code = bad ? kStatusInvalid : need > static_cast<uint64_t>(kept[0]) + kept[1] ? kStatusNoSpace : need > p.ncopies ? kStatusInvalid : 0;
   if (!code) {
@@ -560,7 +559,10 @@ cudaError_t launch_fork(const PagesParams& p, int num_sms, cudaStream_t stream) 
 
 cudaError_t launch_compact(const PagesParams& p, int num_sms, cudaStream_t stream) {
   const unsigned grid = grid_of(p.nseq, p.max_blocks, num_sms);
-  const cudaError_t e = launch_ahead(compact_plan_kernel, grid, kThreads, 0, stream, p);
+  // The stacks are looked through as well, an id to a thread.
+  const uint64_t stacks = (static_cast<uint64_t>(p.capacity[0]) + p.capacity[1] + kThreads - 1) / kThreads, most = static_cast<uint64_t>(num_sms);
+  const unsigned plan = static_cast<unsigned>(stacks < grid ? grid : stacks < most ? stacks : most);
+  const cudaError_t e = launch_ahead(compact_plan_kernel, plan, kThreads, 0, stream, p);
   return e != cudaSuccess ? e : launch_ahead(compact_cells_kernel, grid, kThreads, 0, stream, p);
 }
 
