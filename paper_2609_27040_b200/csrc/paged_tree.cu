@@ -3,20 +3,21 @@
 //
 //   o = softmax(s q K^T) V over the context and those of the request's new tokens that the row sees, per query head.
 //
-// The query rows of one KV head (tokens x heads of the group) are tiles of 128, the M side of tcgen05 products; with one tile
-// the 64 KB of K and V of 128 positions (head_dim 128) take the tensor cores 1536 cycles and an SM's share of HBM about 2800,
-// with two tiles 3072: few drafted tokens are bound by HBM, two tiles by both about alike, prompts by the products.
-//   * An item is up to two tiles of one (request, KV head). The line of all items' positions, in steps of kTok, is cut into equal
-//     ranges, one to a CTA: an item may be cut, and its parts are joined by a second launch.
-//   * Warp 8 copies K and V (tiled bulk copies; the block format's order of 16-byte units within 128 bytes is the one that the
-//     tensor cores want, so a tile is used as it lies in the block), warp 9 issues the products, and two groups of four warps do the
-//     softmax, a row to a thread. Each group has a stream of its own: scores, weights and sums O in tensor memory. With two
-//     tiles a stream is a tile; with one, the streams take every other step and are added at the end. While one group works on
-//     its scores the tensor cores work for the other one. (head_dim 256: O takes half of the tensor memory, so there is one stream
-//     with two buffers for scores.)
+// The query rows of one KV head (tokens x heads of the group) are tiles of 128, the M side of tcgen05 products. Of a step of 128
+// positions (head_dim 128: 64 KB of K and V, 2470 cycles of an SM's share of HBM at 1.67 GHz) the scores take the tensor cores 560 cycles a tile, and
+// the product with V 770 or, with weights as two numbers, 1540: an operand in tensor memory takes 96 cycles where N = 128 would take 64.
+//   * An item is up to two tiles of one (request, KV head). The line of all items' steps is cut into equal ranges, one to a CTA: an item
+//     may be cut, and its parts are joined by a second launch.
+//   * Two warps copy K and V (tiled bulk copies; the block format's order of 16-byte units within 128 bytes is the one that the tensor
+//     cores want, so a tile is used as it lies in the block), one issues the products, two groups of four do the softmax, a row to a
+//     thread, and four write rows out while the next item goes on. Each softmax group has a stream of its own: scores, weights and
+//     sums O in tensor memory. With two tiles a stream is a tile; with one, the streams take every other step and are added at the
+//     end. While one group works on its scores the tensor cores work for the other one. (head_dim 256: O takes half of the tensor
+//     memory, so there is one tile, one stream with two buffers for scores, and one of the groups is idle.)
 //   * Weights take the place of their scores in tensor memory. Where a request's rows are one tile (drafted tokens, bound by HBM), they are the sum of two
 //     16-bit numbers (error 2^-16 for bf16), as in attention of single tokens; where they are more (prompts, bound by the products), one rounded number:
-//     that adds an error as large as the output's own rounding, and takes 0.90 ms instead of 1.10 (8 pieces of 900 to 2001 tokens). Sums and statistics are f32.
+//     that adds an error as large as the output's own rounding, and takes 0.90 ms instead
+//     of 1.10 (8 pieces of 900 to 2001 tokens). Sums and statistics are f32.
 //   * O is rescaled only when a row's maximum has grown by more than 2^kSlack; until then weights are larger than 1.
 #include <cuda.h>
 #include <cuda_bf16.h>
@@ -438,10 +439,15 @@ __device__ void feed(const TreeParams& p, const Maps& maps, Control<D>& ctl, uin
       k = 0;
       if (++head == p.num_kv_heads) {
         head = 0;
-        do {
-          ++seq;
-          r = seq < p.nseq ? request(p, seq) : Request{};
-        } while (seq < p.nseq && r.m == 0);
+        // The next request with new tokens, 32 looked at together (a batch may be mostly padding).
+        for (++seq; seq < p.nseq; seq += 32) {
+          const uint32_t some = __ballot_sync(0xffffffffu, seq + lane < p.nseq && request(p, seq + lane).m > 0);
+          if (some) {
+            seq += __ffs(some) - 1;
+            break;
+          }
+        }
+        r = seq < p.nseq ? request(p, seq) : Request{};
         items = (r.m + each - 1) / each;
       }
     }
@@ -931,8 +937,10 @@ __global__ void __launch_bounds__(kThreads, 1) paged_tree_kernel(const TreeParam
   const uint32_t run = (p.nseq + kThreads - 1) / kThreads, each = S::kStreams * tile_tokens(p);
   const uint32_t i0 = min(tid * run, p.nseq), i1 = min(i0 + run, p.nseq);
   unsigned long long mine = 0;
+  bool bad = false;
   for (uint32_t i = i0; i < i1; ++i) {
     const Request r = request(p, i);
+    bad |= !r.ok;
     unsigned long long one = 0;
     for (uint32_t k = 0; k * each < r.m; ++k) one += range_of<D>(p, r, k, each).tiles + S::kItem;
     mine += one * p.num_kv_heads;
@@ -956,7 +964,7 @@ __global__ void __launch_bounds__(kThreads, 1) paged_tree_kernel(const TreeParam
   // A part of less than two steps would leave a group without work.
   const unsigned long long share = (total + gridDim.x - 1) / gridDim.x;
   const uint32_t size = static_cast<uint32_t>(min(max(share, 2ull), 0xffffffffull));
-  __syncthreads();
+  bad = __syncthreads_or(bad);
 
   if (warp >= kSoftWarp && warp < kOutWarp) {
     asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoftRegs));
@@ -976,7 +984,7 @@ __global__ void __launch_bounds__(kThreads, 1) paged_tree_kernel(const TreeParam
 
   // Requests whose length or offsets are out of range: zeros, where the offsets name rows.
   const uint32_t heads = p.num_kv_heads * p.group;
-  for (uint32_t i = blockIdx.x; i < p.nseq; i += gridDim.x) {
+  for (uint32_t i = blockIdx.x; bad && i < p.nseq; i += gridDim.x) {
     if (request(p, i).ok) continue;
     if (tid == 0) ptx::report_status(p.status, kStatusInvalid);
     const int32_t a = p.offsets[i], b = p.offsets[i + 1];

@@ -303,12 +303,13 @@ def test_kernels_that_start_ahead_read_through_coherent_loads():
 
 
 def test_the_matrix_kernels_fit_their_cta():
-    """One CTA of 320 threads to an SM: ten warps, three of them on some schedulers."""
+    """One CTA of 512 threads to an SM, launched with 128 registers each, which its warps then divide among themselves; nothing spills
+    (300 bytes of spills in the softmax loops cost a third of the speed)."""
     res = build_mod.kernel_resources()
     main = {k: v for k, v in res.items() if "paged_tree_kernel" in k}
     assert len(main) == 6
     for name, r in main.items():
-        assert r["registers"] <= 168, (name, r)
+        assert r["registers"] == 128 and r["stack"] == r["spill_stores"] == r["spill_loads"] == 0, (name, r)
     for part in ("tree_join_kernel", "fork_kernel", "free_kernel", "compact_plan_kernel", "compact_cells_kernel", "copy_rows_kernel", "keep_rows_kernel"):
         found = [r for k, r in res.items() if part in k]
         assert found and all(r["spill_stores"] == r["spill_loads"] == 0 for r in found), part
