@@ -15,8 +15,8 @@
 //     end. While one group works on its scores the tensor cores work for the other one. (head_dim 256: O takes half of the tensor
 //     memory, so there is one tile, one stream with two buffers for scores, and one of the groups is idle.)
 //   * Weights take the place of their scores in tensor memory, each as one 16-bit number; sums of weights are taken before the rounding, in f32. (As
-//     the sum of two numbers, as in attention of single tokens, the errors of 64 requests' outputs would be 0.0017 of their size instead of 0.0019,
-//     0.0017 of which is the outputs' own rounding; the second product takes 768 cycles of the tensor cores a step, the rounding's rest
+//     the sum of two numbers, as in attention of single tokens, the errors of 64 requests' outputs would be 0.0017 of their size instead of 0.0023,
+//     as the outputs' own rounding is alone; the second product takes 768 cycles of the tensor cores a step, the rounding's rest
 //     a quarter of the softmax: 64 requests with 24 tokens each 142 us instead of 127, one call after the other.)
 //   * O is rescaled only when a row's maximum has grown by more than 2^kSlack; until then weights are larger than 1.
 #include <cuda.h>

@@ -439,3 +439,27 @@ def test_blocks_far_behind_the_arenas_start():
     c.tables[0, :10] = gpu(c.table_np[0, :10].tolist())
     c.cache = B.PagedCache(arena)
     c.run().check()
+
+
+@pytest.mark.parametrize("seed", range(12))
+def test_mixed_batches(seed):
+    """Requests of one tile, of two and of many behind one another in a CTA, padding between them, whatever the shape."""
+    rng = np.random.default_rng(1000 + seed)
+    D, T, G = int(rng.choice([64, 128, 256])), int(rng.choice([16, 32, 64])), int(rng.choice([1, 2, 4, 7, 16]))
+    Hkv = int(rng.integers(1, 5))
+    n = int(rng.integers(20, 60))
+    tile = 128 // G
+    m = [int(x) for x in rng.choice([0, 0, 1, 2, tile - 1, tile, tile + 1, 2 * tile, 2 * tile + 1, 5 * tile + 3], n)]
+    ctx = [int(rng.integers(0, 10 ** rng.integers(1, 4))) for _ in range(n)]
+    kind = ["chain", "tree", "any"][seed % 3]
+    window = int(rng.choice([0, 0, 50, 400]))
+    c = Case(ctx, m, Hkv, G, D, T, BF if seed % 2 else HF, lent=0.3, seed=seed, kind=kind, window=window, positions=bool(window and seed % 2))
+    c.run().check()
+
+
+def test_a_batch_that_is_mostly_padding():
+    n = 3000
+    ctx, m = [0] * n, [0] * n
+    for i in (0, 5, 1600, 1601, 2999):
+        ctx[i], m[i] = 100 + i // 7, 3
+    Case(ctx, m, 2, 4, 128, 16, BF, kind="tree").run().check()
