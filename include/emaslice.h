@@ -755,7 +755,8 @@ int paged_fork(const paged_fork_t* args, void* stream);
 
 /* Requests that end or shrink, where blocks may be shared: request i gives up the blocks past new_lens[i] tokens (those with
  * new_lens[i] >= lens[i] none). A block's id is pushed when its last holder has given it up: of the blocks freed by a call, the highest id of each arena
- * first. Tables are not changed. Status: EINVAL (a length or a top out of range: nothing has changed; an entry outside its arena: passed over; a
+ * first. Tables are not changed. (A request that is cut inside a block that others hold goes on sharing it, and must not grow from there: cut it at the
+ * block's beginning, or fork it into an empty request, which copies those rows.) Status: EINVAL (a length or a top out of range: nothing has changed; an entry outside its arena: passed over; a
  * block given up more often than it is held: pushed once; ids that exceed a stack's capacity: dropped). Returns EINVAL, ECUDA. */
 typedef struct {
   const paged_pool_t* pool;

@@ -1144,7 +1144,8 @@ cudaError_t launch(const TreeParams& p, const Maps& maps, uint32_t grid, int dev
   }
   const cudaError_t e = launch_ahead(paged_tree_kernel<D, kBf16>, grid, kThreads, kSharedBytes, stream, p, maps);
   if (e != cudaSuccess) return e;
-  return launch_ahead(tree_join_kernel<D, kBf16>, grid * 2, kJoinThreads, 0, stream, p, grid);
+  // Three CTAs of the join fit an SM (with two: 64 requests with 24 tokens each 130 us, now 125).
+  return launch_ahead(tree_join_kernel<D, kBf16>, grid * 3, kJoinThreads, 0, stream, p, grid);
 }
 
 template <uint32_t D>

@@ -637,3 +637,32 @@ def test_a_verification_step_with_forks_as_it_is_used():
     assert B.paged_copy_blocks(layers, gpu(moves), w.status, stream) == B.OK
     same_rows()
     assert all(0 <= e < len(held) for r in w.rows for e in r)
+
+
+def test_calls_without_requests():
+    """Tops are handed on; a compaction still takes ids off the stacks."""
+    w = World(3, 16, 8, (30, 10))
+    i32 = dict(dtype=torch.int32, device="cuda")
+    none, tables = torch.zeros(0, **i32), torch.zeros((0, 8), **i32)
+    assert B.paged_free(w.pool, w.shares, none, none, 16, tables, w.status) == B.OK
+    assert B.paged_fork(w.pool, w.shares, none, none, none, none, 16, tables, torch.zeros((0, 3), **i32), w.status) == B.OK
+    torch.cuda.synchronize()
+    w.same()
+    copies = torch.full((2, 3), 7, **i32)
+    assert B.paged_compact(w.pool, w.shares, gpu([20, 0]), none, 16, tables, copies, w.status) == B.OK
+    torch.cuda.synchronize()
+    w.stacks = [[x for x in w.stacks[0] if x < 20], []]
+    assert int(w.status) == 0 and not copies.any()
+    w.same()
+
+
+def test_a_request_cut_inside_a_shared_block_is_forked_to_go_on():
+    w = World(4, 16, 8, (30, 0))
+    w.grow([64, 0, 0, 0])
+    w.fork([0], [1])
+    w.release([64, 40, 0, 0])                                    # the third block stays shared, eight rows of it are this request's
+    assert w.fork([1], [2])[0][2] == 8
+    w.release([64, 0, 40, 0])
+    w.grow([64, 0, 60, 0])
+    w.same()
+    assert w.rows[2][2] != w.rows[0][2]
