@@ -463,3 +463,28 @@ def test_a_batch_that_is_mostly_padding():
     for i in (0, 5, 1600, 1601, 2999):
         ctx[i], m[i] = 100 + i // 7, 3
     Case(ctx, m, 2, 4, 128, 16, BF, kind="tree").run().check()
+
+
+@pytest.mark.parametrize("D", [64, 128, 256])
+def test_a_cache_in_the_second_arena_alone(D):
+    c = Case([200, 0, 33], [5, 9, 70], 2, 4, D, 16, BF, kind="tree")
+    c.local, c.lent = None, c.local
+    held = c.table_np < 0x7fffffff
+    c.table_np[held] = ~c.table_np[held]
+    c.tables.copy_(torch.from_numpy(c.table_np).to(torch.int32))
+    c.cache = B.PagedCache(None, c.lent)
+    c.run().check()
+
+
+def test_results_are_the_same_in_a_batch_and_alone():
+    """Items that are not cut are computed alike, whoever else is in the batch: here all of them, on both sides."""
+    c = Case([40, 90, 17, 60], [3, 5, 2, 7], 2, 4, 128, 16, BF, kind="tree")
+    want = c.run().out.clone()
+    for i in range(4):
+        one = Case([1], [1], 2, 4, 128, 16, BF, spare=0)
+        rows = slice(c.off[i], c.off[i + 1])
+        out = torch.zeros_like(want[rows]).contiguous()
+        assert B.paged_tree_attention(c.cache, c.tables[i:i + 1], c.lens_t[i:i + 1], gpu([0, c.m[i]]), c.q[rows], c.scale, out, one.work,
+                                      mask=c.mask[rows]) == B.OK
+        torch.cuda.synchronize()
+        assert torch.equal(out, want[rows])
