@@ -284,6 +284,7 @@ __device__ void feed(const TreeParams& p, const Maps& maps, Control<D>& ctl, uin
     n -= half;
   }
   uint64_t at = before[x];
+  ptx::fence_proxy_async();
   asm volatile("bar.sync 1, 64;" ::: "memory");  // both have read the sums: copies may take their place
   uint32_t seq = x * run, head = 0, k = 0, items = 0;
   Request r{};
@@ -928,6 +929,7 @@ __global__ void __launch_bounds__(kThreads, 1) paged_tree_kernel(const TreeParam
     total += ctl.warp_total[x];
   }
   before[tid] = sum;
+  ptx::fence_proxy_async();       // written (and read) before bulk copies of queries write there
   // A part of less than two steps would leave a group without work.
   const unsigned long long share = (total + gridDim.x - 1) / gridDim.x;
   const uint32_t size = static_cast<uint32_t>(min(max(share, 2ull), 0xffffffffull));
