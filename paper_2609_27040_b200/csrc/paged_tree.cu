@@ -648,6 +648,7 @@ __device__ void soften(const TreeParams& p, Control<D>& ctl, uint8_t* slots) {
             if (lane == 0) by_words[w] = see;
           }
         }
+        __syncwarp();            // one lane has stored: the warp together again for the aligned wait
         tc::wait_st();
         if (simple) {
           wipe = t0 < n.lo || t0 + kTok > n.hi;
@@ -736,6 +737,7 @@ __device__ void soften(const TreeParams& p, Control<D>& ctl, uint8_t* slots) {
         }
         ptx::fence_proxy_async();
       }
+      __syncwarp();              // some lanes have wiped rows
       tc::wait_st();
       tc::fence_before();
       __syncwarp();
@@ -896,6 +898,7 @@ __global__ void __launch_bounds__(kThreads, 1) paged_tree_kernel(const TreeParam
     asm volatile("prefetch.tensormap [%0];" ::"l"(&maps.q));
     ctl.dead = 0;
   }
+  __syncwarp();                   // one thread has been here, and it is the allocating warp's
   if (warp == kIssueWarp) tc::alloc(ptx::smem_u32(&ctl.tmem), 512);
   ptx::launch_dependents();
   ptx::grid_dependency_wait();
