@@ -491,7 +491,8 @@ __global__ void __launch_bounds__(kKeepThreads) keep_rows_kernel(const __grid_co
   const int32_t* keep = p.keep + i * p.keep_stride;
   for (int32_t j = static_cast<int32_t>(tid); !bad && j < n; j += kKeepThreads) {
     const int32_t k = keep[j];
-    bad = k < (j ? keep[j - 1] + 1 : 0) || len + static_cast<int64_t>(k) >= room;
+    // By itself, as the entries before may be anything: from j on (so that row j is in range where row k is), above the one before.
+    bad = k < j || (j && k <= keep[j - 1]) || len + static_cast<int64_t>(k) >= room;
     if (bad) break;
     for (uint32_t x = 0; x < 2; ++x) {
       const int32_t e = p.tables[i * p.table_stride + ((static_cast<uint32_t>(len) + (x ? k : j)) >> p.block_shift)];

@@ -523,6 +523,20 @@ def test_lists_that_are_refused(bad):
     assert torch.equal(r.arena.view(torch.int16), want)
 
 
+@pytest.mark.parametrize("bad", [[-9, -3], [-2 ** 31, -2 ** 31 + 1, 5], [0, -8, -7], list(range(-60, 0)), [0, 2 ** 31 - 1], [2 ** 31 - 1, -2 ** 31],
+                                 list(range(10)) + [0] + list(range(49)), list(range(60, 0, -1)), [0, 1] * 30])
+@pytest.mark.parametrize("at", [0, 1, 36])
+def test_lists_whose_entries_pass_one_by_one(bad, at):
+    """Entries below 0 that rise, and entries of long lists that are far below their place: none of them leads out of the request's
+    cells, with a request at its first row and one that reaches to its table's last cell."""
+    r = Rows([at, 30], 12, 16, 2, 64, 2, BF)                       # 48 positions in either row of the table
+    r.tables = gpu([row[:3] for row in r.table.tolist()])
+    r.tables[r.tables == 0x7fffffff] = 0
+    want = r.expected([[], [3, 5]])
+    r.call([bad, [3, 5]], 64, status=EINVAL)
+    assert torch.equal(r.arena.view(torch.int16), want)
+
+
 def test_entries_of_accepted_rows_outside_their_arena():
     r = Rows([14, 30], 12, 16, 2, 64, 2, BF)
     want = r.expected([[], [3, 5]])
