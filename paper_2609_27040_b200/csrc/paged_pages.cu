@@ -290,7 +290,8 @@ __global__ void __launch_bounds__(kThreads, 1) compact_plan_kernel(const PagesPa
   // How many free ids stay: every CTA counts a share of the stacks.
   for (uint32_t a = 0; !bad && a < 2; ++a) {
     uint32_t count = 0;
-    for (int32_t k = static_cast<int32_t>(blockIdx.x * kThreads + tid); k < top[a]; k += static_cast<int32_t>(gridDim.x * kThreads)) {
+    // (unsigned: the sum of a place and a stride may pass 2^31)
+    for (uint32_t k = blockIdx.x * kThreads + tid; k < static_cast<uint32_t>(top[a]); k += gridDim.x * kThreads) {
       const uint32_t id = static_cast<uint32_t>(p.ids[a][k]);
       count += id < limit[a];
       if (id >= p.blocks[a]) ptx::report_status(p.status, kStatusInvalid);  // dropped as well

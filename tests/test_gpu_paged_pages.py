@@ -353,6 +353,23 @@ def test_ids_beyond_the_limits_and_strange_ones_leave_the_stacks():
     w.same()
 
 
+def test_a_stack_of_nearly_2_to_the_31_ids():
+    """Places on a stack are counted without wrapping, in front and at the end of the largest stack that a pool may have."""
+    n = 2 ** 31 - 1
+    i32 = dict(dtype=torch.int32, device="cuda")
+    ids = torch.full((n,), 5, **i32)
+    ids[0], ids[n - 2], ids[n - 1] = 1, 2, 0
+    free, status = gpu([n, 0]), gpu([0])
+    pool = B.PagedPool(ids, None, free, free, torch.zeros(1, **i32))
+    shares = B.PagedShares(torch.zeros(6, **i32), None, torch.zeros(B.paged_shares_workspace(6, 0), dtype=torch.uint8, device="cuda"))
+    tables, copies = gpu([[4, 3, 0]]), torch.full((3, 3), 7, **i32)
+    torch.cuda.synchronize()
+    assert B.paged_compact(pool, shares, gpu([4, 0]), gpu([20]), 16, tables, copies, status) == B.OK
+    torch.cuda.synchronize()
+    assert int(status) == 0 and free.tolist() == [2, 0] and ids[:2].tolist() == [1, 2]
+    assert tables.tolist() == [[0, 3, 0]] and copies.tolist() == [[4, 0, 16], [0, 0, 0], [0, 0, 0]]
+
+
 def test_a_step_of_frees_forks_and_copies_captured_and_replayed():
     """Beams: every replay frees the forks and makes others, from device arrays that change between replays."""
     T, n = 16, 10
