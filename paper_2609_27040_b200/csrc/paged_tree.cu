@@ -678,7 +678,8 @@ __device__ void soften(const TreeParams& p, Control<D>& ctl, uint8_t* slots) {
         for (uint32_t i = 0; i < 32; ++i) mx[i & 3u] = fmaxf(mx[i & 3u], __uint_as_float(s[i]));
       }
       const float most = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
-      if (__any_sync(0xffffffffu, (most - top) * p.scale_log2 > kSlack<kBf16>)) {
+      // (Rows of nobody's have no say: what they hold would move the others' references, and with them the rounding of their weights.)
+      if (__any_sync(0xffffffffu, mine && (most - top) * p.scale_log2 > kSlack<kBf16>)) {
         const float now = fmaxf(top, most), al = now == kMinusInf ? 1.f : ptx::exp2_approx((top - now) * p.scale_log2);
         top = now;
         sum *= al;

@@ -488,3 +488,27 @@ def test_results_are_the_same_in_a_batch_and_alone():
                                       mask=c.mask[rows]) == B.OK
         torch.cuda.synchronize()
         assert torch.equal(out, want[rows])
+
+
+@pytest.mark.parametrize("D,G,m,ctx", [(128, 4, [5, 9, 3], [700, 1500, 900]), (128, 3, [42, 37, 40], [800, 513, 2000]), (128, 7, [18, 17, 16], [640, 900, 1300]),
+                                       (64, 4, [30, 3, 45], [900, 1500, 700]), (256, 3, [42, 5, 33], [500, 700, 1100]), (128, 33, [3, 1, 2], [700, 800, 1200])])
+@pytest.mark.parametrize("dtype", [BF, HF])
+def test_results_do_not_depend_on_rows_that_are_nobodys(D, G, m, ctx, dtype):
+    """To the bit, with steps that no mask touches: the queries of other requests and of rows that the offsets leave out, and what a
+    kernel before has left in shared memory where a group's heads leave rows of a tile free."""
+    n = 48                                                         # more items than CTAs: several steps of one lie in a CTA
+    c = Case((ctx * n)[:n], (m * n)[:n], 4, G, D, 16, dtype, seed=G + D, kind="tree", spare=9)
+    c.offsets.copy_(gpu([x + 4 for x in c.off]))                   # four rows in front, five behind
+    c.mask[4:4 + c.tokens] = c.mask[:c.tokens].clone()
+    first, lse = c.run().out.clone(), c.lse.clone()
+    q = c.q.clone()
+    dirt = Case([900] * 40, [50] * 40, 4, 4, 128, 16, dtype, seed=1)
+    dirt.q *= 100.0
+    for part in range(3):
+        mine = torch.cat([torch.arange(4 + c.off[i], 4 + c.off[i + 1]) for i in range(n) if i % 3 == part]).cuda()
+        for factor in (100.0, -30.0, 0.0):
+            c.q.copy_(q * factor)
+            c.q[mine] = q[mine]
+            dirt.run()
+            c.run()
+            assert torch.equal(c.out[mine], first[mine]) and torch.equal(c.lse[mine], lse[mine]), (part, factor)
