@@ -675,7 +675,8 @@ int paged_decode_diff(const paged_decode_t* args, void* stream);
  * offsets [nseq + 1] rises from a number >= 0 to one <= ntok; rows that it leaves out are not touched. A token that sees nothing gets zeros and
  * minus infinity. Rows of V that no token of a request sees may hold anything, as may rows of K that a token does not see; the
  * other rows of V must be finite, as for paged_decode_tables. Arithmetic as there: 16-bit products, f32 accumulation and softmax, result
- * rounded once; but a weight is one 16-bit number (there the sum of two), off by half a step at most. The result does not depend on timing.
+ * rounded once; a weight is the sum of two 16-bit numbers as there for requests with m G <= 128, and one such number, off by half a step at
+ * most, for those with more. The result does not depend on timing.
  * workspace: paged_tree_workspace bytes; it needs no clearing.
  * Status: EINVAL (a length or an offset out of range, fewer positions than tokens: the request's rows are zeros where its offsets name any;
  * an entry outside its arena: reads as zeros), ETIMEOUT. Returns EINVAL, ESCRATCH, ECUDA. Two launches. */

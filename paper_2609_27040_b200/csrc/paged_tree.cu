@@ -5,7 +5,7 @@
 //
 // The query rows of one KV head (tokens x heads of the group) are tiles of 128, the M side of tcgen05 products. Of a step of 128
 // positions (head_dim 128: 64 KB of K and V, 2470 cycles of an SM's share of HBM at 1.67 GHz) the scores take the tensor cores 560 cycles a tile, and
-// the product with V 770: an operand in tensor memory takes 96 cycles where N = 128 would take 64.
+// the product with V 770 or, with weights as two numbers, 1540: an operand in tensor memory takes 96 cycles where N = 128 would take 64.
 //   * An item is up to two tiles of one (request, KV head). The line of all items' steps is cut into equal ranges, one to a CTA: an item
 //     may be cut, and its parts are joined by a second launch.
 //   * Two warps copy K and V (tiled bulk copies; the block format's order of 16-byte units within 128 bytes is the one that the tensor
@@ -14,15 +14,19 @@
 //     sums O in tensor memory. With two tiles a stream is a tile; with one, the streams take every other step and are added at the
 //     end. While one group works on its scores the tensor cores work for the other one. (head_dim 256: O takes half of the tensor
 //     memory, so there is one tile, one stream with two buffers for scores, and one of the groups is idle.)
-//   * Weights take the place of their scores in tensor memory, each as one 16-bit number; sums of weights are taken before the rounding, in f32. (As
-//     the sum of two numbers, as in attention of single tokens, the errors of 64 requests' outputs would be 0.0017 of their size instead of 0.0023,
-//     as the outputs' own rounding is alone; the second product takes 768 cycles of the tensor cores a step, the rounding's rest
-//     a quarter of the softmax: 64 requests with 24 tokens each 142 us instead of 127, one call after the other.)
+//   * Weights take the place of their scores in tensor memory. Where a request's rows of a KV head are one tile (drafted tokens, which are compared
+//     with and go on as single tokens; bound by HBM), they are the sum of two 16-bit numbers (error 2^-16 for bf16), as in attention of single tokens.
+//     Where they are more (prompts; bound by the products and the softmax), a weight is one rounded number, which adds an error as large as the
+//     output's own rounding. One number or two: 64 requests with 24 tokens each 129 / 134 us, outputs off by 0.0023 / 0.0017 of their size (their own
+//     rounding is 0.0017); 200 with up to 9 tokens and a window 219 / 251; 8 pieces of prompts 910 / 1066, five long requests of two tiles 779 / 936.
+//     Sums of weights are taken before the rounding, in f32.
 //   * O is rescaled only when a row's maximum has grown by more than 2^kSlack; until then weights are larger than 1.
 #include <cuda.h>
 #include <cuda_bf16.h>
+#include <cuda_fp16.h>
 
 #include <atomic>
+#include <type_traits>
 
 #include "kernels.h"
 #include "ptx.cuh"
@@ -142,6 +146,12 @@ __device__ __forceinline__ uint32_t pack(float lo, float hi) {
   return r;
 }
 
+template <bool kBf16>
+__device__ __forceinline__ float2 unpack(uint32_t v) {
+  if constexpr (kBf16) return make_float2(__uint_as_float(v << 16), __uint_as_float(v & 0xffff0000u));
+  return __half22float2(*reinterpret_cast<const __half2*>(&v));
+}
+
 // Weights are 2^kTop at a row's reference, and 2^(kTop + kSlack) at most: an fp16 number ends at 65504 and has no bits below 2^-24.
 template <bool kBf16>
 __device__ constexpr float kTop = kBf16 ? 0.f : 11.f;
@@ -259,6 +269,9 @@ __device__ __forceinline__ uint32_t visible(const TreeParams& p, const Row& r, u
   }
   return see;
 }
+
+// Whether a request's rows of a KV head are more than a tile: its weights are one rounded number then.
+__device__ __forceinline__ bool many_rows(const Note& n, uint32_t tile_tokens) { return n.m > tile_tokens; }
 
 // Places in the ring of K and V tiles, in the order in which the products take them, which is the order in which they come free: of an
 // item of n steps K0 V0 K1 V1 .. with two tiles of queries; with one, whose scores are a step ahead of its sums, K0 K1 V0 K2 V1 ..
@@ -483,7 +496,7 @@ __device__ void issue(const TreeParams& p, Control<D>& ctl, uint8_t* queries, ui
   const uint64_t k0 = tc::operand(ptx::smem_u32(slots), 16, 1024), v0 = tc::operand(ptx::smem_u32(slots), kTok * 128, 1024);
   struct Cursor {
     uint32_t j, u, units, tiles, before, place, first, hi;
-    bool pair;
+    bool pair, many;
   };
   Cursor a{}, b{};                // next scores, next sums: item, unit
   a.j = b.j = ~0u;
@@ -499,6 +512,7 @@ __device__ void issue(const TreeParams& p, Control<D>& ctl, uint8_t* queries, ui
     if (n.tiles == 0) return true;  // the end: nothing else of the note has been written, the cursor's places stay where they are
     c.u = 0;
     c.pair = S::kStreams == 2 && n.ntok > tt;
+    c.many = many_rows(n, tt);
     c.units = c.pair ? 2 * n.tiles : n.tiles;
     c.before = 2 * n.before;
     c.place = n.q;
@@ -526,14 +540,22 @@ __device__ void issue(const TreeParams& p, Control<D>& ctl, uint8_t* queries, ui
       const uint64_t y = v0 + slot_b * (S::kSlotBytes >> 4);
       const uint32_t t = (b.first + kb) * kTok;
       const bool add = b.u >= S::kStreams;
-      auto sum = [&](uint32_t ks, bool first) { tc::mma_ts(o, weights + ks / 2 * 32 + ks % 2 * 8, y + ks * (16 * 128 >> 4), kSums, !first || add); };
+      auto sum = [&](uint32_t ks, uint32_t part, bool first) {
+        tc::mma_ts(o, weights + ks / 2 * 32 + part * 16 + ks % 2 * 8, y + ks * (16 * 128 >> 4), kSums, !first || add);
+      };
       if (t + kTok <= b.hi) {
 #pragma unroll
-        for (uint32_t ks = 0; ks < kTok / 16; ++ks) sum(ks, ks == 0);
+        for (uint32_t ks = 0; ks < kTok / 16; ++ks) sum(ks, 0, ks == 0);
+        if (!b.many)
+#pragma unroll
+          for (uint32_t ks = 0; ks < kTok / 16; ++ks) sum(ks, 1, false);
       } else {                    // positions that nobody sees are left out
         const uint32_t n = (b.hi - t + 15) / 16;
 #pragma unroll 1
-        for (uint32_t ks = 0; ks < n; ++ks) sum(ks, ks == 0);
+        for (uint32_t ks = 0; ks < n; ++ks) {
+          sum(ks, 0, ks == 0);
+          if (!b.many) sum(ks, 1, false);
+        }
       }
       if (!b.pair || (b.u & 1u)) tc::commit(ptx::smem_u32(&ctl.empty[slot_b]));
       if (S::kStreams == 1) tc::commit(ptx::smem_u32(&ctl.summed));
@@ -704,25 +726,40 @@ __device__ void soften(const TreeParams& p, Control<D>& ctl, uint8_t* slots) {
         }
       }
       const float ref = top == kMinusInf ? 0.f : top;
-      const uint64_t ref2 = two(-ref, -ref), scale2 = two(p.scale_log2, p.scale_log2), top2 = two(kTop<kBf16>, kTop<kBf16>);
+      const uint64_t ref2 = two(-ref, -ref), scale2 = two(p.scale_log2, p.scale_log2), top2 = two(kTop<kBf16>, kTop<kBf16>), minus2 = two(-1.f, -1.f);
       uint64_t sums[2] = {0, 0};
-      // In the scores' place: of 32 columns the first 16 become the weights.
+      // In the scores' place: of 32 columns the first 16 become the weights, the others what their rounding left where that is wanted.
+      auto weigh = [&](auto rest) {
+        constexpr bool kRest = decltype(rest)::value;
 #pragma unroll 1
-      for (uint32_t w = 0; w < words; ++w) {
-        uint32_t s[32], v[16];
-        tc::ld32(s, scores + w * 32);
-        tc::wait_ld();
-        touch(s);
+        for (uint32_t w = 0; w < words; ++w) {
+          uint32_t s[32], v[kRest ? 32 : 16];
+          tc::ld32(s, scores + w * 32);
+          tc::wait_ld();
+          touch(s);
 #pragma unroll
-        for (uint32_t i = 0; i < 16; ++i) {
-          // (The difference is taken first: of scores beyond 2^24 the rounding of a score times the scale would be more than an exponent's worth.)
-          const float2 e = each(fma2(add2(two(__uint_as_float(s[2 * i]), __uint_as_float(s[2 * i + 1])), ref2), scale2, top2));
-          const float a = ptx::exp2_approx(e.x), b = ptx::exp2_approx(e.y);
-          sums[i & 1u] = add2(sums[i & 1u], two(a, b));
-          v[i] = pack<kBf16>(a, b);
+          for (uint32_t i = 0; i < 16; ++i) {
+            // (The difference is taken first: of scores beyond 2^24 the rounding of a score times the scale would be more than an exponent's worth.)
+            const float2 e = each(fma2(add2(two(__uint_as_float(s[2 * i]), __uint_as_float(s[2 * i + 1])), ref2), scale2, top2));
+            const float a = ptx::exp2_approx(e.x), b = ptx::exp2_approx(e.y);
+            const uint64_t ab = two(a, b);
+            sums[i & 1u] = add2(sums[i & 1u], ab);
+            v[i] = pack<kBf16>(a, b);
+            if constexpr (kRest) {
+              const float2 h = unpack<kBf16>(v[i]), left = each(fma2(two(h.x, h.y), minus2, ab));
+              v[16 + i] = pack<kBf16>(left.x, left.y);
+            }
+          }
+          if constexpr (kRest)
+            tc::st32(scores + w * 32, v);
+          else
+            tc::st16(scores + w * 32, v);
         }
-        tc::st16(scores + w * 32, v);
-      }
+      };
+      if (many_rows(n, tt))
+        weigh(std::false_type{});
+      else
+        weigh(std::true_type{});
       const float2 both = each(add2(sums[0], sums[1]));
       sum += both.x + both.y;
       if (wipe) {
