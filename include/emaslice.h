@@ -668,6 +668,9 @@ int paged_decode_diff(const paged_decode_t* args, void* stream);
  *     mask given  (a tree) new token b where bit b of the token's mask is set (its own bit as any other), and the context; with a
  *                 window the context's positions above the token's position - window
  *   The token's position is positions[t], taken into c .. lens[i] - 1, or c + j where that is NULL.
+ *   So a window takes away new tokens of a chain, but none that a mask names. A tree deeper than the window, which is to give what decoding
+ *   its branches token by token with that window gives, needs two things of the caller: bits of ancestors `window` or more levels above the token
+ *   cleared, and positions (c + the token's depth); without positions the window goes by the token's index j, which is the depth in a chain alone.
  *   q, out     [ntok] rows of [num_heads][head_dim], q_stride / out_stride bytes apart
  *   mask       [ntok] rows of mask_words 64-bit words, mask_stride words apart: bit b of a row is bit b % 64 of word b / 64; tokens
  *              past the row's words are not seen, bits past m mean nothing

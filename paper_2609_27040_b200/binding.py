@@ -652,7 +652,8 @@ def paged_tree_workspace(cache: PagedCache, num_heads: int) -> int:
 def paged_tree_attention(cache: PagedCache, tables, lens, offsets, q, sm_scale: float, out, workspace, mask=None, lse=None, window: int = 0,
                          positions=None, status=None, stream=None) -> int:
     """Attention of several new tokens per request: a tree of drafted tokens (`mask`, int64 [tokens, words], bit b of a row: the token sees new
-    token b of its request) or a chain. stream=None: the legacy default stream."""
+    token b of its request) or a chain. A window takes away new tokens of a chain, but none that a mask names: clear the bits of ancestors that
+    are `window` or more levels up, and give `positions` (context + depth). stream=None: the legacy default stream."""
     return (_calls or _torch_calls()).tree(cache._addr, cache._dev, tables, lens, offsets, q, sm_scale, out, workspace, mask, lse, window,
                                            positions, status, stream)
 

@@ -548,3 +548,25 @@ def test_one_token_and_decode_differ_by_their_own_rounding(dtype):
         slack = row_error(c.lens[i], 128, size, vmax)
         far = torch.finfo(dtype).eps * (ref[0].abs() + slack) + 2 * slack + 2.0 ** -24
         assert bool(((out[i].double() - c.out[i].double()).abs() <= far).all()), i
+
+
+@pytest.mark.parametrize("window", [1, 3, 40])
+def test_a_window_and_a_mask(window):
+    """Drafts deeper than the window: a chain under a window, the same as a mask whose caller has cleared the ancestors that the window leaves out
+    (both: what decoding token by token gives), and as one that names them, which are seen then."""
+    ctx, m, bf = [0, 5, 129, 700], [9, 20, 60, 33], torch.finfo(BF).eps
+    chain = Case(ctx, m, 2, 2, 128, 16, BF, seed=window, window=window).run().check()
+    cleared = Case(ctx, m, 2, 2, 128, 16, BF, seed=window, window=window, kind="tree")
+    for name in ("local", "tables", "table_np", "cache", "q"):
+        setattr(cleared, name, getattr(chain, name))
+    for back in (window, 10 ** 6):
+        cleared.bits = [[(1 << j + 1) - 1 & ~((1 << max(0, j + 1 - back)) - 1) for j in range(k)] for k in m]
+        cleared.mask[:cleared.tokens, 0] = gpu([b - (1 << 64) if b >> 63 else b for row in cleared.bits for b in row], torch.int64)
+        for i in range(4):                                         # a window longer than the chain takes none of it away
+            assert np.array_equal(chain.sees(i), cleared.sees(i)) == (back == window or m[i] <= window)
+        cleared.run().check()
+        if back == window:
+            for i in range(4):
+                ref, _, size, vmax = chain.reference(i)
+                rows = slice(chain.off[i], chain.off[i + 1])
+                assert close(cleared.out[rows], ref, row_error(chain.lens[i], 128, size, vmax) + 2.0 ** -20 * vmax + chain.rounded, bf)[0], i
