@@ -570,3 +570,40 @@ def test_a_window_and_a_mask(window):
                 ref, _, size, vmax = chain.reference(i)
                 rows = slice(chain.off[i], chain.off[i + 1])
                 assert close(cleared.out[rows], ref, row_error(chain.lens[i], 128, size, vmax) + 2.0 ** -20 * vmax + chain.rounded, bf)[0], i
+
+
+@pytest.mark.parametrize("D,T", [(64, 16), (64, 64), (128, 16), (128, 32), (128, 64), (256, 16), (256, 64)])
+@pytest.mark.parametrize("arenas", ["both", "first", "second"])
+def test_bad_entries_give_what_blocks_of_zeros_give(D, T, arenas):
+    """Entries just and far outside either arena, or of one that the cache does not have, in the context, before a step's end and among the
+    new tokens: as if there were a block of zeros."""
+    c = Case([700, 50, 3 * T - 2], [4, 5, 9], 2, 4, D, T, BF, lent=0.5 if arenas == "both" else 0.0, seed=T, kind="any")
+    zero = next(x for x in range(c.local.shape[0]) if x not in set(c.table_np.flatten().tolist()))
+    c.local[zero] = 0.0
+    if arenas == "second":
+        c.local, c.lent = None, c.local
+        held = c.table_np < 0x7fffffff
+        c.table_np[held] = ~c.table_np[held]
+        c.tables.copy_(torch.from_numpy(c.table_np).to(torch.int32))
+        c.cache = B.PagedCache(None, c.lent)
+    n0, n1 = (0 if a is None else a.shape[0] for a in (c.local, c.lent))
+    bad = [n0, n0 + 1, 2 ** 31 - 1, ~n1, ~(n1 + 1), -2 ** 31]
+    last = (c.lens[0] - 1) // T
+    cells = [(0, x % last) for x in (0, 3, 5, 7, 9)] + [(0, last), (2, 1), (2, 3)]
+    for x, (i, j) in enumerate(cells):
+        c.tables[i, j] = bad[x % len(bad)]
+        c.table_np[i, j] = ~zero if arenas == "second" else zero
+    c.run(status=-1).check()
+
+
+def test_positions_outside_the_request_give_what_its_first_and_last_give():
+    c = Case([300, 20], [6, 5], 2, 2, 128, 16, BF, kind="tree", window=40, positions=True)
+    given = [-5, 2 ** 31 - 1, 303, 306, 299, 305, 10 ** 6, -2 ** 31, 22, 25, 19]
+    first = [c.ctx[0]] * 6 + [c.ctx[1]] * 5
+    last = [305] * 6 + [24] * 5
+    outs = []
+    for pos in (given, [min(max(x, a), b) for x, a, b in zip(given, first, last)]):
+        c.positions[:11] = gpu(pos)
+        c.pos = [[min(max(x, 300), 305) for x in pos[:6]], [min(max(x, 20), 24) for x in pos[6:]]]
+        outs.append(c.run().check().out.clone())
+    assert torch.equal(*outs)
