@@ -70,3 +70,24 @@ def test_device_driven_kernels_fit_their_cta_and_do_not_spill():
     for name, r in others.items():
         assert r["stack"] == r["spill_stores"] == r["spill_loads"] == 0, (name, r)
         assert r["registers"] <= (64 if "write_kv" in name else 128), (name, r)   # four CTAs of 256 threads; one of 512
+
+
+def test_kernels_of_several_new_tokens_and_shared_blocks():
+    """paged_tree_kernel moves registers between its warps by setmaxnreg: 168 for the eight softmax warps and 88 for the others are what 512
+    threads of 128 have. Launched with fewer, the request for more would wait for good, so the number is exact."""
+    res = build_mod.kernel_resources()
+    tree = {k: v for k, v in res.items() if "paged_tree_kernel" in k}
+    assert len(tree) == 6, sorted(res)                    # heads of 64 / 128 / 256 x bf16 / fp16
+    for name, r in tree.items():
+        assert r["registers"] == 128 and r["stack"] == r["spill_stores"] == r["spill_loads"] == 0, (name, r)
+    join = {k: v for k, v in res.items() if "tree_join_kernel" in k}
+    assert len(join) == 6, sorted(res)
+    for name, r in join.items():                          # three CTAs of 256 threads to an SM
+        assert r["registers"] * 256 * 3 <= 65536 and r["stack"] == r["spill_stores"] == r["spill_loads"] == 0, (name, r)
+    # CTAs of 512 threads (two to an SM of the kernel that rewrites cells), of 256 (four) and of 128 (eight)
+    for part, most in (("free_kernel", 128), ("fork_kernel", 128), ("compact_plan_kernel", 128), ("compact_cells_kernel", 64), ("copy_rows_kernel", 64),
+                       ("keep_rows_kernel", 64)):
+        found = [(k, v) for k, v in res.items() if part in k]
+        assert len(found) == 1, (part, sorted(res))
+        for name, r in found:                             # (8 bytes of stack: the two arenas' limits, indexed by an entry's arena)
+            assert r["registers"] <= most and r["stack"] <= 8 and r["spill_stores"] == r["spill_loads"] == 0, (name, r)
