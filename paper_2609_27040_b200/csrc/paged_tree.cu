@@ -17,9 +17,9 @@
 //   * Weights take the place of their scores in tensor memory. Where a request's rows of a KV head are one tile (drafted tokens, which are compared
 //     with and go on as single tokens; bound by HBM), they are the sum of two 16-bit numbers (error 2^-16 for bf16), as in attention of single tokens.
 //     Where they are more (prompts; bound by the products and the softmax), a weight is one rounded number, which adds an error as large as the
-//     output's own rounding. One number or two: 64 requests with 24 tokens each 129 / 134 us, outputs off by 0.0023 / 0.0017 of their size (their own
-//     rounding is 0.0017); 200 with up to 9 tokens and a window 219 / 251; 8 pieces of prompts 910 / 1066, five long requests of two tiles 779 / 936.
-//     Sums of weights are taken before the rounding, in f32.
+//     output's own rounding. One number / two: 64 requests with 24 tokens each 129 / 134 us (145 / 167 one call after the other, at the clocks that
+//     power leaves), outputs off by 0.0023 / 0.0017 of their size (their own rounding is 0.0017); 200 with up to 9 tokens and a window 219 / 251; 8
+//     pieces of prompts 910 / 1066, five long requests of two tiles 779 / 936. Sums of weights are taken before the rounding, in f32.
 //   * O is rescaled only when a row's maximum has grown by more than 2^kSlack; until then weights are larger than 1.
 #include <cuda.h>
 #include <cuda_bf16.h>
@@ -40,7 +40,8 @@ constexpr float kMinusInf = -INFINITY;
 // Warps: one that issues the products, two that copy (and an idle one), two groups of four for the softmax, four that write rows out.
 constexpr uint32_t kThreads = 512, kIssueWarp = 0, kFeedWarp = 1, kSoftWarp = 4, kOutWarp = 12;
 constexpr uint32_t kNotes = 4;
-// Registers of a thread: the launch has 128 for everybody; the last two groups of warps give up what the first two get.
+// Registers of a thread: the launch has 128 for everybody (exactly: with fewer the request for more would not end); the two groups of the softmax
+// get what warps 0 to 3 and those that write out give up.
 constexpr uint32_t kSoftRegs = 168, kOtherRegs = 88;
 static_assert(2 * kSoftRegs + 2 * kOtherRegs <= 4 * 128, "no more than the block was launched with");
 
@@ -687,8 +688,8 @@ __device__ void soften(const TreeParams& p, Control<D>& ctl, uint8_t* slots) {
         }
         wipe = wipe && tile == 0;
       }
-      // Twice over the scores, 32 at a time, the next ones on their way: in registers all at once they and their code, straight
-      // through, took longer to fetch than to run.
+      // Twice over the scores, 32 at a time, each load waited for: in registers all at once they and their code, straight
+      // through, took longer to fetch than to run, and a second buffer of 32 spilled.
       float mx[4] = {kMinusInf, kMinusInf, kMinusInf, kMinusInf};
 #pragma unroll 1
       for (uint32_t w = 0; w < words; ++w) {
@@ -1187,7 +1188,7 @@ cudaError_t launch(const TreeParams& p, const Maps& maps, uint32_t grid, int dev
   }
   const cudaError_t e = launch_ahead(paged_tree_kernel<D, kBf16>, grid, kThreads, kSharedBytes, stream, p, maps);
   if (e != cudaSuccess) return e;
-  // Three CTAs of the join fit an SM (with two: 64 requests with 24 tokens each 130 us, now 125).
+  // Three CTAs of the join fit an SM. Two / three: 64 requests with 24 tokens each 146 / 140 us, with heads of 256 140 / 134, one of 8000 tokens 29.4 / 31.5.
   return launch_ahead(tree_join_kernel<D, kBf16>, grid * 3, kJoinThreads, 0, stream, p, grid);
 }
 
